@@ -78,7 +78,11 @@ typedef enum {
     FLOE_KERNEL_GATE_DOWN = 5,
     FLOE_KERNEL_COMBINE = 6,
     FLOE_KERNEL_STAGE = 7,
-    FLOE_KERNEL_FUSED_FFN = 8 /* (router +) up GEMV + selection + gate/down of small batches, one kernel */
+    FLOE_KERNEL_FUSED_FFN = 8, /* (router +) up GEMV + selection + gate/down of small batches, one kernel */
+    FLOE_KERNEL_KV_APPEND = 9,
+    FLOE_KERNEL_KV_GATHER = 10,
+    FLOE_KERNEL_KV_ATTENTION = 11,
+    FLOE_KERNEL_KV_JOIN = 12 /* partial results of one sequence's tokens, where the attention was split over them */
 } floe_kernel_id;
 int floe_profile_kernel(int kernel_id, void* start_event, void* stop_event);
 
@@ -393,6 +397,103 @@ int floe_moe_layer_decode_cached(const floe_layer* L, const floe_channel_cache* 
  */
 int floe_stage_channels(const floe_half* host_gd, int d, int f, const int32_t* idx, const int32_t* count,
                         int capacity_rows, floe_half* hbm_dst, int32_t* overflow, void* side_stream, void* done);
+
+/* ------------------------------------------------------------------------------------------------
+ * Attention in front of the MoE layer, on a paged cache of keys and values held in 8 bits.
+ *
+ * A page holds `block` tokens.  Per page and KV head: the codes of K, those of V, and one binary32 scale for each; a value is
+ * code * scale.  Codes are int8 (largest 127) or e4m3 (largest 448).
+ *   k  dev uint8 [n_pages][kv_heads][block][head_dim]
+ *   v  dev uint8 [n_pages][kv_heads][block / 32][head_dim / 2][4 g][2 dim % 2][2 tile][4 i],  token = 32 group + 16 tile + 4 g + i
+ *      (the eight tokens that a lane of the matrix cores multiplies lie next to each other)
+ *   k_scale, v_scale  dev float [n_pages][kv_heads]
+ * Supported: head_dim in {64, 128, 192, 256}; block in {32, 64, 128}; kv_heads <= 256; n_pages >= 1.  k and v 16-byte aligned.
+ * Nothing has to be initialised: a block is opened by the append that writes its first token.
+ *
+ * The rows of a call belong to sequences: sequence s has rows cu_rows[s] .. cu_rows[s + 1) of the call's tensors (possibly none) and a
+ * length.  Token t of a sequence lies in page block_table[s][t / block] at place t % block.  What the device arrays say is never
+ * trusted with an address: a table entry outside [0, n_pages) or a block behind max_blocks is an absent page (nothing is written
+ * to it, its tokens are left out of the attention and read back as zeros), rows outside [0, n_rows) are not touched, and rows of
+ * a sequence behind its first max_rows are left out.  Tables of different sequences may name the same page for reading; an append must be
+ * the only one that writes to a page.
+ */
+typedef enum { FLOE_FP16 = 0, FLOE_BF16 = 1 } floe_dtype;
+typedef enum { FLOE_KV_INT8 = 0, FLOE_KV_E4M3 = 1 } floe_kv_format;
+
+typedef struct {
+    int32_t n_pages, kv_heads, head_dim, block;
+    int32_t format; /* floe_kv_format */
+    int32_t dtype;  /* floe_dtype of the 16-bit tensors of every call on this cache */
+    uint8_t* k;
+    uint8_t* v;
+    float* k_scale;
+    float* v_scale;
+} floe_kv_cache;
+
+typedef struct {
+    int32_t n_seqs, n_rows; /* 0 <= n_seqs <= 65535; n_rows: rows of the call's tensors */
+    int32_t max_rows;       /* at least the rows of any sequence (host side: it sizes the launches) */
+    int32_t max_blocks;     /* width of block_table */
+    const int32_t* cu_rows;     /* dev [n_seqs + 1], ascending */
+    const int32_t* len;         /* dev [n_seqs]; meaning per call */
+    const int32_t* block_table; /* dev [n_seqs][max_blocks] */
+} floe_kv_seqs;
+
+/*
+ * Rotary positions: dims (i, rot_dim/2 + i), or (2 i, 2 i + 1) when interleaved, of the first rot_dim dims of a head are turned by
+ * table[position][i] = (cos, sin):  a' = a cos - b sin, b' = b cos + a sin, binary32, one rounding per operation.
+ * rot_dim: a multiple of 16, at most head_dim.  table dev float [n_positions][rot_dim / 2][2], 16-byte aligned.  positions dev int32
+ * [n_rows], or NULL: a row's place in its sequence.  A row whose position lies outside the table becomes NaN.
+ */
+typedef struct {
+    const float* table;
+    const int32_t* positions;
+    int32_t n_positions, rot_dim, interleaved;
+} floe_rope;
+/* table[p][i] = (cos, sin) of p * base^(-2 i / rot_dim), formed in binary64 and rounded once. */
+int floe_rope_table(float* table, int n_positions, int rot_dim, double base, void* stream);
+
+/*
+ * Appends the call's rows behind the first len[s] tokens of every sequence, with the rotation applied to K (and to Q) on the way.
+ *   need = max(largest |x| of the rows that this call brings to the block / largest code, 2^-60)       (x: K after the rotation, V)
+ *   a block whose first token is among them is opened: scale = need.  Otherwise scale *= 2^k with the least k >= 0 that reaches need,
+ *   and the block's older codes become round(code * 2^-k);  new codes are round(x / scale), cut to the largest code.
+ * binary32, one rounding per operation, round = ties to even: the result is defined bit for bit.  A block that takes an infinity or a
+ * NaN has the scale NaN until it is opened again, and attention over any token of it (of its K or its V) gives out and lse NaN.
+ * k, v dev 16-bit [n_rows] rows of [kv_heads][head_dim], k_stride / v_stride elements from row to row (multiples of 8; the three may
+ * be views of one projection's output).  q (or NULL) dev [n_rows] rows of [q_heads][head_dim]: its rotated values, rounded once, go to
+ * q_out dev [n_rows][q_heads][head_dim] (which may not overlap the inputs).  rope: NULL = no rotation (q must be NULL then).
+ * Rows of no sequence are left alone.  len is not changed.  One launch, no workspace.
+ */
+int floe_kv_append(const floe_kv_cache* c, const floe_kv_seqs* s, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                   const void* q, int64_t q_stride, int q_heads, void* q_out, const floe_rope* rope, void* stream);
+
+/*
+ * Reads tokens back: row cu_rows[s] + i is token len[s] + i of sequence s (here len is the first token to read), K and V as 16-bit
+ * values code * scale, rounded once.  k_out, v_out dev [n_rows][kv_heads][head_dim], 16-byte aligned.
+ */
+int floe_kv_gather(const floe_kv_cache* c, const floe_kv_seqs* s, void* k_out, void* v_out, void* stream);
+
+/*
+ * Attention of the call's rows over the cache: row i of a sequence with n rows sits at position len[s] - n + i (len: all tokens of the
+ * sequence, those of the rows among them) and sees
+ *   keys j <= its position (causal) or all j < len[s];  with window > 0 only j > position - window
+ * Query head h reads KV head h / (q_heads / kv_heads).  out[row][h] = softmax(scale q.K) V, fp32 statistics and sums, rounded once;
+ * lse[row][h] (dev float, or NULL) = log of the sum of exp(scale q.K).  A row that sees no key: out 0, lse -infinity.
+ * q dev 16-bit, q_stride elements from row to row (a multiple of 8), heads contiguous; out dev [n_rows][q_heads][head_dim]; both 16-byte
+ * aligned.  max_len: at least every len (host side).  It only chooses between kernels: results agree to rounding whatever it says.
+ * workspace: dev, 256-byte aligned, floe_kv_attention_workspace_bytes(); contents are scratch.
+ */
+typedef struct {
+    int32_t q_heads;
+    int32_t causal;
+    int32_t window; /* 0: none */
+    int32_t max_len;
+    float scale;
+} floe_attention;
+size_t floe_kv_attention_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a);
+int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, const void* q, int64_t q_stride, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

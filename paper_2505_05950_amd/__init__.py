@@ -14,4 +14,5 @@ from .binding import (  # noqa: F401
     words_per_channel, SLOT_STAT_DTYPE, floe_profile_kernel, KERNEL_IDS, floe_tuning, TUNE_UNION_KERNELS, TUNE_STAGE_WORKGROUPS, TUNE_GROUPED_GEMV, TUNE_FUSED_TASKS,
     ChannelCache, floe_channel_cache_load, floe_moe_layer_decode_cached,
     floe_expert_ffn_sparsified, SPARSIFY_UP, SPARSIFY_GATE, SPARSIFY_DOWN,
+    KVCache, Rope, KV_INT8, KV_E4M3, floe_rope_table, floe_kv_append, floe_kv_gather, floe_kv_attention,
 )

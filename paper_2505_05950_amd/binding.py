@@ -66,6 +66,26 @@ class _ChannelCache(C.Structure):
     _fields_ = [("pool", C.c_void_p), ("row_of", C.c_void_p), ("resident_rows", C.c_int32), ("capacity_rows", C.c_int32)]
 
 
+class _KvCache(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block", C.c_int32),
+                ("format", C.c_int32), ("dtype", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
+class _KvSeqs(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32), ("max_blocks", C.c_int32),
+                ("cu_rows", C.c_void_p), ("len", C.c_void_p), ("block_table", C.c_void_p)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_void_p), ("n_positions", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("q_heads", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32), ("max_len", C.c_int32), ("scale", C.c_float)]
+
+
 def lib_path() -> str:
     return os.path.join(_HERE, _LIB_NAME)
 
@@ -113,6 +133,13 @@ def load():
     lib.floe_moe_layer_decode_cached.argtypes = [C.POINTER(_Layer), C.POINTER(_ChannelCache), C.POINTER(_MissPath), vp, i32,
                                                  vp, vp, vp, vp, sz, vp]
     lib.floe_stage_channels.argtypes = [vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
+    i64, kv, seqs, attn = C.c_int64, C.POINTER(_KvCache), C.POINTER(_KvSeqs), C.POINTER(_Attention)
+    lib.floe_rope_table.argtypes = [vp, i32, i32, C.c_double, vp]
+    lib.floe_kv_append.argtypes = [kv, seqs, vp, i64, vp, i64, vp, i64, i32, vp, C.POINTER(_Rope), vp]
+    lib.floe_kv_gather.argtypes = [kv, seqs, vp, vp, vp]
+    lib.floe_kv_attention_workspace_bytes.restype = sz
+    lib.floe_kv_attention_workspace_bytes.argtypes = [kv, seqs, attn]
+    lib.floe_kv_attention.argtypes = [kv, seqs, attn, vp, i64, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -122,7 +149,7 @@ def floe_status_string(status: int) -> str:
 
 
 KERNEL_IDS = {"none": 0, "quantize": 1, "router": 2, "up_gemv": 3, "select": 4, "gate_down": 5, "combine": 6, "stage": 7,
-              "fused_ffn": 8}
+              "fused_ffn": 8, "kv_append": 9, "kv_gather": 10, "kv_attention": 11, "kv_join": 12}
 
 
 def floe_profile_kernel(kernel: str, start_event=None, stop_event=None):
@@ -494,3 +521,141 @@ def floe_stage_channels(host_gd: torch.Tensor, idx, count, capacity_rows: int, h
     _check(load().floe_stage_channels(C.c_void_p(host_gd.data_ptr()), d, f, _ptr(idx), _ptr(count), int(capacity_rows),
                                       _ptr(hbm_dst), _ptr(overflow), _stream(side_stream), ev), "floe_stage_channels")
     return hbm_dst
+
+
+# ---- attention in front of the MoE layer: the paged cache in 8 bits (layout and arithmetic in include/floe.h)
+KV_INT8, KV_E4M3 = 0, 1
+_KV_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+class KVCache:
+    """Pages of `block` tokens: codes of K and V (uint8) and one fp32 scale per page and head for each.  tensors=(k, v, k_scale,
+    v_scale) wraps arrays that exist; otherwise they are allocated (and need no initialising).  dtype: of the 16-bit tensors of the calls."""
+
+    def __init__(self, n_pages: int, kv_heads: int, head_dim: int, block: int = 64, fmt: int = KV_INT8, dtype=torch.float16,
+                 device="cuda", tensors=None):
+        self.n_pages, self.kv_heads, self.head_dim, self.block = int(n_pages), int(kv_heads), int(head_dim), int(block)
+        self.fmt, self.dtype = int(fmt), dtype
+        if dtype not in _KV_DTYPES:
+            raise ValueError(f"KVCache: dtype is torch.float16 or torch.bfloat16, not {dtype}")
+        n = self.n_pages * self.kv_heads
+        if tensors is None:
+            codes = [torch.empty((self.n_pages, self.kv_heads, self.block, self.head_dim), dtype=torch.uint8, device=device) for _ in range(2)]
+            tensors = (*codes, *(torch.empty((self.n_pages, self.kv_heads), dtype=torch.float32, device=device) for _ in range(2)))
+        self.k, self.v, self.k_scale, self.v_scale = tensors
+        for t, size, kind in ((self.k, n * self.block * self.head_dim, torch.uint8), (self.v, n * self.block * self.head_dim, torch.uint8),
+                              (self.k_scale, n, torch.float32), (self.v_scale, n, torch.float32)):
+            if t.numel() != size or t.dtype != kind or not t.is_contiguous():
+                raise ValueError(f"KVCache: expected a contiguous {kind} tensor of {size} elements, got {t.dtype} {tuple(t.shape)}")
+        self._c = _KvCache(self.n_pages, self.kv_heads, self.head_dim, self.block, self.fmt, _KV_DTYPES[dtype], self.k.data_ptr(),
+                           self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
+        self._ws = {}
+
+    def workspace(self, nbytes: int) -> torch.Tensor:
+        """Scratch of the attention calls on the current stream (one array per stream: calls on one stream are ordered)."""
+        key = _stream(None)
+        ws = self._ws.get(key)
+        if ws is None or ws.numel() < nbytes + 256:
+            ws = self._ws[key] = _workspace(nbytes, self.k.device)
+        return ws
+
+
+class Rope:
+    """The rotation that an append applies: table fp32 [positions][rot_dim / 2][2] of (cos, sin)."""
+
+    def __init__(self, table: torch.Tensor, interleaved: bool = False):
+        if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+            raise ValueError("Rope: table is a contiguous fp32 tensor [positions][rot_dim / 2][2]")
+        self.table, self.interleaved = table, bool(interleaved)
+        self.n_positions, self.rot_dim = int(table.shape[0]), 2 * int(table.shape[1])
+
+
+def floe_rope_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
+    table = torch.empty((int(n_positions), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
+    _check(load().floe_rope_table(_ptr(table), int(n_positions), int(rot_dim), float(base), _stream(stream)), "floe_rope_table")
+    return table
+
+
+def _kv_seqs(cu_rows, length, block_table, n_rows, max_rows) -> _KvSeqs:
+    n = cu_rows.shape[0] - 1
+    for t in (cu_rows, length, block_table):
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise ValueError("cu_rows, lengths and block_table are contiguous int32 tensors")
+    if length.shape[0] != n or block_table.dim() != 2 or block_table.shape[0] != n:
+        raise ValueError(f"{n} sequences in cu_rows, {tuple(length.shape)} lengths, block_table {tuple(block_table.shape)}")
+    return _KvSeqs(n, int(n_rows), int(max_rows), block_table.shape[1], cu_rows.data_ptr(), length.data_ptr(), block_table.data_ptr())
+
+
+def _kv_rows(t, cache: KVCache, heads, name: str, n_rows=None):
+    """A 16-bit tensor [rows][heads][head_dim] whose rows may lie anywhere: its row stride."""
+    if t.dtype != cache.dtype or t.dim() != 3 or t.shape[2] != cache.head_dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name}: expected {cache.dtype} [rows][{'heads' if heads is None else heads}][{cache.head_dim}], got {t.dtype} {tuple(t.shape)}")
+    if n_rows is not None and t.shape[0] != n_rows:
+        raise ValueError(f"{name}: {t.shape[0]} rows, expected {n_rows}")
+    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != cache.head_dim)):
+        raise ValueError(f"{name}: the heads of a row lie one behind the other (strides {t.stride()})")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * cache.head_dim
+
+
+def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows: int, q=None, rope: Rope = None, positions=None,
+                   q_out=None, stream=None):
+    """Appends k, v [rows][kv_heads][head_dim] behind the first length[s] tokens of each sequence; rope turns k, and q
+    [rows][q_heads][head_dim] into q_out, which is returned (None without q).  max_rows: at least the rows of any sequence."""
+    n_rows = k.shape[0]
+    ks, vs = _kv_rows(k, cache, cache.kv_heads, "k"), _kv_rows(v, cache, cache.kv_heads, "v", n_rows)
+    qs, heads = 0, 0
+    if q is not None:
+        qs, heads = _kv_rows(q, cache, None, "q", n_rows), q.shape[1]
+        if q_out is None:
+            q_out = torch.empty((n_rows, heads, cache.head_dim), dtype=cache.dtype, device=q.device)
+        elif tuple(q_out.shape) != (n_rows, heads, cache.head_dim) or q_out.dtype != cache.dtype or not q_out.is_contiguous():
+            raise ValueError(f"q_out: expected a contiguous {cache.dtype} tensor {(n_rows, heads, cache.head_dim)}")
+    if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n_rows,) or not positions.is_contiguous()):
+        raise ValueError(f"positions: expected contiguous int32 [{n_rows}]")
+    s = _kv_seqs(cu_rows, length, block_table, n_rows, max_rows)
+    r = None if rope is None else _Rope(rope.table.data_ptr(), None if positions is None else positions.data_ptr(), rope.n_positions,
+                                        rope.rot_dim, rope.interleaved)
+    _check(load().floe_kv_append(cache._c, s, k.data_ptr(), ks, v.data_ptr(), vs, None if q is None else q.data_ptr(), qs, heads,
+                                 None if q is None else q_out.data_ptr(), r, _stream(stream)), "floe_kv_append")
+    return q_out if q is not None else None
+
+
+def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max_rows: int, k_out=None, v_out=None, stream=None):
+    """Rows cu_rows[s] .. cu_rows[s + 1) are tokens first[s], first[s] + 1, ... of sequence s: (k, v) 16-bit [n_rows][kv_heads][head_dim]."""
+    shape = (int(n_rows), cache.kv_heads, cache.head_dim)
+    out = [torch.empty(shape, dtype=cache.dtype, device=cache.k.device) if t is None else t for t in (k_out, v_out)]
+    for t in out:
+        if tuple(t.shape) != shape or t.dtype != cache.dtype or not t.is_contiguous():
+            raise ValueError(f"floe_kv_gather: outputs are contiguous {cache.dtype} tensors {shape}")
+    s = _kv_seqs(cu_rows, first, block_table, n_rows, max_rows)
+    _check(load().floe_kv_gather(cache._c, s, out[0].data_ptr(), out[1].data_ptr(), _stream(stream)), "floe_kv_gather")
+    return out[0], out[1]
+
+
+def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows: int, max_len: int, scale: float = None,
+                      causal: bool = True, window: int = 0, want_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
+    """Attention of q [rows][q_heads][head_dim] over the cache; length[s] counts the rows' own tokens.  Returns out, or (out, lse) with
+    want_lse.  scale: 1 / sqrt(head_dim) by default.  workspace: the cache's own (one per stream) unless handed over."""
+    qs, (n_rows, heads) = _kv_rows(q, cache, None, "q"), q.shape[:2]
+    if out is None:
+        out = torch.empty((n_rows, heads, cache.head_dim), dtype=cache.dtype, device=q.device)
+    elif tuple(out.shape) != tuple(q.shape) or out.dtype != cache.dtype or not out.is_contiguous():
+        raise ValueError(f"floe_kv_attention: out is a contiguous {cache.dtype} tensor {tuple(q.shape)}")
+    if want_lse and lse is None:
+        lse = torch.empty((n_rows, heads), dtype=torch.float32, device=q.device)
+    if lse is not None and (tuple(lse.shape) != (n_rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise ValueError(f"floe_kv_attention: lse is a contiguous fp32 tensor {(n_rows, heads)}")
+    s = _kv_seqs(cu_rows, length, block_table, n_rows, max_rows)
+    a = _Attention(heads, int(causal), int(window), int(max_len), cache.head_dim ** -0.5 if scale is None else float(scale))
+    lib = load()
+    if workspace is None:
+        nbytes = lib.floe_kv_attention_workspace_bytes(cache._c, s, a)
+        if stream is None or stream == torch.cuda.current_stream():
+            workspace = cache.workspace(nbytes)
+        else:
+            with torch.cuda.stream(stream):
+                workspace = cache.workspace(nbytes)
+    wp, wn = _aligned_ptr(workspace)
+    _check(lib.floe_kv_attention(cache._c, s, a, q.data_ptr(), qs, out.data_ptr(), None if lse is None else lse.data_ptr(), wp, wn,
+                                 _stream(stream)), "floe_kv_attention")
+    return (out, lse) if lse is not None else out

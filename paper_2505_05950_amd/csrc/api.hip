@@ -7,6 +7,7 @@
 
 #include <vector>
 
+#include "host_call.h"
 #include "launch.h"
 
 using namespace floe;
@@ -15,48 +16,6 @@ static_assert(sizeof(floe_slot_stat) == sizeof(SlotStat), "stat record layout");
 static_assert(sizeof(DevExpert) == 32, "expert table entry");
 
 namespace {
-
-thread_local int g_last_hip_error = 0;
-
-int hip_fail(hipError_t e) {
-    g_last_hip_error = (int)e;
-    return FLOE_EHIP;
-}
-
-#define FLOE_HIP(call)                             \
-    do {                                           \
-        hipError_t e__ = (call);                   \
-        if (e__ != hipSuccess) return hip_fail(e__); \
-    } while (0)
-
-// Optional measurement hook: when armed for kernel `id`, the next launches of that kernel are bracketed
-// by the two events on the launch stream (see floe_profile_kernel in floe.h).
-struct ProfileHook {
-    int id = 0;
-    hipEvent_t start = nullptr, stop = nullptr;
-};
-thread_local ProfileHook g_hook;
-
-struct Bracket {
-    bool on;
-    hipStream_t st;
-    Bracket(int id, hipStream_t s) : on(g_hook.id == id && g_hook.start && g_hook.stop), st(s) {
-        if (on) (void)hipEventRecord(g_hook.start, st);
-    }
-    ~Bracket() {
-        if (on) (void)hipEventRecord(g_hook.stop, st);
-    }
-};
-
-#define FLOE_LAUNCH(id, stream, call) \
-    do {                              \
-        Bracket br__((id), (stream)); \
-        FLOE_HIP(call);               \
-    } while (0)
-
-constexpr size_t kAlign = 256;
-size_t align_up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 int check_shape(const floe_shape* s) {
     if (!s) return FLOE_EINVAL;
@@ -377,7 +336,7 @@ int floe_last_hip_error(void) { return g_last_hip_error; }
 int floe_abi_version(void) { return 4; }
 
 int floe_profile_kernel(int kernel_id, void* start_event, void* stop_event) {
-    if (kernel_id < 0 || kernel_id > FLOE_KERNEL_FUSED_FFN) return FLOE_EINVAL;
+    if (kernel_id < 0 || kernel_id > FLOE_KERNEL_KV_JOIN) return FLOE_EINVAL;
     if (kernel_id != 0 && (!start_event || !stop_event)) return FLOE_EINVAL;
     g_hook.id = kernel_id;
     g_hook.start = (hipEvent_t)start_event;

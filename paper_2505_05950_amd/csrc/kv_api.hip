@@ -1,0 +1,176 @@
+// C entry points of the paged 8-bit cache (declared in include/floe.h): argument checks, workspace, launches.
+#include "host_call.h"
+#include "kv_launch.h"
+
+using namespace floe;
+
+namespace {
+
+constexpr int64_t kMaxGrid = (1 << 24) - 1;  // workgroups of 256 threads along one axis
+
+int check_cache(const floe_kv_cache* c) {
+    if (!c || c->n_pages <= 0 || c->kv_heads <= 0 || !c->k || !c->v || !c->k_scale || !c->v_scale) return FLOE_EINVAL;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return FLOE_EINVAL;
+    if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 192 && c->head_dim != 256) return FLOE_EUNSUPPORTED;
+    if (c->block != 32 && c->block != 64 && c->block != 128) return FLOE_EUNSUPPORTED;
+    if (c->kv_heads > 256) return FLOE_EUNSUPPORTED;
+    if (c->format != FLOE_KV_INT8 && c->format != FLOE_KV_E4M3) return FLOE_EUNSUPPORTED;
+    if (c->dtype != FLOE_FP16 && c->dtype != FLOE_BF16) return FLOE_EUNSUPPORTED;
+    return FLOE_OK;
+}
+int check_seqs(const floe_kv_seqs* s) {
+    if (!s || s->n_seqs < 0 || s->n_rows < 0 || s->max_rows < 0 || s->max_blocks < 0) return FLOE_EINVAL;
+    if (s->n_seqs > 65535 || s->n_rows > (1 << 24) || s->max_blocks > (1 << 24)) return FLOE_EUNSUPPORTED;
+    return FLOE_OK;
+}
+bool nothing(const floe_kv_seqs* s) { return s->n_seqs == 0 || s->n_rows == 0 || s->max_rows == 0; }
+int check_arrays(const floe_kv_seqs* s) {
+    if (!s->cu_rows || !s->len || s->max_blocks == 0 || !s->block_table) return FLOE_EINVAL;
+    return aligned(s->cu_rows, 4) && aligned(s->len, 4) && aligned(s->block_table, 4) ? FLOE_OK : FLOE_EINVAL;
+}
+KvCache dev_cache(const floe_kv_cache* c) {
+    return KvCache{c->k, c->v, c->k_scale, c->v_scale, c->n_pages, c->kv_heads, c->head_dim, c->block};
+}
+KvSeqs dev_seqs(const floe_kv_seqs* s) {
+    const int max_rows = s->max_rows < s->n_rows ? s->max_rows : s->n_rows;
+    return KvSeqs{s->cu_rows, s->len, s->block_table, s->n_seqs, s->n_rows, max_rows, s->max_blocks};
+}
+int64_t block_tasks(const floe_kv_cache* c, const KvSeqs& s) {
+    return (int64_t)s.n_seqs * kv_blocks_per_seq(s.max_rows, c->block) * c->kv_heads * 2;
+}
+
+int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
+    int rc = check_cache(c);
+    if (rc) return rc;
+    if ((rc = check_seqs(s))) return rc;
+    if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0) return FLOE_EINVAL;
+    if (a->q_heads % c->kv_heads != 0) return FLOE_ESHAPE;
+    if (a->q_heads > 1024 || a->window > kKvMaxLen) return FLOE_EUNSUPPORTED;
+    if ((int64_t)a->q_heads * s->max_rows > kMaxGrid) return FLOE_EUNSUPPORTED;
+    return FLOE_OK;
+}
+// [partial sums][their maxima and sums][plan]
+struct AttnWs {
+    int mt, workgroups;
+    size_t ml_off, plan_off, total;
+};
+AttnWs attn_ws(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
+    AttnWs w;
+    const KvSeqs k = dev_seqs(s);
+    w.mt = kv_rows_tiles_for(c->head_dim, k.max_rows * (a->q_heads / c->kv_heads));
+    w.workgroups = kv_rows_workgroups(c->head_dim, w.mt);
+    const size_t rows = (size_t)2 * w.workgroups * 16 * w.mt;
+    w.ml_off = align_up(rows * c->head_dim * 4);
+    w.plan_off = w.ml_off + align_up(rows * 8);
+    w.total = w.plan_off + align_up(((size_t)s->n_seqs + 2) * 8);
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+int floe_rope_table(float* table, int n_positions, int rot_dim, double base, void* stream) {
+    if (!table || !aligned(table, 16) || n_positions < 0 || rot_dim <= 0 || !(base > 0.0)) return FLOE_EINVAL;
+    if (rot_dim % 16 != 0) return FLOE_ESHAPE;
+    if (rot_dim > 256 || n_positions > (1 << 28)) return FLOE_EUNSUPPORTED;
+    if (n_positions == 0) return FLOE_OK;
+    FLOE_HIP(launch_rope_table(table, n_positions, rot_dim, base, (hipStream_t)stream));
+    return FLOE_OK;
+}
+
+int floe_kv_append(const floe_kv_cache* c, const floe_kv_seqs* s, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                   const void* q, int64_t q_stride, int q_heads, void* q_out, const floe_rope* rope, void* stream) {
+    int rc = check_cache(c);
+    if (rc) return rc;
+    if ((rc = check_seqs(s))) return rc;
+    const int64_t row = (int64_t)c->kv_heads * c->head_dim, limit = (int64_t)1 << 40;
+    if (q_heads < 0 || k_stride < row || v_stride < row || k_stride % 8 || v_stride % 8) return FLOE_EINVAL;
+    if (k_stride > limit || v_stride > limit || q_heads > 1024) return FLOE_EUNSUPPORTED;
+    if (rope) {
+        if (!rope->table || !aligned(rope->table, 16) || rope->n_positions <= 0 || rope->rot_dim <= 0 || !aligned(rope->positions, 4))
+            return FLOE_EINVAL;
+        if (rope->rot_dim % 16 != 0 || rope->rot_dim > c->head_dim) return FLOE_ESHAPE;
+    }
+    if (q) {
+        if (!rope || q_heads == 0 || !q_out || !aligned(q, 16) || !aligned(q_out, 16)) return FLOE_EINVAL;
+        if (q_stride < (int64_t)q_heads * c->head_dim || q_stride % 8) return FLOE_EINVAL;
+        if (q_stride > limit) return FLOE_EUNSUPPORTED;
+    }
+    if (nothing(s)) return FLOE_OK;
+    if ((rc = check_arrays(s))) return rc;
+    if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return FLOE_EINVAL;
+    const KvSeqs ds = dev_seqs(s);
+    const int64_t q_groups = q ? (int64_t)ds.n_rows * ((q_heads * (c->head_dim / 16) + 255) / 256) : 0;
+    if (block_tasks(c, ds) + q_groups > kMaxGrid) return FLOE_EUNSUPPORTED;
+    KvAppendArgs a{};
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.q = static_cast<const uint16_t*>(q);
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_stride = q_stride;
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.q_heads = q_heads;
+    if (rope) a.rope = KvRope{rope->table, rope->positions, rope->n_positions, rope->rot_dim, rope->interleaved != 0};
+    hipStream_t st = (hipStream_t)stream;
+    FLOE_LAUNCH(FLOE_KERNEL_KV_APPEND, st, launch_kv_append(dev_cache(c), ds, a, c->format, c->dtype == FLOE_BF16, st));
+    return FLOE_OK;
+}
+
+int floe_kv_gather(const floe_kv_cache* c, const floe_kv_seqs* s, void* k_out, void* v_out, void* stream) {
+    int rc = check_cache(c);
+    if (rc) return rc;
+    if ((rc = check_seqs(s))) return rc;
+    if (nothing(s)) return FLOE_OK;
+    if ((rc = check_arrays(s))) return rc;
+    if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16)) return FLOE_EINVAL;
+    const KvSeqs ds = dev_seqs(s);
+    if (block_tasks(c, ds) > kMaxGrid) return FLOE_EUNSUPPORTED;
+    hipStream_t st = (hipStream_t)stream;
+    FLOE_LAUNCH(FLOE_KERNEL_KV_GATHER, st,
+                launch_kv_gather(dev_cache(c), ds, static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), c->format,
+                                 c->dtype == FLOE_BF16, st));
+    return FLOE_OK;
+}
+
+size_t floe_kv_attention_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
+    return check_attention(c, s, a) == FLOE_OK ? attn_ws(c, s, a).total : 0;
+}
+
+int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, const void* q, int64_t q_stride, void* out,
+                      float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_attention(c, s, a);
+    if (rc) return rc;
+    if (q_stride < (int64_t)a->q_heads * c->head_dim || q_stride % 8) return FLOE_EINVAL;
+    if (q_stride > (int64_t)1 << 40) return FLOE_EUNSUPPORTED;
+    if (nothing(s)) return FLOE_OK;
+    if ((rc = check_arrays(s))) return rc;
+    if (!q || !out || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, kAlign)) return FLOE_EINVAL;
+    const AttnWs w = attn_ws(c, s, a);
+    if (workspace_bytes < w.total) return FLOE_EWORKSPACE;
+    char* base = static_cast<char*>(workspace);
+    KvAttnArgs k{};
+    k.c = dev_cache(c);
+    k.s = dev_seqs(s);
+    k.q = static_cast<const uint16_t*>(q);
+    k.q_stride = q_stride;
+    k.out = static_cast<uint16_t*>(out);
+    k.lse = lse;
+    k.q_heads = a->q_heads;
+    k.group = a->q_heads / c->kv_heads;
+    k.scale_log2 = a->scale * 1.4426950408889634f;
+    k.causal = a->causal != 0;
+    k.window = a->window;
+    k.bf16 = c->dtype == FLOE_BF16;
+    k.part_o = reinterpret_cast<float*>(base);
+    k.part_ml = reinterpret_cast<float*>(base + w.ml_off);
+    k.plan = reinterpret_cast<int64_t*>(base + w.plan_off);
+    hipStream_t st = (hipStream_t)stream;
+    FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st,
+                c->format == FLOE_KV_INT8 ? launch_kv_rows_int8(k, w.mt, w.workgroups, st) : launch_kv_rows_e4m3(k, w.mt, w.workgroups, st));
+    FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, st));
+    return FLOE_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,30 @@
+// Joins what the shares of the rows kernel left (kv_rows.h).
+#include "kv_rows.h"
+
+namespace floe {
+
+namespace {
+template <int D>
+hipError_t join_tiles(const KvAttnArgs& a, int mt, hipStream_t st) {
+    const dim3 grid(a.q_heads * a.s.max_rows, a.s.n_seqs), wg(256);
+    if constexpr (kv_rows_most_tiles(D) >= 4) {
+        if (mt == 4) return kv_join_kernel<D, 4><<<grid, wg, 0, st>>>(a), hipGetLastError();
+    }
+    if constexpr (kv_rows_most_tiles(D) >= 2) {
+        if (mt == 2) return kv_join_kernel<D, 2><<<grid, wg, 0, st>>>(a), hipGetLastError();
+    }
+    kv_join_kernel<D, 1><<<grid, wg, 0, st>>>(a);
+    return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_kv_join(const KvAttnArgs& a, int mt, hipStream_t st) {
+    switch (a.c.dim) {
+        case 64: return join_tiles<64>(a, mt, st);
+        case 128: return join_tiles<128>(a, mt, st);
+        case 192: return join_tiles<192>(a, mt, st);
+        default: return join_tiles<256>(a, mt, st);
+    }
+}
+
+}  // namespace floe

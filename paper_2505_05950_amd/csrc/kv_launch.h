@@ -1,0 +1,59 @@
+// Launchers of the kernels on the paged 8-bit cache (host side).  Arguments are checked in kv_api.hip before anything is enqueued.
+#pragma once
+
+#include "kv_cache.h"
+#include "launch.h"
+
+namespace floe {
+
+struct KvRope {
+    const float* table;        // [n_positions][rot / 2][2]
+    const int32_t* positions;  // [n_rows] or nullptr: a row's place in its sequence
+    int n_positions, rot, interleaved;
+};
+
+struct KvAppendArgs {
+    const uint16_t *k, *v, *q;
+    int64_t k_stride, v_stride, q_stride;
+    uint16_t* q_out;
+    int q_heads;
+    KvRope rope;
+    int blocks_per_seq, tasks, q_chunks;  // set by the launcher
+};
+// blocks that `rows` consecutive tokens can touch
+inline int kv_blocks_per_seq(int rows, int block) { return (rows + block - 2) / block + 1; }
+hipError_t launch_kv_append(const KvCache& c, const KvSeqs& s, const KvAppendArgs& a, int format, bool bf16, hipStream_t st);
+hipError_t launch_kv_gather(const KvCache& c, const KvSeqs& s, uint16_t* k_out, uint16_t* v_out, int format, bool bf16, hipStream_t st);
+hipError_t launch_rope_table(float* table, int n_positions, int rot, double base, hipStream_t st);
+
+struct KvAttnArgs {
+    KvCache c;
+    KvSeqs s;  // len: tokens of each sequence, the call's own among them
+    const uint16_t* q;
+    int64_t q_stride;
+    uint16_t* out;
+    float* lse;  // [n_rows][q_heads] or nullptr
+    int q_heads, group;
+    float scale_log2;  // softmax scale * log2(e)
+    int causal, window;
+    bool bf16;
+    // rows kernel (kv_rows.h)
+    float* part_o;   // [slots][16 MT][dim]
+    float* part_ml;  // [slots][16 MT][2]
+    int64_t* plan;   // [n_seqs + 2]: units before each sequence, all units, units per workgroup
+};
+
+constexpr int kKvMinShare = 8;  // units of 32 tokens: two per wave
+// Tiles of sixteen rows that a workgroup of the rows kernel takes at once: as many as its registers hold beside two units of the cache
+constexpr int kv_rows_most_tiles(int dim) { return dim == 64 ? 4 : dim <= 192 ? 2 : 1; }
+inline int kv_rows_tiles_for(int dim, int rows) {
+    const int most = kv_rows_most_tiles(dim), want = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
+    return want < most ? want : most;
+}
+constexpr int kv_rows_wgs_per_cu(int dim, int mt) { return dim * mt <= 128 ? 3 : dim * mt <= 192 ? 2 : 1; }
+inline int kv_rows_workgroups(int dim, int mt) { return num_cus() * kv_rows_wgs_per_cu(dim, mt); }
+hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, int workgroups, hipStream_t st);
+hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, int workgroups, hipStream_t st);
+hipError_t launch_kv_join(const KvAttnArgs& a, int mt, hipStream_t st);
+
+}  // namespace floe

@@ -1,0 +1,433 @@
+// Attention of a few query rows per sequence over the paged 8-bit cache (decoding, drafted tokens, short chunks).
+//
+// Mathematics, for the query rows r = (token, head of the group) that share a KV head:
+//   t_rj = scale * log2(e) * (q_r . kcode_j) * kscale_j + log2(vscale_j)      o_r = sum_j 2^t_rj vcode_j / sum_j 2^(t_rj) / vscale_j
+// i.e. the softmax with the scale of V inside the exponent: codes go to the matrix cores as they are (int8 and e4m3 are exact in
+// fp16), no product with a scale is formed per element, and the largest weight that V is multiplied with is a fixed power of two
+// whatever the scales are.  The running maximum M is that of t, lowered by 14 so that the fp16 weights use the type's range (a weight
+// of 2^-38 of the largest still counts).  Queries in bf16 are scaled per row by a power of two into fp16's range.
+//
+// S^T = K Q^T and O^T = V^T P^T, both as v_mfma_f32_16x16x32_f16: a column is a query row, so its maximum and sum live in the four
+// lanes that hold the column, and the rows of S^T that a lane holds (tokens 4 g + i of two tiles) are exactly the operand of the
+// second product when V is stored in that order: the weights never leave their lane.
+//
+// What bounds it: the bytes of the cache.  All (sequence, KV head, tile of rows) x 32-token units of a call form one line that is
+// cut into equal shares, one per workgroup; a share that ends inside a sequence leaves a partial result, joined by kv_join_kernel.
+// So ragged batches and single long sequences fill the card alike.  The four waves of a workgroup take the units of its share in
+// turn, one unit ahead in registers.
+#pragma once
+
+#include "kv_launch.h"
+
+namespace floe {
+
+constexpr int kRowsWaves = 4;
+constexpr float kWeightBits = 14.0f;
+
+// Units of one sequence: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on.
+struct KvUnits {
+    KvSpan span;
+    int tiles, units, lo;
+    __device__ __forceinline__ int64_t all(int heads) const { return (int64_t)heads * tiles * units; }
+};
+template <int MT>
+__device__ __forceinline__ KvUnits kv_units(const KvAttnArgs& a, int seq) {
+    KvUnits u;
+    u.span = kv_span(a.s, seq);
+    u.tiles = (u.span.rows * a.group + 16 * MT - 1) / (16 * MT);
+    u.lo = a.window > 0 ? max(0, u.span.len - u.span.rows - a.window + 1) & ~(kKvGroup - 1) : 0;
+    u.units = max(1, (u.span.len - u.lo + kKvGroup - 1) / kKvGroup);
+    return u;
+}
+
+template <int N>
+__device__ __forceinline__ int64_t workgroup_scan(int64_t x, int64_t* lds) {  // inclusive, over the N waves of a workgroup
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int64_t y = __shfl_up(x, o, kWave);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) lds[w] = x;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) x += lds[i];
+    return x;
+}
+
+template <int D, int FMT>
+struct KvFrag {  // one unit in registers
+    uint4 k[2 * (D / 64)];
+    uint4 v[D / 32];
+    float ks, vs;
+};
+
+template <int D, int FMT>
+__device__ __forceinline__ void load_unit(KvFrag<D, FMT>& f, const KvCache& c, int head, int page, int token_in_page, int r, int g) {
+    const size_t slot = (size_t)max(page, 0) * c.heads + head;
+    const size_t base = (slot * c.block + token_in_page) * D;  // the same in every lane
+    const unsigned char *k = scalar_ptr(c.k + base), *v = scalar_ptr(c.v + base);
+    const uint32_t k_lane = r * D + 16 * g, v_lane = r * 64 + 16 * g;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < D / 64; ++kk) f.k[t * (D / 64) + kk] = gload16(k + (k_lane + t * 16 * D + kk * 64));
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) f.v[dt] = gload16(v + (v_lane + dt * 1024));
+    f.ks = gloadf(c.k_scale + slot);
+    f.vs = gloadf(c.v_scale + slot);
+}
+
+// One query row's eight halves of a reduction step, in the order in which the codes of K arrive; rows without a query are zero.
+template <int D, int MT>
+struct KvQueries {
+    h16x8 q[MT][D / 32];
+    float unscale[MT];  // what the row was divided by
+};
+template <int D, int MT>
+__device__ __forceinline__ void load_queries(KvQueries<D, MT>& Q, const KvAttnArgs& a, const KvSpan& span, int head, int row0, int r, int g) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int rr = row0 + 16 * m + r;
+        const bool there = rr < span.rows * a.group;
+        const int token = there ? rr / a.group : 0, h = there ? rr - token * a.group : 0;
+        const uint16_t* p = a.q + (span.row0 + token) * a.q_stride + (size_t)(head * a.group + h) * D + 16 * g;
+        Q.unscale[m] = 1.0f;
+        uint4 raw[D / 32];
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) raw[s] = there ? gload16(p + (s >> 1) * 64 + (s & 1) * 8) : make_uint4(0, 0, 0, 0);
+        if (!a.bf16) {
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) Q.q[m][s] = __builtin_bit_cast(h16x8, raw[s]);
+            continue;
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+        }
+        // the largest exponent of the row becomes 14 (2^14 <= largest < 2^15); zeros, infinities and NaN stay as they are
+        const float big = quad_max(bf16_to_f32(top));
+        const int e = (int)(__builtin_bit_cast(uint32_t, big) >> 23) - 127;
+        const int up = (e == 128 || big == 0.0f) ? 0 : min(14 - e, 126);
+        const float f = __builtin_bit_cast(float, (uint32_t)(up + 127) << 23);
+        Q.unscale[m] = __builtin_bit_cast(float, (uint32_t)(127 - up) << 23);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            float x[8];
+            unpack8<true>(raw[s], x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const h16x2 p2 = __builtin_convertvector(f32x2{x[2 * j] * f, x[2 * j + 1] * f}, h16x2);
+                Q.q[m][s][2 * j] = p2.x;
+                Q.q[m][s][2 * j + 1] = p2.y;
+            }
+        }
+    }
+}
+
+// Running state of 16 MT query rows: column r of the tiles, tokens 4 g + i in lane (r, g).
+template <int D, int MT>
+struct KvState {
+    f32x4 o[MT][D / 16];  // O^T: tile dt, parity e: dims 32 dt + 8 g + 2 i + e in o[2 dt + e][i]
+    float top[MT], sum[MT];
+};
+
+template <int D, int FMT, int MT>
+__device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D, MT>& Q, const KvFrag<D, FMT>& f, const KvAttnArgs& a,
+                                          bool mask, int token0, int len, const int* first_key, const int* last_key, int g) {
+    f32x4 s[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) s[m][0] = s[m][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int kk = 0; kk < D / 64; ++kk) {
+            const uint4 c = f.k[t * (D / 64) + kk];
+            const h16x8 k0 = codes_to_h8<FMT>(c.x, c.y), k1 = codes_to_h8<FMT>(c.z, c.w);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                s[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, Q.q[m][2 * kk], s[m][t], 0, 0, 0);
+                s[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, Q.q[m][2 * kk + 1], s[m][t], 0, 0, 0);
+            }
+        }
+    const float lv = __builtin_amdgcn_logf(f.vs), rv = 1.0f / f.vs;
+    h16x8 p[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const float c = a.scale_log2 * Q.unscale[m] * f.ks;
+        float x[8], mx = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(s[m][j >> 2][j & 3], c, lv);
+        if (mask) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int key = token0 + 16 * (j >> 2) + 4 * g + (j & 3);
+                if (key < first_key[m] || key > last_key[m]) x[j] = -__builtin_inff();
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, x[j]);
+        mx = quad_max(mx) - kWeightBits;
+        const float top = fmaxf(st.top[m], mx), base = top == -__builtin_inff() ? 0.0f : top;
+        if (__ballot(top != st.top[m])) {
+            const float shrink = __builtin_amdgcn_exp2f(st.top[m] - base);
+            st.sum[m] *= shrink;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) st.o[m][d] *= shrink;
+            st.top[m] = top;
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = __builtin_amdgcn_exp2f(x[j] - base);
+            sum += x[j];
+        }
+        // (a block whose scale is NaN counts only where something of it is seen)
+        st.sum[m] += sum != 0.0f ? sum * rv : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const h16x2 p2 = __builtin_convertvector(f32x2{x[2 * j], x[2 * j + 1]}, h16x2);
+            p[m][2 * j] = p2.x;
+            p[m][2 * j + 1] = p2.y;
+        }
+    }
+    // codes behind the last token are whatever the page held before (e4m3 has NaN): they become zeros
+    uint4 vc[D / 32];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) vc[dt] = f.v[dt];
+    if (mask) {
+        const int n0 = min(max(len - token0 - 4 * g, 0), 4), n1 = min(max(len - token0 - 16 - 4 * g, 0), 4);
+        const uint32_t keep0 = n0 == 4 ? ~0u : (1u << (8 * n0)) - 1u, keep1 = n1 == 4 ? ~0u : (1u << (8 * n1)) - 1u;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) vc[dt].x &= keep0, vc[dt].y &= keep1, vc[dt].z &= keep0, vc[dt].w &= keep1;
+    }
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) {
+        const uint4 c = vc[dt];
+        const h16x8 v0 = codes_to_h8<FMT>(c.x, c.y), v1 = codes_to_h8<FMT>(c.z, c.w);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            st.o[m][2 * dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[m], st.o[m][2 * dt], 0, 0, 0);
+            st.o[m][2 * dt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[m], st.o[m][2 * dt + 1], 0, 0, 0);
+        }
+    }
+}
+
+__device__ __forceinline__ float weight_of(float top, float all) { return top == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - all); }
+
+// four dims of a finished row
+__device__ __forceinline__ void write_row4(const KvAttnArgs& a, int D, size_t row, int head, int d, f32x4 o, float top, float sum) {
+    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+    uint2 w;
+    if (a.bf16) w = make_uint2(pack16<true>(o[0] * f, o[1] * f), pack16<true>(o[2] * f, o[3] * f));
+    else w = make_uint2(pack16<false>(o[0] * f, o[1] * f), pack16<false>(o[2] * f, o[3] * f));
+    *reinterpret_cast<uint2*>(a.out + (row * a.q_heads + head) * D + d) = w;
+    if (a.lse && d == 0)
+        a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+
+template <int D, int FMT, int MT>
+__global__ __launch_bounds__(64 * kRowsWaves, kv_rows_wgs_per_cu(D, MT)) void kv_rows_kernel(KvAttnArgs a, int64_t min_share) {
+    constexpr int kStride = D + 4;
+    __shared__ float slab[kRowsWaves][16][kStride];
+    __shared__ float ml[kRowsWaves][16 * MT][2];
+    __shared__ int64_t scan_lds[kRowsWaves];
+    __shared__ int64_t found[2];  // units before the sequence, its number
+    __shared__ int64_t carry;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    // ---- the share of this workgroup
+    int64_t sum = 0;
+    for (int s = tid; s < a.s.n_seqs; s += 64 * kRowsWaves) sum += kv_units<MT>(a, s).all(a.c.heads);
+    sum = workgroup_scan<kRowsWaves>(sum, scan_lds);
+    if (tid == 64 * kRowsWaves - 1) found[0] = sum;
+    __syncthreads();
+    const int64_t total = found[0];
+    const int64_t even = (total + gridDim.x - 1) / gridDim.x, share = even > min_share ? even : min_share;
+    const int64_t u0 = blockIdx.x * share, u1 = u0 + share < total ? u0 + share : total;
+    __syncthreads();
+    if (blockIdx.x != 0 && u0 >= total) return;  // the whole workgroup
+    int64_t before = 0;
+    for (int s0 = 0; s0 < a.s.n_seqs; s0 += 64 * kRowsWaves) {
+        const int s = s0 + tid;
+        const int64_t mine = s < a.s.n_seqs ? kv_units<MT>(a, s).all(a.c.heads) : 0;
+        const int64_t upto = before + workgroup_scan<kRowsWaves>(mine, scan_lds);
+        if (u0 >= upto - mine && u0 < upto) {
+            found[0] = upto - mine;
+            found[1] = s;
+        }
+        if (blockIdx.x == 0 && s < a.s.n_seqs) a.plan[s] = upto - mine;
+        if (tid == 64 * kRowsWaves - 1) carry = upto;
+        __syncthreads();
+        before = carry;
+        if (blockIdx.x != 0 && before > u0) break;
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        a.plan[a.s.n_seqs] = total;
+        a.plan[a.s.n_seqs + 1] = share;
+    }
+    if (u0 >= total) return;  // nothing to do at all
+    int seq = __builtin_amdgcn_readfirstlane((int)found[1]);
+    int64_t in_seq = u0 - found[0];
+    // ---- segments: (sequence, KV head, tile of rows)
+    for (int64_t u = u0; u < u1;) {
+        const KvUnits w = kv_units<MT>(a, seq);
+        const int64_t all = w.all(a.c.heads);
+        if (in_seq >= all) {
+            ++seq;
+            in_seq = 0;
+            continue;
+        }
+        const int tile_of_seq = (int)(in_seq / w.units);
+        const int j0 = (int)(in_seq - (int64_t)tile_of_seq * w.units);
+        const int j1 = (int)(w.units - j0 < u1 - u ? w.units : j0 + (u1 - u));
+        const int head = tile_of_seq / w.tiles, row0 = (tile_of_seq - head * w.tiles) * 16 * MT;
+        KvQueries<D, MT> Q;
+        load_queries<D, MT>(Q, a, w.span, head, row0, r, g);
+        KvState<D, MT> st;
+        int first_key[MT], last_key[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            st.top[m] = -__builtin_inff();
+            st.sum[m] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) st.o[m][d] = f32x4{0, 0, 0, 0};
+            const int token = min((row0 + 16 * m + r) / a.group, w.span.rows - 1), pos = w.span.len - w.span.rows + token;
+            first_key[m] = a.window > 0 ? pos - a.window + 1 : 0;
+            last_key[m] = a.causal ? pos : w.span.len - 1;
+        }
+        // units between these need no mask
+        const int pos0 = w.span.len - w.span.rows + row0 / a.group;
+        const int pos1 = w.span.len - w.span.rows + min((row0 + 16 * MT - 1) / a.group, w.span.rows - 1);
+        const int clear_lo = a.window > 0 ? pos1 - a.window + 1 : 0;
+        const int clear_hi = a.causal ? pos0 + 1 : w.span.len;  // first token that some row does not see
+        const int end = a.causal ? pos1 + 1 : w.span.len;       // behind the last token that any row sees
+        const int upb = a.c.block / kKvGroup, unit0 = w.lo / kKvGroup;
+        int pages = -1;
+        auto fetch_pages = [&](int j) {  // pages of this wave's next 64 units
+            const int mine = j + kRowsWaves * lane;
+            pages = mine < j1 ? kv_page(a.s, a.c, seq, (unit0 + mine) / upb) : -1;
+        };
+        auto page_of = [&](int it) { return __builtin_amdgcn_readlane(pages, it & 63); };
+        const int n = (j1 - j0 - wave + kRowsWaves - 1) / kRowsWaves;  // units of this wave (may be none)
+        KvFrag<D, FMT> now, next;
+        int page_now = -1, page_next = -1;
+        auto request = [&](int it, KvFrag<D, FMT>& f) {
+            const int j = j0 + wave + kRowsWaves * it;
+            if ((it & 63) == 0) fetch_pages(j);
+            const int page = w.lo + j * kKvGroup >= end ? -1 : page_of(it);
+            load_unit<D, FMT>(f, a.c, head, page, ((unit0 + j) % upb) * kKvGroup, r, g);
+            return page;
+        };
+        if (n > 0) page_next = request(0, next);
+        for (int it = 0; it < n; ++it) {
+            now = next;
+            page_now = page_next;
+            if (it + 1 < n) page_next = request(it + 1, next);
+            if (page_now < 0) continue;
+            const int token0 = w.lo + (j0 + wave + kRowsWaves * it) * kKvGroup;
+            take_unit<D, FMT, MT>(st, Q, now, a, token0 < clear_lo || token0 + kKvGroup > clear_hi, token0, w.span.len, first_key, last_key, g);
+        }
+        // ---- the four waves meet
+        const bool whole = j0 == 0 && j1 == w.units;
+        const size_t slot = 2 * (size_t)blockIdx.x + (j0 == 0 ? 1 : 0);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            st.sum[m] = quad_sum(st.sum[m]);
+            if (g == 0) {
+                ml[wave][16 * m + r][0] = st.top[m];
+                ml[wave][16 * m + r][1] = st.sum[m];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float all_top = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < kRowsWaves; ++i) all_top = fmaxf(all_top, ml[i][16 * m + r][0]);
+            const float f0 = weight_of(st.top[m], all_top);
+            if (m) __syncthreads();  // the slab of the tile before is read
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) {
+                float* at = &slab[wave][r][32 * dt + 8 * g];
+                *reinterpret_cast<f32x4*>(at) = f32x4{st.o[m][2 * dt][0], st.o[m][2 * dt + 1][0], st.o[m][2 * dt][1], st.o[m][2 * dt + 1][1]} * f0;
+                *reinterpret_cast<f32x4*>(at + 4) = f32x4{st.o[m][2 * dt][2], st.o[m][2 * dt + 1][2], st.o[m][2 * dt][3], st.o[m][2 * dt + 1][3]} * f0;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                const int id = tid + 256 * i, row = id / (D / 4), d = (id - row * (D / 4)) * 4, rr = row0 + 16 * m + row;
+                if (rr >= w.span.rows * a.group) continue;
+                float top = -__builtin_inff(), l = 0.0f;
+                f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < kRowsWaves; ++k) top = fmaxf(top, ml[k][16 * m + row][0]);
+#pragma unroll
+                for (int k = 0; k < kRowsWaves; ++k) {
+                    l += ml[k][16 * m + row][1] * weight_of(ml[k][16 * m + row][0], top);
+                    o += *reinterpret_cast<const f32x4*>(&slab[k][row][d]);
+                }
+                if (whole) {
+                    const int token = rr / a.group;
+                    write_row4(a, D, w.span.row0 + token, head * a.group + rr - token * a.group, d, o, top, l);
+                } else {
+                    *reinterpret_cast<f32x4*>(a.part_o + ((slot * 16 * MT) + 16 * m + row) * D + d) = o;
+                    if (d == 0) {
+                        a.part_ml[(slot * 16 * MT + 16 * m + row) * 2] = top;
+                        a.part_ml[(slot * 16 * MT + 16 * m + row) * 2 + 1] = l;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        u += j1 - j0;
+        in_seq += j1 - j0;
+    }
+}
+
+// Joins the partial results of the rows whose units lay in several shares.  A workgroup takes one query row of one head; 256 / (D / 4)
+// pieces are read side by side.
+template <int D, int MT>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
+    constexpr int kLanes = D / 4, kSide = 256 / kLanes;
+    __shared__ f32x4 so[kSide][kLanes];
+    __shared__ float sm[kSide], sl[kSide];
+    const int seq = blockIdx.y, head_q = blockIdx.x % a.q_heads, token = blockIdx.x / a.q_heads;
+    const KvUnits w = kv_units<MT>(a, seq);
+    if (token >= w.span.rows) return;
+    const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / (16 * MT);
+    const int64_t share = a.plan[a.s.n_seqs + 1];
+    const int64_t from = a.plan[seq] + ((int64_t)head * w.tiles + tile) * w.units, to = from + w.units;
+    const int64_t w0 = from / share, w1 = (to - 1) / share;
+    if (w0 == w1) return;  // one share had it all
+    const int tid = threadIdx.x, lane = tid % kLanes, side = tid / kLanes, row = rr - tile * 16 * MT;
+    float top = -__builtin_inff(), l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    if (side < kSide) {
+        for (int64_t p = w0 + side; p <= w1; p += kSide) {
+            const size_t at = (2 * (size_t)p + (p == w0 ? 1 : 0)) * 16 * MT + row;
+            const float t = a.part_ml[2 * at], s = a.part_ml[2 * at + 1];
+            const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * lane);
+            const float m = fmaxf(top, t), f0 = weight_of(top, m), f1 = weight_of(t, m);
+            o = o * f0 + x * f1;
+            l = l * f0 + s * f1;
+            top = m;
+        }
+        so[side][lane] = o;
+        if (lane == 0) sm[side] = top, sl[side] = l;
+    }
+    __syncthreads();
+    if (side != 0) return;
+#pragma unroll
+    for (int i = 1; i < kSide; ++i) {
+        const float m = fmaxf(top, sm[i]), f0 = weight_of(top, m), f1 = weight_of(sm[i], m);
+        o = o * f0 + so[i][lane] * f1;
+        l = l * f0 + sl[i] * f1;
+        top = m;
+    }
+    write_row4(a, D, w.span.row0 + token, head_q, 4 * lane, o, top, l);
+}
+
+}  // namespace floe

@@ -1,0 +1,123 @@
+"""Refusals of the calls on the paged 8-bit cache: every bad argument comes back as its status before anything is enqueued (the pointers
+are made up and never followed), and the binding refuses tensors that do not fit."""
+import ctypes as C
+import os
+
+import pytest
+import torch
+
+import paper_2505_05950_amd as F
+from paper_2505_05950_amd import binding as B
+
+EINVAL, ESHAPE, EUNSUPPORTED, EWORKSPACE, EHIP = -1, -2, -3, -4, -5
+P = 1 << 20  # an address that fits every alignment
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.lib_path()):
+        from paper_2505_05950_amd import build
+        build.build()
+    return B.load()
+
+
+def cache(n_pages=4, kv_heads=2, head_dim=128, block=64, fmt=0, dtype=0, k=P, v=P, ks=P, vs=P):
+    return B._KvCache(n_pages, kv_heads, head_dim, block, fmt, dtype, k, v, ks, vs)
+
+
+def seqs(n_seqs=2, n_rows=2, max_rows=1, max_blocks=3, cu=P, length=P, table=P):
+    return B._KvSeqs(n_seqs, n_rows, max_rows, max_blocks, cu, length, table)
+
+
+def attn(q_heads=8, causal=1, window=0, max_len=100, scale=0.1):
+    return B._Attention(q_heads, causal, window, max_len, scale)
+
+
+def rope(table=P, positions=None, n_positions=10, rot=128, interleaved=0):
+    return B._Rope(table, positions, n_positions, rot, interleaved)
+
+
+BAD_CACHES = [(dict(n_pages=0), EINVAL), (dict(kv_heads=0), EINVAL), (dict(k=None), EINVAL), (dict(v=P + 8), EINVAL), (dict(ks=None), EINVAL),
+              (dict(vs=P + 2), EINVAL), (dict(head_dim=96), EUNSUPPORTED), (dict(head_dim=0), EUNSUPPORTED), (dict(head_dim=512), EUNSUPPORTED),
+              (dict(block=16), EUNSUPPORTED), (dict(block=256), EUNSUPPORTED), (dict(kv_heads=257), EUNSUPPORTED), (dict(fmt=2), EUNSUPPORTED),
+              (dict(dtype=2), EUNSUPPORTED), (dict(dtype=-1), EUNSUPPORTED)]
+BAD_SEQS = [(dict(n_seqs=-1), EINVAL), (dict(n_rows=-1), EINVAL), (dict(max_rows=-1), EINVAL), (dict(max_blocks=0), EINVAL), (dict(cu=None), EINVAL),
+            (dict(length=None), EINVAL), (dict(table=None), EINVAL), (dict(table=P + 2), EINVAL), (dict(n_seqs=65536), EUNSUPPORTED),
+            (dict(n_rows=(1 << 24) + 1), EUNSUPPORTED)]
+
+
+@pytest.mark.parametrize("c,s,code", [(c, {}, rc) for c, rc in BAD_CACHES] + [({}, s, rc) for s, rc in BAD_SEQS])
+def test_a_bad_cache_or_batch_is_refused_by_every_call(lib, c, s, code):
+    c, s = cache(**c), seqs(**s)
+    assert lib.floe_kv_append(c, s, P, 256, P, 256, None, 0, 0, None, None, None) == code
+    assert lib.floe_kv_gather(c, s, P, P, None) == code
+    assert lib.floe_kv_attention(c, s, attn(), P, 1024, P, None, P, 1 << 40, None) == code
+
+
+def test_append_refuses(lib):
+    def call(k=P, ks=256, v=P, vs=256, q=None, qs=0, heads=0, out=None, r=None, s=None):
+        return lib.floe_kv_append(cache(), s or seqs(), k, ks, v, vs, q, qs, heads, out, r, None)
+    assert call(k=None) == EINVAL and call(v=None) == EINVAL and call(k=P + 8) == EINVAL
+    assert call(ks=255) == EINVAL and call(ks=260) == EINVAL and call(vs=8) == EINVAL and call(ks=1 << 41) == EUNSUPPORTED
+    assert call(r=rope(table=None)) == EINVAL and call(r=rope(table=P + 4)) == EINVAL and call(r=rope(n_positions=0)) == EINVAL
+    assert call(r=rope(rot=24)) == ESHAPE and call(r=rope(rot=144)) == ESHAPE and call(r=rope(rot=0)) == EINVAL and call(r=rope(positions=P + 2)) == EINVAL
+    good = dict(q=P, qs=1024, heads=8, out=P, r=rope())
+    for change, rc in ((dict(r=None), EINVAL), (dict(out=None), EINVAL), (dict(heads=0), EINVAL), (dict(qs=1000), EINVAL), (dict(qs=1028), EINVAL),
+                       (dict(q=P + 2), EINVAL), (dict(out=P + 8), EINVAL), (dict(heads=1025, qs=1 << 20), EUNSUPPORTED)):
+        assert call(**{**good, **change}) == rc, change
+    # launches that no grid holds
+    assert call(s=seqs(n_seqs=65535, n_rows=1 << 24, max_rows=1 << 24)) == EUNSUPPORTED
+    # nothing to do: nothing is looked at
+    assert call(k=None, s=seqs(n_seqs=0)) == 0 and call(k=None, s=seqs(n_rows=0)) == 0 and call(k=None, s=seqs(max_rows=0, cu=None)) == 0
+
+
+def test_attention_refuses(lib):
+    need = lib.floe_kv_attention_workspace_bytes(cache(), seqs(), attn())
+    assert need > 0
+    def call(a=None, q=P, qs=1024, out=P, lse=None, ws=P, n=need, s=None):
+        return lib.floe_kv_attention(cache(), s or seqs(), a or attn(), q, qs, out, lse, ws, n, None)
+    for a, rc in ((dict(q_heads=0), EINVAL), (dict(q_heads=7), ESHAPE), (dict(window=-1), EINVAL), (dict(max_len=-1), EINVAL),
+                  (dict(q_heads=1026), EUNSUPPORTED), (dict(window=(1 << 30) + 1), EUNSUPPORTED)):
+        assert call(attn(**a), qs=1 << 20) == rc, a
+        assert lib.floe_kv_attention_workspace_bytes(cache(), seqs(), attn(**a)) == 0
+    assert call(q=None) == EINVAL and call(out=None) == EINVAL and call(ws=None) == EINVAL and call(qs=1020) == EINVAL and call(qs=512) == EINVAL
+    assert call(ws=P + 128) == EINVAL and call(lse=P + 2) == EINVAL and call(q=P + 8) == EINVAL
+    assert call(n=need - 1) == EWORKSPACE
+    assert call(q=None, s=seqs(n_rows=0)) == 0
+    if not torch.cuda.is_available():
+        assert call() == EHIP
+
+
+def test_rope_table_refuses(lib):
+    def call(table=P, n=10, rot=64, base=1e4):
+        return lib.floe_rope_table(table, n, rot, base, None)
+    assert call(table=None) == EINVAL and call(n=-1) == EINVAL and call(rot=0) == EINVAL and call(base=0.0) == EINVAL and call(base=float("nan")) == EINVAL
+    assert call(rot=24) == ESHAPE and call(rot=272) == EUNSUPPORTED and call(n=0) == 0
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    c = F.KVCache(2, 2, 64, 32, device="cpu")
+    cu, n, table = torch.tensor([0, 3], dtype=torch.int32), torch.tensor([3], dtype=torch.int32), torch.zeros((1, 2), dtype=torch.int32)
+    x = torch.zeros((3, 2, 64), dtype=torch.float16)
+    bad = [x.float(), x.bfloat16(), x[:, :1], torch.zeros((3, 2, 32), dtype=torch.float16), x.transpose(0, 1).contiguous().transpose(0, 1), x[0]]
+    for t in bad:
+        with pytest.raises(ValueError):
+            F.floe_kv_append(c, t, x, cu, n, table, 3)
+    with pytest.raises(ValueError):
+        F.floe_kv_append(c, x, x[:2], cu, n, table, 3)
+    for args in ((cu.long(), n, table), (cu, n.long(), table), (cu, torch.zeros(2, dtype=torch.int32), table), (cu, n, table[0]),
+                 (cu, n, torch.zeros((2, 2), dtype=torch.int32)), (cu, n, torch.zeros((1, 4), dtype=torch.int32)[:, ::2].expand(1, 2).t().t()[:, :1].expand(1, 2))):
+        with pytest.raises(ValueError):
+            F.floe_kv_append(c, x, x, *args, 3)
+    with pytest.raises(ValueError):
+        F.floe_kv_attention(c, x, cu, n, table, 3, 3, out=torch.zeros((3, 2, 64)))
+    with pytest.raises(ValueError):
+        F.floe_kv_attention(c, x, cu, n, table, 3, 3, lse=torch.zeros((3, 1)))
+    with pytest.raises(ValueError):
+        F.floe_kv_gather(c, n, cu, table, 3, 3, k_out=torch.zeros((2, 2, 64), dtype=torch.float16))
+    with pytest.raises(ValueError):
+        F.KVCache(2, 2, 64, 32, dtype=torch.float32, device="cpu")
+    with pytest.raises(ValueError):
+        F.KVCache(2, 2, 64, 32, device="cpu", tensors=(c.k, c.v, c.k_scale, c.v_scale[:1]))
+    with pytest.raises(ValueError):
+        F.Rope(torch.zeros((4, 8), dtype=torch.float32))
