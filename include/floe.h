@@ -82,7 +82,8 @@ typedef enum {
     FLOE_KERNEL_KV_APPEND = 9,
     FLOE_KERNEL_KV_GATHER = 10,
     FLOE_KERNEL_KV_ATTENTION = 11,
-    FLOE_KERNEL_KV_JOIN = 12 /* partial results of one sequence's tokens, where the attention was split over them */
+    FLOE_KERNEL_KV_JOIN = 12,  /* partial results of one sequence's tokens, where the attention was split over them */
+    FLOE_KERNEL_KV_PROMPT = 13 /* attention of the sequences with many rows in the call */
 } floe_kernel_id;
 int floe_profile_kernel(int kernel_id, void* start_event, void* stop_event);
 

@@ -149,7 +149,7 @@ def floe_status_string(status: int) -> str:
 
 
 KERNEL_IDS = {"none": 0, "quantize": 1, "router": 2, "up_gemv": 3, "select": 4, "gate_down": 5, "combine": 6, "stage": 7,
-              "fused_ffn": 8, "kv_append": 9, "kv_gather": 10, "kv_attention": 11, "kv_join": 12}
+              "fused_ffn": 8, "kv_append": 9, "kv_gather": 10, "kv_attention": 11, "kv_join": 12, "kv_prompt": 13}
 
 
 def floe_profile_kernel(kernel: str, start_event=None, stop_event=None):

@@ -336,7 +336,7 @@ int floe_last_hip_error(void) { return g_last_hip_error; }
 int floe_abi_version(void) { return 4; }
 
 int floe_profile_kernel(int kernel_id, void* start_event, void* stop_event) {
-    if (kernel_id < 0 || kernel_id > FLOE_KERNEL_KV_JOIN) return FLOE_EINVAL;
+    if (kernel_id < 0 || kernel_id > FLOE_KERNEL_KV_PROMPT) return FLOE_EINVAL;
     if (kernel_id != 0 && (!start_event || !stop_event)) return FLOE_EINVAL;
     g_hook.id = kernel_id;
     g_hook.start = (hipEvent_t)start_event;

@@ -46,18 +46,36 @@ int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_at
     if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0) return FLOE_EINVAL;
     if (a->q_heads % c->kv_heads != 0) return FLOE_ESHAPE;
     if (a->q_heads > 1024 || a->window > kKvMaxLen) return FLOE_EUNSUPPORTED;
-    if ((int64_t)a->q_heads * s->max_rows > kMaxGrid) return FLOE_EUNSUPPORTED;
+    // (the widest grid: a workgroup per 128 query rows of a KV head, or per row where there are few)
+    const KvSeqs k = dev_seqs(s);
+    if (((int64_t)k.max_rows * (a->q_heads / c->kv_heads) / 128 + 1) * k.n_seqs * c->kv_heads > kMaxGrid) return FLOE_EUNSUPPORTED;
+    if ((int64_t)k.max_rows * a->q_heads > 0x7fffffff) return FLOE_EUNSUPPORTED;
     return FLOE_OK;
 }
-// [partial sums][their maxima and sums][plan]
-struct AttnWs {
+// Which kernels a call runs, and its workspace: [partial sums][their maxima and sums][plan]
+struct AttnPlan {
+    bool rows, prompt;
+    int most_rows;  // sequences of up to so many rows are the rows kernel's
+    int join_rows;  // at least the rows of any of those
     int mt, workgroups;
     size_t ml_off, plan_off, total;
 };
-AttnWs attn_ws(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
-    AttnWs w;
+AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
+    AttnPlan w{};
     const KvSeqs k = dev_seqs(s);
-    w.mt = kv_rows_tiles_for(c->head_dim, k.max_rows * (a->q_heads / c->kv_heads));
+    const int group = a->q_heads / c->kv_heads, most = kKvRowsLimit / group;
+    w.rows = true;
+    w.most_rows = w.join_rows = k.max_rows;
+    if (k.max_rows > most) {
+        // where no sequence can have few rows (n_rows are too many for that) the rows kernel has nothing to look for
+        w.prompt = true;
+        w.rows = k.n_rows - (int64_t)(k.n_seqs - 1) * k.max_rows <= most;
+        w.most_rows = w.rows ? most : 0;
+        w.join_rows = most;
+        if (most == 0) w.rows = false;
+    }
+    if (!w.rows) return w;
+    w.mt = kv_rows_tiles_for(c->head_dim, w.join_rows * group);
     w.workgroups = kv_rows_workgroups(c->head_dim, w.mt);
     const size_t rows = (size_t)2 * w.workgroups * 16 * w.mt;
     w.ml_off = align_up(rows * c->head_dim * 4);
@@ -135,7 +153,7 @@ int floe_kv_gather(const floe_kv_cache* c, const floe_kv_seqs* s, void* k_out, v
 }
 
 size_t floe_kv_attention_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
-    return check_attention(c, s, a) == FLOE_OK ? attn_ws(c, s, a).total : 0;
+    return check_attention(c, s, a) == FLOE_OK && !nothing(s) ? attn_plan(c, s, a).total : 0;
 }
 
 int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, const void* q, int64_t q_stride, void* out,
@@ -147,7 +165,7 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     if (nothing(s)) return FLOE_OK;
     if ((rc = check_arrays(s))) return rc;
     if (!q || !out || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, kAlign)) return FLOE_EINVAL;
-    const AttnWs w = attn_ws(c, s, a);
+    const AttnPlan w = attn_plan(c, s, a);
     if (workspace_bytes < w.total) return FLOE_EWORKSPACE;
     char* base = static_cast<char*>(workspace);
     KvAttnArgs k{};
@@ -163,13 +181,18 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     k.causal = a->causal != 0;
     k.window = a->window;
     k.bf16 = c->dtype == FLOE_BF16;
+    k.most_rows = w.most_rows;
     k.part_o = reinterpret_cast<float*>(base);
     k.part_ml = reinterpret_cast<float*>(base + w.ml_off);
     k.plan = reinterpret_cast<int64_t*>(base + w.plan_off);
     hipStream_t st = (hipStream_t)stream;
-    FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st,
-                c->format == FLOE_KV_INT8 ? launch_kv_rows_int8(k, w.mt, w.workgroups, st) : launch_kv_rows_e4m3(k, w.mt, w.workgroups, st));
-    FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, st));
+    const bool int8 = c->format == FLOE_KV_INT8;
+    if (w.prompt) FLOE_LAUNCH(FLOE_KERNEL_KV_PROMPT, st, int8 ? launch_kv_prompt_int8(k, st) : launch_kv_prompt_e4m3(k, st));
+    if (w.rows) {
+        FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st,
+                    int8 ? launch_kv_rows_int8(k, w.mt, w.workgroups, st) : launch_kv_rows_e4m3(k, w.mt, w.workgroups, st));
+        FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, w.join_rows, st));
+    }
     return FLOE_OK;
 }
 

@@ -5,8 +5,8 @@ namespace floe {
 
 namespace {
 template <int D>
-hipError_t join_tiles(const KvAttnArgs& a, int mt, hipStream_t st) {
-    const dim3 grid(a.q_heads * a.s.max_rows, a.s.n_seqs), wg(256);
+hipError_t join_tiles(const KvAttnArgs& a, int mt, int rows, hipStream_t st) {
+    const dim3 grid(a.q_heads * rows, a.s.n_seqs), wg(256);
     if constexpr (kv_rows_most_tiles(D) >= 4) {
         if (mt == 4) return kv_join_kernel<D, 4><<<grid, wg, 0, st>>>(a), hipGetLastError();
     }
@@ -18,12 +18,12 @@ hipError_t join_tiles(const KvAttnArgs& a, int mt, hipStream_t st) {
 }
 }  // namespace
 
-hipError_t launch_kv_join(const KvAttnArgs& a, int mt, hipStream_t st) {
+hipError_t launch_kv_join(const KvAttnArgs& a, int mt, int rows, hipStream_t st) {
     switch (a.c.dim) {
-        case 64: return join_tiles<64>(a, mt, st);
-        case 128: return join_tiles<128>(a, mt, st);
-        case 192: return join_tiles<192>(a, mt, st);
-        default: return join_tiles<256>(a, mt, st);
+        case 64: return join_tiles<64>(a, mt, rows, st);
+        case 128: return join_tiles<128>(a, mt, rows, st);
+        case 192: return join_tiles<192>(a, mt, rows, st);
+        default: return join_tiles<256>(a, mt, rows, st);
     }
 }
 

@@ -37,12 +37,14 @@ struct KvAttnArgs {
     float scale_log2;  // softmax scale * log2(e)
     int causal, window;
     bool bf16;
+    int most_rows;  // sequences of up to so many rows are the rows kernel's, the others the prompt kernel's
     // rows kernel (kv_rows.h)
     float* part_o;   // [slots][16 MT][dim]
     float* part_ml;  // [slots][16 MT][2]
     int64_t* plan;   // [n_seqs + 2]: units before each sequence, all units, units per workgroup
 };
 
+constexpr int kKvRowsLimit = 64;  // query rows per KV head up to which a sequence is the rows kernel's
 constexpr int kKvMinShare = 8;  // units of 32 tokens: two per wave
 // Tiles of sixteen rows that a workgroup of the rows kernel takes at once: as many as its registers hold beside two units of the cache
 constexpr int kv_rows_most_tiles(int dim) { return dim == 64 ? 4 : dim <= 192 ? 2 : 1; }
@@ -54,6 +56,11 @@ constexpr int kv_rows_wgs_per_cu(int dim, int mt) { return dim * mt <= 128 ? 3 :
 inline int kv_rows_workgroups(int dim, int mt) { return num_cus() * kv_rows_wgs_per_cu(dim, mt); }
 hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, int workgroups, hipStream_t st);
 hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, int workgroups, hipStream_t st);
-hipError_t launch_kv_join(const KvAttnArgs& a, int mt, hipStream_t st);
+// prompt kernel (kv_prompt.h): waves of a workgroup, 32 query rows each, and how many of them a SIMD holds
+constexpr int kv_prompt_waves(int dim) { return dim == 128 ? 8 : 4; }
+constexpr int kv_prompt_waves_per_simd(int dim) { return dim <= 128 ? 2 : 1; }
+hipError_t launch_kv_prompt_int8(const KvAttnArgs& a, hipStream_t st);
+hipError_t launch_kv_prompt_e4m3(const KvAttnArgs& a, hipStream_t st);
+hipError_t launch_kv_join(const KvAttnArgs& a, int mt, int rows, hipStream_t st);  // rows: at least those of any sequence it joins
 
 }  // namespace floe

@@ -1,0 +1,264 @@
+// Attention of many query rows per sequence over the paged 8-bit cache (chunks of prompts, whole prompts).
+//
+// The same formula as the rows kernel (kv_rows.h), here bound by arithmetic: a workgroup of NW waves takes 32 NW query rows of one KV
+// head (row = (token, head of the group)) and walks the tokens in tiles of 64.  A tile's codes are turned into fp16 once per
+// workgroup, on their way into LDS, and read from there by every wave as operand of v_mfma_f32_32x32x16_f16.  S^T = K Q^T: a column is
+// a query row, held by lanes l and l + 32, so the maximum needs one exchange; the rows of S^T in a lane (tokens 8 a + 4 h + b of a
+// 32-token tile) are the operand of O^T = V^T P^T when the tokens of V lie in LDS in that order, so the weights stay in registers.
+// Two LDS buffers: a wave converts the next tile's codes while others still multiply, one barrier per tile, and the tile after next is on
+// its way from memory.
+// The exponent's base of a row is moved only when a weight would leave fp16 (2^15): after the first tiles it hardly ever is.
+#pragma once
+
+#include "kv_rows.h"
+
+namespace floe {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kPromptTokens = 64;             // of a tile: two units of 32, each inside one page
+constexpr float kPromptBits = 7.0f;           // a row's largest weight is 2^7 when its base is set ...
+constexpr float kPromptTop = 15.0f;           // ... and may grow to 2^15 before it is set again
+
+// rows of a workgroup and workgroups that a sequence's rows make
+constexpr int kv_prompt_rows(int waves) { return 32 * waves; }
+
+template <int D, int NW>
+struct PromptStage {  // a thread's share of a tile on its way: 16-byte pieces of the codes
+    static constexpr int kPieces = 4 * D / (64 * NW);
+    uint4 k[kPieces], v[kPieces];
+};
+
+template <int D, int FMT, int NW>
+__global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_prompt_kernel(KvAttnArgs a, int tiles_per_seq) {
+    constexpr int kThreads = 64 * NW, kPieces = PromptStage<D, NW>::kPieces, kChunks = D / 8;
+    static_assert(kPieces * kThreads == 4 * D, "a tile is dealt out evenly");
+    __shared__ uint4 ldsK[2][kPromptTokens * kChunks];  // [token][chunk ^ token % 8]: eight dims of a token
+    __shared__ uint4 ldsV[2][D * 8];                    // [dim][chunk ^ dim % 8]: chunk 2 s + h holds tokens 16 s + {4 h .. + 3, 8 + 4 h .. + 3}
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
+    const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads;
+    const int seq = rest % a.s.n_seqs, tile = tiles_per_seq - 1 - rest / a.s.n_seqs;  // the last rows of a prompt see most: they go first
+    const KvSpan span = kv_span(a.s, seq);
+    const int all_rows = span.rows * a.group, row0 = tile * 32 * NW;
+    if (row0 >= all_rows || span.rows <= a.most_rows) return;
+    // ---- queries of this wave
+    const int rr = row0 + 32 * wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.len - span.rows + token;
+    const bool there = rr < all_rows;
+    const int head_q = head * a.group + (there ? rr - token * a.group : 0);
+    h16x8 q[D / 16];
+    float unscale = 1.0f;
+    {
+        const uint16_t* p = a.q + (span.row0 + token) * a.q_stride + (size_t)head_q * D + 8 * h;
+        const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;  // the sign of the scale goes into the queries: larger S, larger weight
+        uint4 raw[D / 16];
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            raw[s] = there ? gload16(p + 16 * s) : make_uint4(0, 0, 0, 0);
+            raw[s].x ^= flip, raw[s].y ^= flip, raw[s].z ^= flip, raw[s].w ^= flip;
+        }
+        if (a.bf16) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) top = max(top, largest_bf16(raw[s]));
+            float x0, x1;
+            swap32(bf16_to_f32(top), x0, x1);
+            const PowerOfTwo f = bring_to_fp16(fmaxf(x0, x1));
+            unscale = f.down;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) q[s] = bf16_to_h8(raw[s], f.up);
+        } else {
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) q[s] = __builtin_bit_cast(h16x8, raw[s]);
+        }
+    }
+    const float row_scale = fabsf(a.scale_log2) * unscale;
+    // ---- tokens that the workgroup and this wave's rows see
+    const int first_key = a.window > 0 ? pos - a.window + 1 : 0, last_key = a.causal ? pos : span.len - 1;
+    const int base_pos = span.len - span.rows;
+    const int wg_last = base_pos + min((row0 + 32 * NW - 1) / a.group, span.rows - 1), wg_first = base_pos + row0 / a.group;
+    const int w_first = base_pos + min((row0 + 32 * wave) / a.group, span.rows - 1);
+    const int w_last = base_pos + min((row0 + 32 * wave + 31) / a.group, span.rows - 1);
+    const int end = a.causal ? wg_last + 1 : span.len;  // behind the last token that any row sees
+    const int start = a.window > 0 ? max(0, wg_first - a.window + 1) & ~(kPromptTokens - 1) : 0;
+    const int n_tiles = max(0, (end - start + kPromptTokens - 1) / kPromptTokens);
+    const int w_lo = a.window > 0 ? w_first - a.window + 1 : 0, w_hi = a.causal ? w_last : span.len - 1;     // any row sees
+    const int w_clear_lo = a.window > 0 ? w_last - a.window + 1 : 0, w_clear_hi = a.causal ? w_first : span.len - 1;  // every row sees
+    const bool live_wave = row0 + 32 * wave < all_rows;
+
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[d][j] = 0.0f;
+    float top = -__builtin_inff(), sum = 0.0f;
+
+    const int upb = a.c.block / kKvGroup;
+    int pages = -1;
+    auto page_of = [&](int unit) {  // page of the walk's unit-th unit of 32 tokens (0, 1, 2 ... in order), -1 where there is none
+        if ((unit & 63) == 0) {
+            const int t = start + (unit + lane) * kKvGroup;
+            pages = t < span.len ? kv_page(a.s, a.c, seq, (t / kKvGroup) / upb) : -1;
+        }
+        return __builtin_amdgcn_readlane(pages, unit & 63);
+    };
+    PromptStage<D, NW> next;
+    int page[2] = {-1, -1};
+    float ks[2], vs[2];
+    auto request = [&](int it) {
+        const uint8_t *kp[2], *vp[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            page[u] = page_of(2 * it + u);
+            const size_t slot = (size_t)max(page[u], 0) * a.c.heads + head;
+            const int unit = start / kKvGroup + 2 * it + u;
+            const size_t at = (slot * a.c.block + (unit % upb) * kKvGroup) * D;
+            kp[u] = scalar_ptr(a.c.k + at);
+            vp[u] = scalar_ptr(a.c.v + at);
+            ks[u] = gloadf(a.c.k_scale + slot);
+            vs[u] = gloadf(a.c.v_scale + slot);
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int id = tid + i * kThreads, u = id / (2 * D), in = id - u * 2 * D;  // (2 D is a multiple of the wave: u is the same in a wave)
+            next.k[i] = gload16((u ? kp[1] : kp[0]) + 16 * in);
+            next.v[i] = gload16((u ? vp[1] : vp[0]) + 16 * in);
+        }
+    };
+    auto convert = [&](int it, int buf) {
+        const int tokens_left = span.len - (start + it * kPromptTokens);  // of the tile
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int id = tid + i * kThreads;
+            {
+                const int t = id / (D / 16), c = 2 * (id - t * (D / 16));
+                const uint4 w = next.k[i];
+                ldsK[buf][t * kChunks + (c ^ (t & 7))] = __builtin_bit_cast(uint4, codes_to_h8<FMT>(w.x, w.y));
+                ldsK[buf][t * kChunks + ((c + 1) ^ (t & 7))] = __builtin_bit_cast(uint4, codes_to_h8<FMT>(w.z, w.w));
+            }
+            {
+                const int u = id / (2 * D), in = id - u * 2 * D, pair = in >> 2, g = in & 3;
+                uint4 w = next.v[i];
+                const int left = (u ? page[1] : page[0]) < 0 ? 0 : tokens_left - 32 * u;
+                if (left < kKvGroup) {  // codes behind the last token are whatever the page held before, those of an absent page are nobody's
+                    const int n0 = min(max(left - 4 * g, 0), 4), n1 = min(max(left - 16 - 4 * g, 0), 4);
+                    const uint32_t m0 = n0 == 4 ? ~0u : (1u << (8 * n0)) - 1u, m1 = n1 == 4 ? ~0u : (1u << (8 * n1)) - 1u;
+                    w.x &= m0, w.y &= m1, w.z &= m0, w.w &= m1;
+                }
+#pragma unroll
+                for (int par = 0; par < 2; ++par) {
+                    const int d = 2 * pair + par;
+                    const uint4 x = __builtin_bit_cast(uint4, par ? codes_to_h8<FMT>(w.z, w.w) : codes_to_h8<FMT>(w.x, w.y));
+                    uint2* row = reinterpret_cast<uint2*>(&ldsV[buf][d * 8]);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const int chunk = 2 * (2 * u + t) + (g & 1);
+                        row[2 * (chunk ^ (d & 7)) + (g >> 1)] = t ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y);
+                    }
+                }
+            }
+        }
+    };
+    if (n_tiles > 0) request(0);
+    for (int it = 0; it < n_tiles; ++it) {
+        const int buf = it & 1, t0 = start + it * kPromptTokens;
+        convert(it, buf);
+        const float ks_now[2] = {ks[0], ks[1]}, vs_now[2] = {vs[0], vs[1]};
+        const bool have[2] = {page[0] >= 0, page[1] >= 0};
+        if (it + 1 < n_tiles) request(it + 1);
+        __syncthreads();
+        if (!live_wave || t0 > w_hi || t0 + kPromptTokens <= w_lo || !(have[0] || have[1])) continue;
+        // ---- S^T
+        f32x16 s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[u][j] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const int t = 32 * u + c32;
+                const h16x8 kf = __builtin_bit_cast(h16x8, ldsK[buf][t * kChunks + ((2 * k + h) ^ (t & 7))]);
+                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[k], s[u], 0, 0, 0);
+            }
+        }
+        const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || !have[0] || !have[1];
+        uint32_t unseen = 0;
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int key = t0 + 32 * u + 8 * (j >> 2) + 4 * h + (j & 3);
+                    if (key < first_key || key > last_key || !have[u]) {
+                        s[u][j] = -__builtin_inff();
+                        unseen |= 1u << (16 * u + j);
+                    }
+                }
+        }
+        // ---- weights
+        float c[2], lv[2], mx = -__builtin_inff();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float m = -__builtin_inff();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) m = fmaxf(m, s[u][j]);
+            c[u] = row_scale * ks_now[u];
+            lv[u] = __builtin_amdgcn_logf(vs_now[u]);
+            // (nothing seen: m is -inf, and must stay so whatever the scales are)
+            mx = fmaxf(mx, m == -__builtin_inff() ? m : __builtin_fmaf(m, c[u], lv[u]));
+        }
+        float x0, x1;
+        swap32(mx, x0, x1);
+        mx = fmaxf(x0, x1);
+        const bool move = mx > top + kPromptTop;
+        if (__ballot(move)) {
+            const float new_top = move ? mx - kPromptBits : top;
+            const float f = move ? __builtin_amdgcn_exp2f(top - new_top) : 1.0f;
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[d] *= f;
+            top = new_top;
+        }
+        const float base = top == -__builtin_inff() ? 0.0f : top;
+        h16x8 p[4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const float off = lv[u] - base;
+            float part = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[u][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][j], c[u], off));
+            if (masked) {  // (0 and NaN times -infinity are no weight either)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (unseen & (1u << (16 * u + j))) s[u][j] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) part += s[u][j];
+            sum += part != 0.0f ? part * (1.0f / vs_now[u]) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const h16x2 w = __builtin_convertvector(f32x2{s[u][2 * j], s[u][2 * j + 1]}, h16x2);
+                p[2 * u + (j >> 2)][2 * (j & 3)] = w.x;
+                p[2 * u + (j >> 2)][2 * (j & 3) + 1] = w.y;
+            }
+        }
+        // ---- O^T
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) {
+                const int dim = 32 * d + c32;
+                const h16x8 vf = __builtin_bit_cast(h16x8, ldsV[buf][dim * 8 + ((2 * k + h) ^ (dim & 7))]);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[k], o[d], 0, 0, 0);
+            }
+    }
+    swap32(sum, ks[0], ks[1]);
+    sum = ks[0] + ks[1];
+    if (!there) return;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            write_row4(a, D, span.row0 + token, head_q, 32 * d + 8 * j + 4 * h, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, top, sum);
+}
+
+}  // namespace floe

@@ -34,6 +34,7 @@ template <int MT>
 __device__ __forceinline__ KvUnits kv_units(const KvAttnArgs& a, int seq) {
     KvUnits u;
     u.span = kv_span(a.s, seq);
+    if (u.span.rows > a.most_rows) u.span.rows = 0;  // the prompt kernel's
     u.tiles = (u.span.rows * a.group + 16 * MT - 1) / (16 * MT);
     u.lo = a.window > 0 ? max(0, u.span.len - u.span.rows - a.window + 1) & ~(kKvGroup - 1) : 0;
     u.units = max(1, (u.span.len - u.lo + kKvGroup - 1) / kKvGroup);
@@ -78,6 +79,36 @@ __device__ __forceinline__ void load_unit(KvFrag<D, FMT>& f, const KvCache& c, i
     f.vs = gloadf(c.v_scale + slot);
 }
 
+// A row of bf16 queries is multiplied with the power of two that gives its largest exponent 14 (2^14 <= largest < 2^15): what fp16
+// cannot hold then is below 2^-38 of the largest.  Zeros, infinities and NaN stay as they are.
+struct PowerOfTwo {
+    float up, down;
+};
+__device__ __forceinline__ PowerOfTwo bring_to_fp16(float largest) {
+    const int e = (int)(__builtin_bit_cast(uint32_t, largest) >> 23) - 127;
+    const int up = (e == 128 || largest == 0.0f) ? 0 : min(14 - e, 126);
+    return PowerOfTwo{__builtin_bit_cast(float, (uint32_t)(127 + up) << 23), __builtin_bit_cast(float, (uint32_t)(127 - up) << 23)};
+}
+__device__ __forceinline__ uint32_t largest_bf16(uint4 q) {  // of the absolute values, as bits
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+    return top;
+}
+__device__ __forceinline__ h16x8 bf16_to_h8(uint4 q, float f) {
+    float x[8];
+    unpack8<true>(q, x);
+    h16x8 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const h16x2 p = __builtin_convertvector(f32x2{x[2 * j] * f, x[2 * j + 1] * f}, h16x2);
+        r[2 * j] = p.x;
+        r[2 * j + 1] = p.y;
+    }
+    return r;
+}
+
 // One query row's eight halves of a reduction step, in the order in which the codes of K arrive; rows without a query are zero.
 template <int D, int MT>
 struct KvQueries {
@@ -103,28 +134,11 @@ __device__ __forceinline__ void load_queries(KvQueries<D, MT>& Q, const KvAttnAr
         }
         uint32_t top = 0;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+        for (int s = 0; s < D / 32; ++s) top = max(top, largest_bf16(raw[s]));
+        const PowerOfTwo f = bring_to_fp16(quad_max(bf16_to_f32(top)));
+        Q.unscale[m] = f.down;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-        }
-        // the largest exponent of the row becomes 14 (2^14 <= largest < 2^15); zeros, infinities and NaN stay as they are
-        const float big = quad_max(bf16_to_f32(top));
-        const int e = (int)(__builtin_bit_cast(uint32_t, big) >> 23) - 127;
-        const int up = (e == 128 || big == 0.0f) ? 0 : min(14 - e, 126);
-        const float f = __builtin_bit_cast(float, (uint32_t)(up + 127) << 23);
-        Q.unscale[m] = __builtin_bit_cast(float, (uint32_t)(127 - up) << 23);
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            float x[8];
-            unpack8<true>(raw[s], x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const h16x2 p2 = __builtin_convertvector(f32x2{x[2 * j] * f, x[2 * j + 1] * f}, h16x2);
-                Q.q[m][s][2 * j] = p2.x;
-                Q.q[m][s][2 * j + 1] = p2.y;
-            }
-        }
+        for (int s = 0; s < D / 32; ++s) Q.q[m][s] = bf16_to_h8(raw[s], f.up);
     }
 }
 
