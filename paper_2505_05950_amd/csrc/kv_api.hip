@@ -57,11 +57,12 @@ struct AttnPlan {
     bool rows, prompt;
     int most_rows;  // sequences of up to so many rows are the rows kernel's
     int join_rows;  // at least the rows of any of those
-    int mt, workgroups;
+    int mt, workgroups;  // workgroups 0: no sequence is split
     size_t ml_off, plan_off, total;
 };
 AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
     AttnPlan w{};
+    w.total = kAlign;  // (so that a workspace is a workspace whichever kernels run)
     const KvSeqs k = dev_seqs(s);
     const int group = a->q_heads / c->kv_heads, most = kKvRowsLimit / group;
     w.rows = true;
@@ -76,6 +77,8 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
     }
     if (!w.rows) return w;
     w.mt = kv_rows_tiles_for(c->head_dim, w.join_rows * group);
+    const int64_t keys = a->window > 0 && a->window + (int64_t)w.join_rows < a->max_len ? a->window + (int64_t)w.join_rows : a->max_len;
+    if (keys <= kKvWholeLen) return w;  // no sequence is split
     w.workgroups = kv_rows_workgroups(c->head_dim, w.mt);
     const size_t rows = (size_t)2 * w.workgroups * 16 * w.mt;
     w.ml_off = align_up(rows * c->head_dim * 4);
@@ -164,7 +167,8 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     if (q_stride > (int64_t)1 << 40) return FLOE_EUNSUPPORTED;
     if (nothing(s)) return FLOE_OK;
     if ((rc = check_arrays(s))) return rc;
-    if (!q || !out || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, kAlign)) return FLOE_EINVAL;
+    if (!q || !out || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, kAlign))
+        return FLOE_EINVAL;
     const AttnPlan w = attn_plan(c, s, a);
     if (workspace_bytes < w.total) return FLOE_EWORKSPACE;
     char* base = static_cast<char*>(workspace);
@@ -190,8 +194,9 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     if (w.prompt) FLOE_LAUNCH(FLOE_KERNEL_KV_PROMPT, st, int8 ? launch_kv_prompt_int8(k, st) : launch_kv_prompt_e4m3(k, st));
     if (w.rows) {
         FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st,
-                    int8 ? launch_kv_rows_int8(k, w.mt, w.workgroups, st) : launch_kv_rows_e4m3(k, w.mt, w.workgroups, st));
-        FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, w.join_rows, st));
+                    int8 ? launch_kv_rows_int8(k, w.mt, w.workgroups, w.join_rows, st)
+                         : launch_kv_rows_e4m3(k, w.mt, w.workgroups, w.join_rows, st));
+        if (w.workgroups) FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, w.join_rows, st));
     }
     return FLOE_OK;
 }

@@ -45,7 +45,9 @@ struct KvAttnArgs {
 };
 
 constexpr int kKvRowsLimit = 64;  // query rows per KV head up to which a sequence is the rows kernel's
-constexpr int kKvMinShare = 8;  // units of 32 tokens: two per wave
+constexpr int kKvSegmentCost = 4;  // units that a segment costs beside its own
+constexpr int kKvMinShare = 12;    // two units per wave and one segment
+constexpr int kKvWholeLen = 512;   // sequences up to this length are not split
 // Tiles of sixteen rows that a workgroup of the rows kernel takes at once: as many as its registers hold beside two units of the cache
 constexpr int kv_rows_most_tiles(int dim) { return dim == 64 ? 4 : dim <= 192 ? 2 : 1; }
 inline int kv_rows_tiles_for(int dim, int rows) {
@@ -54,8 +56,9 @@ inline int kv_rows_tiles_for(int dim, int rows) {
 }
 constexpr int kv_rows_wgs_per_cu(int dim, int mt) { return dim * mt <= 128 ? 3 : dim * mt <= 192 ? 2 : 1; }
 inline int kv_rows_workgroups(int dim, int mt) { return num_cus() * kv_rows_wgs_per_cu(dim, mt); }
-hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, int workgroups, hipStream_t st);
-hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, int workgroups, hipStream_t st);
+// workgroups: 0 = one per (sequence, KV head, tile of rows), no sequence has more than `rows` rows; else so many equal shares
+hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, int workgroups, int rows, hipStream_t st);
+hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, int workgroups, int rows, hipStream_t st);
 // prompt kernel (kv_prompt.h): waves of a workgroup, 32 query rows each, and how many of them a SIMD holds
 constexpr int kv_prompt_waves(int dim) { return dim == 128 ? 8 : 4; }
 constexpr int kv_prompt_waves_per_simd(int dim) { return dim <= 128 ? 2 : 1; }

@@ -24,11 +24,13 @@ namespace floe {
 constexpr int kRowsWaves = 4;
 constexpr float kWeightBits = 14.0f;
 
-// Units of one sequence: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on.
+// What one sequence costs: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on for each.  A segment (head,
+// tile) is priced as its units and kKvSegmentCost more: what its queries, page ids and meeting of the waves cost even where it has none.
 struct KvUnits {
     KvSpan span;
     int tiles, units, lo;
-    __device__ __forceinline__ int64_t all(int heads) const { return (int64_t)heads * tiles * units; }
+    __device__ __forceinline__ int64_t cost() const { return units + kKvSegmentCost; }
+    __device__ __forceinline__ int64_t all(int heads) const { return heads * tiles * cost(); }
 };
 template <int MT>
 __device__ __forceinline__ KvUnits kv_units(const KvAttnArgs& a, int seq) {
@@ -243,48 +245,61 @@ __device__ __forceinline__ void write_row4(const KvAttnArgs& a, int D, size_t ro
         a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
-template <int D, int FMT, int MT>
+// kWhole: a workgroup per segment (blockIdx.x = head and tile, blockIdx.y = sequence), nothing is split and nothing joined.
+template <int D, int FMT, int MT, bool kWhole>
 __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_wgs_per_cu(D, MT)) void kv_rows_kernel(KvAttnArgs a, int64_t min_share) {
     constexpr int kStride = D + 4;
     __shared__ float slab[kRowsWaves][16][kStride];
     __shared__ float ml[kRowsWaves][16 * MT][2];
     __shared__ int64_t scan_lds[kRowsWaves];
-    __shared__ int64_t found[2];  // units before the sequence, its number
-    __shared__ int64_t carry;
+    __shared__ int64_t found[3];  // cost before the sequence, its number, cost of all
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    // ---- the share of this workgroup
-    int64_t sum = 0;
-    for (int s = tid; s < a.s.n_seqs; s += 64 * kRowsWaves) sum += kv_units<MT>(a, s).all(a.c.heads);
-    sum = workgroup_scan<kRowsWaves>(sum, scan_lds);
-    if (tid == 64 * kRowsWaves - 1) found[0] = sum;
-    __syncthreads();
-    const int64_t total = found[0];
-    const int64_t even = (total + gridDim.x - 1) / gridDim.x, share = even > min_share ? even : min_share;
-    const int64_t u0 = blockIdx.x * share, u1 = u0 + share < total ? u0 + share : total;
-    __syncthreads();
-    if (blockIdx.x != 0 && u0 >= total) return;  // the whole workgroup
-    int64_t before = 0;
-    for (int s0 = 0; s0 < a.s.n_seqs; s0 += 64 * kRowsWaves) {
-        const int s = s0 + tid;
-        const int64_t mine = s < a.s.n_seqs ? kv_units<MT>(a, s).all(a.c.heads) : 0;
-        const int64_t upto = before + workgroup_scan<kRowsWaves>(mine, scan_lds);
-        if (u0 >= upto - mine && u0 < upto) {
-            found[0] = upto - mine;
-            found[1] = s;
+    int seq = 0;
+    int64_t u0 = 0, u1 = 0, in_seq = 0;
+    if constexpr (kWhole) {
+        seq = blockIdx.y;
+        const KvUnits w = kv_units<MT>(a, seq);
+        if ((int)blockIdx.x >= a.c.heads * w.tiles) return;
+        in_seq = blockIdx.x * w.cost();
+        u1 = w.cost();
+    } else {
+        // ---- the share of this workgroup
+        constexpr int kThreads = 64 * kRowsWaves;
+        int64_t before = 0;
+        for (int s0 = 0; s0 < a.s.n_seqs; s0 += kThreads) {
+            const int s = s0 + tid;
+            const int64_t mine = s < a.s.n_seqs ? kv_units<MT>(a, s).all(a.c.heads) : 0;
+            const int64_t upto = before + workgroup_scan<kRowsWaves>(mine, scan_lds);
+            if (tid == kThreads - 1) found[2] = upto;
+            if (blockIdx.x == 0 && s < a.s.n_seqs) a.plan[s] = upto - mine;
+            __syncthreads();
+            before = found[2];
+            if (s0 + kThreads >= a.s.n_seqs) {  // the last ones: where this share begins, if it is among them
+                const int64_t even = (before + gridDim.x - 1) / gridDim.x, share = even > min_share ? even : min_share;
+                u0 = blockIdx.x * share;
+                u1 = u0 + share < before ? u0 + share : before;
+                if (u0 >= upto - mine && u0 < upto) found[0] = upto - mine, found[1] = s;
+                if (blockIdx.x == 0 && tid == 0) a.plan[a.s.n_seqs] = before, a.plan[a.s.n_seqs + 1] = share;
+            }
         }
-        if (blockIdx.x == 0 && s < a.s.n_seqs) a.plan[s] = upto - mine;
-        if (tid == 64 * kRowsWaves - 1) carry = upto;
+        if (u0 >= before) return;  // the whole workgroup
         __syncthreads();
-        before = carry;
-        if (blockIdx.x != 0 && before > u0) break;
+        if (a.s.n_seqs > kThreads) {  // ... or among those before
+            int64_t upto_here = 0;
+            const int last0 = (a.s.n_seqs - 1) / kThreads * kThreads;
+            for (int s0 = 0; s0 < last0; s0 += kThreads) {
+                const int64_t mine = kv_units<MT>(a, s0 + tid).all(a.c.heads);
+                const int64_t upto = upto_here + workgroup_scan<kRowsWaves>(mine, scan_lds);
+                if (u0 >= upto - mine && u0 < upto) found[0] = upto - mine, found[1] = s0 + tid;
+                if (tid == kThreads - 1) found[2] = upto;
+                __syncthreads();
+                upto_here = found[2];
+                if (upto_here > u0) break;
+            }
+        }
+        seq = __builtin_amdgcn_readfirstlane((int)found[1]);
+        in_seq = u0 - found[0];
     }
-    if (blockIdx.x == 0 && tid == 0) {
-        a.plan[a.s.n_seqs] = total;
-        a.plan[a.s.n_seqs + 1] = share;
-    }
-    if (u0 >= total) return;  // nothing to do at all
-    int seq = __builtin_amdgcn_readfirstlane((int)found[1]);
-    int64_t in_seq = u0 - found[0];
     // ---- segments: (sequence, KV head, tile of rows)
     for (int64_t u = u0; u < u1;) {
         const KvUnits w = kv_units<MT>(a, seq);
@@ -294,12 +309,13 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_wgs_per_cu(D, MT)) void kv
             in_seq = 0;
             continue;
         }
-        const int tile_of_seq = (int)(in_seq / w.units);
-        const int j0 = (int)(in_seq - (int64_t)tile_of_seq * w.units);
-        const int j1 = (int)(w.units - j0 < u1 - u ? w.units : j0 + (u1 - u));
+        const int tile_of_seq = (int)(in_seq / w.cost());
+        const int64_t c0 = in_seq - tile_of_seq * w.cost(), left = w.cost() - c0, steps = left < u1 - u ? left : u1 - u;
+        const int j0 = (int)(c0 < kKvSegmentCost ? 0 : c0 - kKvSegmentCost), j1 = (int)(c0 + steps - kKvSegmentCost);
+        u += steps;
+        in_seq += steps;
+        if (j1 <= j0) continue;  // the share ends before the segment's first unit
         const int head = tile_of_seq / w.tiles, row0 = (tile_of_seq - head * w.tiles) * 16 * MT;
-        KvQueries<D, MT> Q;
-        load_queries<D, MT>(Q, a, w.span, head, row0, r, g);
         KvState<D, MT> st;
         int first_key[MT], last_key[MT];
 #pragma unroll
@@ -336,6 +352,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_wgs_per_cu(D, MT)) void kv
             return page;
         };
         if (n > 0) page_next = request(0, next);
+        KvQueries<D, MT> Q;
+        load_queries<D, MT>(Q, a, w.span, head, row0, r, g);
         for (int it = 0; it < n; ++it) {
             now = next;
             page_now = page_next;
@@ -396,8 +414,6 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_wgs_per_cu(D, MT)) void kv
             }
         }
         __syncthreads();
-        u += j1 - j0;
-        in_seq += j1 - j0;
     }
 }
 
@@ -413,7 +429,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     if (token >= w.span.rows) return;
     const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / (16 * MT);
     const int64_t share = a.plan[a.s.n_seqs + 1];
-    const int64_t from = a.plan[seq] + ((int64_t)head * w.tiles + tile) * w.units, to = from + w.units;
+    const int64_t from = a.plan[seq] + (head * w.tiles + tile) * w.cost() + kKvSegmentCost, to = from + w.units;  // of its units
     const int64_t w0 = from / share, w1 = (to - 1) / share;
     if (w0 == w1) return;  // one share had it all
     const int tid = threadIdx.x, lane = tid % kLanes, side = tid / kLanes, row = rr - tile * 16 * MT;

@@ -2,5 +2,7 @@
 #include "kv_rows_launch.h"
 
 namespace floe {
-hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, int workgroups, hipStream_t st) { return kv_rows_dispatch<kKvInt8>(a, mt, workgroups, st); }
+hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, int workgroups, int rows, hipStream_t st) {
+    return kv_rows_dispatch<kKvInt8>(a, mt, workgroups, rows, st);
+}
 }  // namespace floe
