@@ -185,11 +185,13 @@ def _ptr(t):
 
 # The current stream's handle without a Python object for it, 1 us a call (a name that torch does not promise: without it the object is made)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# (torch.cuda.current_device without its look at whether torch has been initialised: a tensor on the GPU has seen to that)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
     if stream is None and _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_current_device())
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
@@ -549,15 +551,16 @@ class KVCache:
                 raise ValueError(f"KVCache: expected a contiguous {kind} tensor of {size} elements, got {t.dtype} {tuple(t.shape)}")
         self._c = _KvCache(self.n_pages, self.kv_heads, self.head_dim, self.block, self.fmt, _KV_DTYPES[dtype], self.k.data_ptr(),
                            self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
+        self._at = C.addressof(self._c)
         self._ws = {}
 
-    def workspace(self, nbytes: int) -> torch.Tensor:
-        """Scratch of the attention calls on the current stream (one array per stream: calls on one stream are ordered)."""
-        key = _stream(None)
-        ws = self._ws.get(key)
-        if ws is None or ws.numel() < nbytes + 256:
-            ws = self._ws[key] = _workspace(nbytes, self.k.device)
-        return ws
+    def workspace(self, nbytes: int, stream: int):
+        """(address, bytes) of scratch for the attention calls on a stream: an array per stream, since the calls on one are ordered."""
+        ws = self._ws.get(stream)
+        if ws is None or ws[2] < nbytes:
+            array = _workspace(nbytes, self.k.device)
+            ws = self._ws[stream] = (array, *_aligned_ptr(array))
+        return ws[1], ws[2]
 
 
 class Rope:
@@ -569,6 +572,10 @@ class Rope:
         self.table, self.interleaved = table, bool(interleaved)
         self.n_positions, self.rot_dim = int(table.shape[0]), 2 * int(table.shape[1])
 
+    def _packed(self, positions):
+        return _ROPE_FIELDS.pack(self.table.data_ptr(), 0 if positions is None else positions.data_ptr(), self.n_positions, self.rot_dim,
+                                 self.interleaved)
+
 
 def floe_rope_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
     table = torch.empty((int(n_positions), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
@@ -576,25 +583,65 @@ def floe_rope_table(n_positions: int, rot_dim: int, base: float = 10000.0, devic
     return table
 
 
-def _kv_seqs(cu_rows, length, block_table, n_rows, max_rows) -> _KvSeqs:
-    n = cu_rows.shape[0] - 1
-    for t in (cu_rows, length, block_table):
-        if t.dtype != torch.int32 or not t.is_contiguous():
-            raise ValueError("cu_rows, lengths and block_table are contiguous int32 tensors")
-    if length.shape[0] != n or block_table.dim() != 2 or block_table.shape[0] != n:
-        raise ValueError(f"{n} sequences in cu_rows, {tuple(length.shape)} lengths, block_table {tuple(block_table.shape)}")
-    return _KvSeqs(n, int(n_rows), int(max_rows), block_table.shape[1], cu_rows.data_ptr(), length.data_ptr(), block_table.data_ptr())
+# A decode step of one sequence is bound by the host: what these calls hand over is packed at once (a structure filled field by field
+# costs a microsecond more), their functions take plain integers, and what is right is seen in one look (_kv_wrong says what is not).
+_SEQS_FIELDS, _ROPE_FIELDS, _ATTENTION_FIELDS = struct.Struct("4i3P"), struct.Struct("2P3i4x"), struct.Struct("4if")
+assert [f.size for f in (_SEQS_FIELDS, _ROPE_FIELDS, _ATTENTION_FIELDS)] == [C.sizeof(t) for t in (_KvSeqs, _Rope, _Attention)]
+_kv_functions = None
 
 
-def _kv_rows(t, cache: KVCache, heads, name: str, n_rows=None):
-    """A 16-bit tensor [rows][heads][head_dim] whose rows may lie anywhere: its row stride."""
-    if t.dtype != cache.dtype or t.dim() != 3 or t.shape[2] != cache.head_dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name}: expected {cache.dtype} [rows][{'heads' if heads is None else heads}][{cache.head_dim}], got {t.dtype} {tuple(t.shape)}")
-    if n_rows is not None and t.shape[0] != n_rows:
-        raise ValueError(f"{name}: {t.shape[0]} rows, expected {n_rows}")
-    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != cache.head_dim)):
-        raise ValueError(f"{name}: the heads of a row lie one behind the other (strides {t.stride()})")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * cache.head_dim
+def _kv_calls():
+    global _kv_functions
+    if _kv_functions is None:
+        lib, vp, i64, i32, packed, sz = load(), C.c_void_p, C.c_int64, C.c_int, C.c_char_p, C.c_size_t
+        append, gather, attention, need = (lib[n] for n in ("floe_kv_append", "floe_kv_gather", "floe_kv_attention",
+                                                            "floe_kv_attention_workspace_bytes"))
+        append.argtypes = [vp, packed, vp, i64, vp, i64, vp, i64, i32, vp, packed, vp]
+        gather.argtypes = [vp, packed, vp, vp, vp]
+        attention.argtypes = [vp, packed, packed, vp, i64, vp, vp, vp, sz, vp]
+        need.argtypes, need.restype = [vp, packed, packed], sz
+        _kv_functions = append, gather, attention, need
+    return _kv_functions
+
+
+def _kv_seqs(cu_rows, length, block_table, n_rows, max_rows) -> bytes:
+    n, i32 = cu_rows.shape[0] - 1, torch.int32
+    shape = block_table.shape
+    if not (cu_rows.dtype is i32 and length.dtype is i32 and block_table.dtype is i32 and cu_rows.is_contiguous() and length.is_contiguous()
+            and block_table.is_contiguous()):
+        raise ValueError("cu_rows, lengths and block_table are contiguous int32 tensors")
+    if length.shape[0] != n or len(shape) != 2 or shape[0] != n:
+        raise ValueError(f"{n} sequences in cu_rows, {tuple(length.shape)} lengths, block_table {tuple(shape)}")
+    return _SEQS_FIELDS.pack(n, n_rows, max_rows, shape[1], cu_rows.data_ptr(), length.data_ptr(), block_table.data_ptr())
+
+
+def _kv_wrong(t, cache, heads, n_rows, name):
+    shape = tuple(t.shape)
+    if t.dtype != cache.dtype or len(shape) != 3 or shape[1:] != (heads, cache.head_dim):
+        raise ValueError(f"{name}: expected {cache.dtype} [rows][{heads}][{cache.head_dim}], got {t.dtype} {shape}")
+    if shape[0] != n_rows:
+        raise ValueError(f"{name}: {shape[0]} rows, expected {n_rows}")
+    raise ValueError(f"{name}: the heads of a row lie one behind the other (strides {t.stride()})")
+
+
+def _kv_rows(t, cache: KVCache, heads, n_rows, name: str):
+    """Row stride of a 16-bit tensor [n_rows][heads][head_dim] whose rows may lie anywhere."""
+    shape, D = t.shape, cache.head_dim
+    if t.dtype is not cache.dtype or len(shape) != 3 or shape[2] != D or shape[1] != heads or shape[0] != n_rows:
+        _kv_wrong(t, cache, heads, n_rows, name)
+    stride = t.stride()
+    if (stride[2] != 1 or (stride[1] != D and heads > 1)) and n_rows:
+        _kv_wrong(t, cache, heads, n_rows, name)
+    return stride[0] if n_rows > 1 else heads * D
+
+
+def _kv_out(t, cache, shape, dtype, device, name):
+    """An output tensor: the caller's, if it fits, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t
 
 
 def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows: int, q=None, rope: Rope = None, positions=None,
@@ -602,60 +649,58 @@ def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows:
     """Appends k, v [rows][kv_heads][head_dim] behind the first length[s] tokens of each sequence; rope turns k, and q
     [rows][q_heads][head_dim] into q_out, which is returned (None without q).  max_rows: at least the rows of any sequence."""
     n_rows = k.shape[0]
-    ks, vs = _kv_rows(k, cache, cache.kv_heads, "k"), _kv_rows(v, cache, cache.kv_heads, "v", n_rows)
-    qs, heads = 0, 0
+    ks, vs = _kv_rows(k, cache, cache.kv_heads, n_rows, "k"), _kv_rows(v, cache, cache.kv_heads, n_rows, "v")
+    qs = heads = q_at = q_out_at = 0
     if q is not None:
-        qs, heads = _kv_rows(q, cache, None, "q", n_rows), q.shape[1]
-        if q_out is None:
-            q_out = torch.empty((n_rows, heads, cache.head_dim), dtype=cache.dtype, device=q.device)
-        elif tuple(q_out.shape) != (n_rows, heads, cache.head_dim) or q_out.dtype != cache.dtype or not q_out.is_contiguous():
-            raise ValueError(f"q_out: expected a contiguous {cache.dtype} tensor {(n_rows, heads, cache.head_dim)}")
+        shape = q.shape
+        heads = shape[1] if len(shape) == 3 else 0
+        qs, q_at = _kv_rows(q, cache, heads, n_rows, "q"), q.data_ptr()
+        q_out = _kv_out(q_out, cache, shape, cache.dtype, q.device, "q_out")
+        q_out_at = q_out.data_ptr()
     if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n_rows,) or not positions.is_contiguous()):
         raise ValueError(f"positions: expected contiguous int32 [{n_rows}]")
-    s = _kv_seqs(cu_rows, length, block_table, n_rows, max_rows)
-    r = None if rope is None else _Rope(rope.table.data_ptr(), None if positions is None else positions.data_ptr(), rope.n_positions,
-                                        rope.rot_dim, rope.interleaved)
-    _check(load().floe_kv_append(cache._c, s, k.data_ptr(), ks, v.data_ptr(), vs, None if q is None else q.data_ptr(), qs, heads,
-                                 None if q is None else q_out.data_ptr(), r, _stream(stream)), "floe_kv_append")
+    rc = _kv_calls()[0](cache._at, _kv_seqs(cu_rows, length, block_table, n_rows, max_rows), k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs,
+                        heads, q_out_at, None if rope is None else rope._packed(positions), _stream(stream))
+    if rc:
+        _check(rc, "floe_kv_append")
     return q_out if q is not None else None
 
 
 def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max_rows: int, k_out=None, v_out=None, stream=None):
     """Rows cu_rows[s] .. cu_rows[s + 1) are tokens first[s], first[s] + 1, ... of sequence s: (k, v) 16-bit [n_rows][kv_heads][head_dim]."""
-    shape = (int(n_rows), cache.kv_heads, cache.head_dim)
-    out = [torch.empty(shape, dtype=cache.dtype, device=cache.k.device) if t is None else t for t in (k_out, v_out)]
-    for t in out:
-        if tuple(t.shape) != shape or t.dtype != cache.dtype or not t.is_contiguous():
-            raise ValueError(f"floe_kv_gather: outputs are contiguous {cache.dtype} tensors {shape}")
-    s = _kv_seqs(cu_rows, first, block_table, n_rows, max_rows)
-    _check(load().floe_kv_gather(cache._c, s, out[0].data_ptr(), out[1].data_ptr(), _stream(stream)), "floe_kv_gather")
-    return out[0], out[1]
+    shape, device = (n_rows, cache.kv_heads, cache.head_dim), cache.k.device
+    k_out = _kv_out(k_out, cache, shape, cache.dtype, device, "k_out")
+    v_out = _kv_out(v_out, cache, shape, cache.dtype, device, "v_out")
+    rc = _kv_calls()[1](cache._at, _kv_seqs(cu_rows, first, block_table, n_rows, max_rows), k_out.data_ptr(), v_out.data_ptr(), _stream(stream))
+    if rc:
+        _check(rc, "floe_kv_gather")
+    return k_out, v_out
 
 
 def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows: int, max_len: int, scale: float = None,
                       causal: bool = True, window: int = 0, want_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
     """Attention of q [rows][q_heads][head_dim] over the cache; length[s] counts the rows' own tokens.  Returns out, or (out, lse) with
     want_lse.  scale: 1 / sqrt(head_dim) by default.  workspace: the cache's own (one per stream) unless handed over."""
-    qs, (n_rows, heads) = _kv_rows(q, cache, None, "q"), q.shape[:2]
-    if out is None:
-        out = torch.empty((n_rows, heads, cache.head_dim), dtype=cache.dtype, device=q.device)
-    elif tuple(out.shape) != tuple(q.shape) or out.dtype != cache.dtype or not out.is_contiguous():
-        raise ValueError(f"floe_kv_attention: out is a contiguous {cache.dtype} tensor {tuple(q.shape)}")
-    if want_lse and lse is None:
-        lse = torch.empty((n_rows, heads), dtype=torch.float32, device=q.device)
-    if lse is not None and (tuple(lse.shape) != (n_rows, heads) or lse.dtype != torch.float32 or not lse.is_contiguous()):
-        raise ValueError(f"floe_kv_attention: lse is a contiguous fp32 tensor {(n_rows, heads)}")
+    shape, device = q.shape, q.device
+    n_rows, heads = shape[0], shape[1] if len(shape) == 3 else 0
+    qs = _kv_rows(q, cache, heads, n_rows, "q")
+    out = _kv_out(out, cache, shape, cache.dtype, device, "out")
+    if want_lse or lse is not None:
+        lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, device, "lse")
+    call, need = _kv_calls()[2:]
     s = _kv_seqs(cu_rows, length, block_table, n_rows, max_rows)
-    a = _Attention(heads, int(causal), int(window), int(max_len), cache.head_dim ** -0.5 if scale is None else float(scale))
-    lib = load()
-    if workspace is None:
-        nbytes = lib.floe_kv_attention_workspace_bytes(cache._c, s, a)
-        if stream is None or stream == torch.cuda.current_stream():
-            workspace = cache.workspace(nbytes)
+    a = _ATTENTION_FIELDS.pack(heads, causal, window, max_len, cache.head_dim ** -0.5 if scale is None else scale)
+    st = _stream(stream)
+    at, size = cache.workspace(256, st) if workspace is None else _aligned_ptr(workspace)
+    args = cache._at, s, a, q.data_ptr(), qs, out.data_ptr(), None if lse is None else lse.data_ptr()
+    rc = call(*args, at, size, st)
+    if rc == -4 and workspace is None:  # refused before anything is enqueued: the cache's workspace has to grow
+        if stream is None:
+            at, size = cache.workspace(need(cache._at, s, a), st)
         else:
             with torch.cuda.stream(stream):
-                workspace = cache.workspace(nbytes)
-    wp, wn = _aligned_ptr(workspace)
-    _check(lib.floe_kv_attention(cache._c, s, a, q.data_ptr(), qs, out.data_ptr(), None if lse is None else lse.data_ptr(), wp, wn,
-                                 _stream(stream)), "floe_kv_attention")
+                at, size = cache.workspace(need(cache._at, s, a), st)
+        rc = call(*args, at, size, st)
+    if rc:
+        _check(rc, "floe_kv_attention")
     return (out, lse) if lse is not None else out

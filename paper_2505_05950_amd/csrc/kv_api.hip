@@ -48,42 +48,61 @@ int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_at
     if (a->q_heads > 1024 || a->window > kKvMaxLen) return FLOE_EUNSUPPORTED;
     // (the widest grid: a workgroup per 128 query rows of a KV head, or per row where there are few)
     const KvSeqs k = dev_seqs(s);
-    if (((int64_t)k.max_rows * (a->q_heads / c->kv_heads) / 128 + 1) * k.n_seqs * c->kv_heads > kMaxGrid) return FLOE_EUNSUPPORTED;
+    if (((int64_t)k.max_rows * (a->q_heads / c->kv_heads) / 128 + 4) * k.n_seqs * c->kv_heads > kMaxGrid) return FLOE_EUNSUPPORTED;
     if ((int64_t)k.max_rows * a->q_heads > 0x7fffffff) return FLOE_EUNSUPPORTED;
     return FLOE_OK;
 }
-// Which kernels a call runs, and its workspace: [partial sums][their maxima and sums][plan]
+// Which kernels a call runs, and its workspace: [partial sums][their maxima and sums]
 struct AttnPlan {
     bool rows, prompt;
     int most_rows;  // sequences of up to so many rows are the rows kernel's
-    int join_rows;  // at least the rows of any of those
-    int mt, workgroups;  // workgroups 0: no sequence is split
-    size_t ml_off, plan_off, total;
+    int row_limit;  // at least the rows of any of those
+    int mt, tiles, chunk, chunks, part_rows;
+    size_t ml_off, total;
 };
+// How segments (sequence, KV head, tile of rows) of up to `units` units of 32 tokens are cut into chunks: as many as give every compute
+// unit one, of 8 to 128 units.  One chunk where that is nearly all of a segment, or little: a join costs about as much as 10 units.
+// us, 32 / 8 heads of 128, chunks of 8, 16, 32, 64, 128 and whole segments: 1 sequence of 512 tokens 8.7 9.1 7.6 - - 7.6, 778: 8.9 10.5 10.2 -
+// - 10.2, 4096: 10.0 11.3 14.5 21.2 32.7 31.4, 16000: 16.1 14.4 15.8 21.9 35.0 107, 131000: 85 69 64 57 56 870; 8 sequences of 2048: 13.9
+// 13.5 15.5 20.8 18.8 18.9, 8000: 37 33 32 31 39 61; 32 of 2048: 37 35 32 31 29 29; 64 of 1000 to 16000: 286 250 239 236 236 245.
+void cut_segments(AttnPlan& w, int64_t segments, int64_t units) {
+    const int64_t cus = num_cus();
+    int64_t chunk = ((segments * units + cus - 1) / cus + 7) & ~(int64_t)7;
+    chunk = chunk < 8 ? 8 : chunk > 128 ? 128 : chunk;
+    if (units <= chunk + chunk / 4 || units <= 20) chunk = units;
+    const int64_t most = segments < kKvMostParts ? kKvMostParts / segments : 1;  // (bounds the workspace of many sequences)
+    int64_t chunks = (units + chunk - 1) / chunk;
+    if (chunks > most) chunks = most;
+    w.chunk = (int)((units + chunks - 1) / chunks);
+    w.chunks = (int)chunks;
+}
 AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
     AttnPlan w{};
     w.total = kAlign;  // (so that a workspace is a workspace whichever kernels run)
     const KvSeqs k = dev_seqs(s);
     const int group = a->q_heads / c->kv_heads, most = kKvRowsLimit / group;
     w.rows = true;
-    w.most_rows = w.join_rows = k.max_rows;
+    w.most_rows = w.row_limit = k.max_rows;
     if (k.max_rows > most) {
         // where no sequence can have few rows (n_rows are too many for that) the rows kernel has nothing to look for
         w.prompt = true;
-        w.rows = k.n_rows - (int64_t)(k.n_seqs - 1) * k.max_rows <= most;
+        w.rows = most > 0 && k.n_rows - (int64_t)(k.n_seqs - 1) * k.max_rows <= most;
         w.most_rows = w.rows ? most : 0;
-        w.join_rows = most;
-        if (most == 0) w.rows = false;
+        w.row_limit = most;
     }
     if (!w.rows) return w;
-    w.mt = kv_rows_tiles_for(c->head_dim, w.join_rows * group);
-    const int64_t keys = a->window > 0 && a->window + (int64_t)w.join_rows < a->max_len ? a->window + (int64_t)w.join_rows : a->max_len;
-    if (keys <= kKvWholeLen) return w;  // no sequence is split
-    w.workgroups = kv_rows_workgroups(c->head_dim, w.mt);
-    const size_t rows = (size_t)2 * w.workgroups * 16 * w.mt;
-    w.ml_off = align_up(rows * c->head_dim * 4);
-    w.plan_off = w.ml_off + align_up(rows * 8);
-    w.total = w.plan_off + align_up(((size_t)s->n_seqs + 2) * 8);
+    const int rows = w.row_limit * group;  // of a KV head
+    w.mt = kv_rows_tiles_for(c->head_dim, rows);
+    w.tiles = (rows + 16 * w.mt - 1) / (16 * w.mt);
+    const int64_t segments = (int64_t)k.n_seqs * c->kv_heads * w.tiles;
+    const int64_t keys = a->window > 0 && a->window + (int64_t)w.row_limit < a->max_len ? a->window + (int64_t)w.row_limit : a->max_len;
+    cut_segments(w, segments, (keys + kKvGroup - 1) / kKvGroup + 1);
+    if (w.chunks > 1) {
+        w.part_rows = rows < 16 * w.mt ? rows : 16 * w.mt;
+        const size_t parts = (size_t)segments * w.chunks * w.part_rows;
+        w.ml_off = align_up(parts * c->head_dim * 4);
+        w.total = w.ml_off + align_up(parts * 8);
+    }
     return w;
 }
 
@@ -188,15 +207,16 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     k.most_rows = w.most_rows;
     k.part_o = reinterpret_cast<float*>(base);
     k.part_ml = reinterpret_cast<float*>(base + w.ml_off);
-    k.plan = reinterpret_cast<int64_t*>(base + w.plan_off);
+    k.tiles = w.tiles;
+    k.chunk = w.chunk;
+    k.chunks = w.chunks;
+    k.part_rows = w.part_rows;
     hipStream_t st = (hipStream_t)stream;
     const bool int8 = c->format == FLOE_KV_INT8;
     if (w.prompt) FLOE_LAUNCH(FLOE_KERNEL_KV_PROMPT, st, int8 ? launch_kv_prompt_int8(k, st) : launch_kv_prompt_e4m3(k, st));
     if (w.rows) {
-        FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st,
-                    int8 ? launch_kv_rows_int8(k, w.mt, w.workgroups, w.join_rows, st)
-                         : launch_kv_rows_e4m3(k, w.mt, w.workgroups, w.join_rows, st));
-        if (w.workgroups) FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, w.join_rows, st));
+        FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st, int8 ? launch_kv_rows_int8(k, w.mt, st) : launch_kv_rows_e4m3(k, w.mt, st));
+        if (w.chunks > 1) FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, w.row_limit, st));
     }
     return FLOE_OK;
 }

@@ -39,26 +39,24 @@ struct KvAttnArgs {
     bool bf16;
     int most_rows;  // sequences of up to so many rows are the rows kernel's, the others the prompt kernel's
     // rows kernel (kv_rows.h)
-    float* part_o;   // [slots][16 MT][dim]
-    float* part_ml;  // [slots][16 MT][2]
-    int64_t* plan;   // [n_seqs + 2]: units before each sequence, all units, units per workgroup
+    float* part_o;   // [n_seqs][heads][tiles][chunks][part_rows][dim]
+    float* part_ml;  // [...][part_rows][2]
+    int tiles;       // of 16 mt rows, per KV head
+    int chunk, chunks;  // units of 32 tokens per chunk, chunks per segment
+    int part_rows;   // rows of a partial result
 };
 
+constexpr int64_t kKvMostParts = 65535;  // partial results of a call
 constexpr int kKvRowsLimit = 64;  // query rows per KV head up to which a sequence is the rows kernel's
-constexpr int kKvSegmentCost = 4;  // units that a segment costs beside its own
-constexpr int kKvMinShare = 12;    // two units per wave and one segment
-constexpr int kKvWholeLen = 512;   // sequences up to this length are not split
 // Tiles of sixteen rows that a workgroup of the rows kernel takes at once: as many as its registers hold beside two units of the cache
 constexpr int kv_rows_most_tiles(int dim) { return dim == 64 ? 4 : dim <= 192 ? 2 : 1; }
 inline int kv_rows_tiles_for(int dim, int rows) {
     const int most = kv_rows_most_tiles(dim), want = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
     return want < most ? want : most;
 }
-constexpr int kv_rows_wgs_per_cu(int dim, int mt) { return dim * mt <= 128 ? 3 : dim * mt <= 192 ? 2 : 1; }
-inline int kv_rows_workgroups(int dim, int mt) { return num_cus() * kv_rows_wgs_per_cu(dim, mt); }
-// workgroups: 0 = one per (sequence, KV head, tile of rows), no sequence has more than `rows` rows; else so many equal shares
-hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, int workgroups, int rows, hipStream_t st);
-hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, int workgroups, int rows, hipStream_t st);
+constexpr int kv_rows_waves_per_simd(int dim, int mt) { return dim * mt <= 128 ? 3 : dim * mt <= 256 && dim < 256 ? 2 : 1; }
+hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, hipStream_t st);  // mt tiles of sixteen rows per workgroup
+hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, hipStream_t st);
 // prompt kernel (kv_prompt.h): waves of a workgroup, 32 query rows each, and how many of them a SIMD holds
 constexpr int kv_prompt_waves(int dim) { return dim == 128 ? 8 : 4; }
 constexpr int kv_prompt_waves_per_simd(int dim) { return dim <= 128 ? 2 : 1; }

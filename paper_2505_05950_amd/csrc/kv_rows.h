@@ -11,10 +11,10 @@
 // lanes that hold the column, and the rows of S^T that a lane holds (tokens 4 g + i of two tiles) are exactly the operand of the
 // second product when V is stored in that order: the weights never leave their lane.
 //
-// What bounds it: the bytes of the cache.  All (sequence, KV head, tile of rows) x 32-token units of a call form one line that is
-// cut into equal shares, one per workgroup; a share that ends inside a sequence leaves a partial result, joined by kv_join_kernel.
-// So ragged batches and single long sequences fill the card alike.  The four waves of a workgroup take the units of its share in
-// turn, one unit ahead in registers.
+// What bounds it: the bytes of the cache, and for few short sequences the way to the first of them.  A workgroup takes one chunk of
+// one segment (sequence, KV head, tile of rows); its four waves take the chunk's units of 32 tokens in turn, one unit ahead in registers,
+// and meet in LDS at the end.  A segment of one chunk is finished there; the others leave a partial result per chunk, which
+// kv_join_kernel joins.  The card deals out the workgroups, so ragged batches and single long sequences fill it alike.
 #pragma once
 
 #include "kv_launch.h"
@@ -24,13 +24,10 @@ namespace floe {
 constexpr int kRowsWaves = 4;
 constexpr float kWeightBits = 14.0f;
 
-// What one sequence costs: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on for each.  A segment (head,
-// tile) is priced as its units and kKvSegmentCost more: what its queries, page ids and meeting of the waves cost even where it has none.
+// Units of one sequence: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on for each.
 struct KvUnits {
     KvSpan span;
     int tiles, units, lo;
-    __device__ __forceinline__ int64_t cost() const { return units + kKvSegmentCost; }
-    __device__ __forceinline__ int64_t all(int heads) const { return heads * tiles * cost(); }
 };
 template <int MT>
 __device__ __forceinline__ KvUnits kv_units(const KvAttnArgs& a, int seq) {
@@ -39,24 +36,11 @@ __device__ __forceinline__ KvUnits kv_units(const KvAttnArgs& a, int seq) {
     if (u.span.rows > a.most_rows) u.span.rows = 0;  // the prompt kernel's
     u.tiles = (u.span.rows * a.group + 16 * MT - 1) / (16 * MT);
     u.lo = a.window > 0 ? max(0, u.span.len - u.span.rows - a.window + 1) & ~(kKvGroup - 1) : 0;
-    u.units = max(1, (u.span.len - u.lo + kKvGroup - 1) / kKvGroup);
+    u.units = (u.span.len - u.lo + kKvGroup - 1) / kKvGroup;
     return u;
 }
-
-template <int N>
-__device__ __forceinline__ int64_t workgroup_scan(int64_t x, int64_t* lds) {  // inclusive, over the N waves of a workgroup
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const int64_t y = __shfl_up(x, o, kWave);
-        if (lane >= o) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) lds[w] = x;
-    __syncthreads();
-    for (int i = 0; i < w; ++i) x += lds[i];
-    return x;
-}
+// Chunks of a segment: a.chunk units each; the last of the a.chunks that the launch has takes whatever is left.
+__device__ __forceinline__ int kv_chunks(const KvAttnArgs& a, int units) { return min(max(1, (units + a.chunk - 1) / a.chunk), a.chunks); }
 
 template <int D, int FMT>
 struct KvFrag {  // one unit in registers
@@ -245,180 +229,121 @@ __device__ __forceinline__ void write_row4(const KvAttnArgs& a, int D, size_t ro
         a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
-// kWhole: a workgroup per segment (blockIdx.x = head and tile, blockIdx.y = sequence), nothing is split and nothing joined.
-template <int D, int FMT, int MT, bool kWhole>
-__global__ __launch_bounds__(64 * kRowsWaves, kv_rows_wgs_per_cu(D, MT)) void kv_rows_kernel(KvAttnArgs a, int64_t min_share) {
-    constexpr int kStride = D + 4;
-    __shared__ float slab[kRowsWaves][16][kStride];
-    __shared__ float ml[kRowsWaves][16 * MT][2];
-    __shared__ int64_t scan_lds[kRowsWaves];
-    __shared__ int64_t found[3];  // cost before the sequence, its number, cost of all
+template <int D, int FMT, int MT>
+__global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) void kv_rows_kernel(KvAttnArgs a) {
+    constexpr int NW = kRowsWaves, kStride = D + 4;
+    __shared__ float slab[NW][16][kStride];
+    __shared__ float ml[NW][16 * MT][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    int seq = 0;
-    int64_t u0 = 0, u1 = 0, in_seq = 0;
-    if constexpr (kWhole) {
-        seq = blockIdx.y;
-        const KvUnits w = kv_units<MT>(a, seq);
-        if ((int)blockIdx.x >= a.c.heads * w.tiles) return;
-        in_seq = blockIdx.x * w.cost();
-        u1 = w.cost();
-    } else {
-        // ---- the share of this workgroup
-        constexpr int kThreads = 64 * kRowsWaves;
-        int64_t before = 0;
-        for (int s0 = 0; s0 < a.s.n_seqs; s0 += kThreads) {
-            const int s = s0 + tid;
-            const int64_t mine = s < a.s.n_seqs ? kv_units<MT>(a, s).all(a.c.heads) : 0;
-            const int64_t upto = before + workgroup_scan<kRowsWaves>(mine, scan_lds);
-            if (tid == kThreads - 1) found[2] = upto;
-            if (blockIdx.x == 0 && s < a.s.n_seqs) a.plan[s] = upto - mine;
-            __syncthreads();
-            before = found[2];
-            if (s0 + kThreads >= a.s.n_seqs) {  // the last ones: where this share begins, if it is among them
-                const int64_t even = (before + gridDim.x - 1) / gridDim.x, share = even > min_share ? even : min_share;
-                u0 = blockIdx.x * share;
-                u1 = u0 + share < before ? u0 + share : before;
-                if (u0 >= upto - mine && u0 < upto) found[0] = upto - mine, found[1] = s;
-                if (blockIdx.x == 0 && tid == 0) a.plan[a.s.n_seqs] = before, a.plan[a.s.n_seqs + 1] = share;
-            }
-        }
-        if (u0 >= before) return;  // the whole workgroup
-        __syncthreads();
-        if (a.s.n_seqs > kThreads) {  // ... or among those before
-            int64_t upto_here = 0;
-            const int last0 = (a.s.n_seqs - 1) / kThreads * kThreads;
-            for (int s0 = 0; s0 < last0; s0 += kThreads) {
-                const int64_t mine = kv_units<MT>(a, s0 + tid).all(a.c.heads);
-                const int64_t upto = upto_here + workgroup_scan<kRowsWaves>(mine, scan_lds);
-                if (u0 >= upto - mine && u0 < upto) found[0] = upto - mine, found[1] = s0 + tid;
-                if (tid == kThreads - 1) found[2] = upto;
-                __syncthreads();
-                upto_here = found[2];
-                if (upto_here > u0) break;
-            }
-        }
-        seq = __builtin_amdgcn_readfirstlane((int)found[1]);
-        in_seq = u0 - found[0];
+    const int segments = a.c.heads * a.tiles, seq = blockIdx.x / segments, seg = blockIdx.x - seq * segments, chunk = blockIdx.y;
+    const int head = seg / a.tiles, tile = seg - head * a.tiles, row0 = tile * 16 * MT;
+    const KvUnits w = kv_units<MT>(a, seq);
+    const int n_chunks = kv_chunks(a, w.units);
+    if (tile >= w.tiles || chunk >= n_chunks) return;
+    const int j0 = chunk * a.chunk, j1 = chunk + 1 < n_chunks ? j0 + a.chunk : w.units;
+    KvState<D, MT> st;
+    int first_key[MT], last_key[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        st.top[m] = -__builtin_inff();
+        st.sum[m] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) st.o[m][d] = f32x4{0, 0, 0, 0};
+        const int token = min((row0 + 16 * m + r) / a.group, w.span.rows - 1), pos = w.span.len - w.span.rows + token;
+        first_key[m] = a.window > 0 ? pos - a.window + 1 : 0;
+        last_key[m] = a.causal ? pos : w.span.len - 1;
     }
-    // ---- segments: (sequence, KV head, tile of rows)
-    for (int64_t u = u0; u < u1;) {
-        const KvUnits w = kv_units<MT>(a, seq);
-        const int64_t all = w.all(a.c.heads);
-        if (in_seq >= all) {
-            ++seq;
-            in_seq = 0;
-            continue;
-        }
-        const int tile_of_seq = (int)(in_seq / w.cost());
-        const int64_t c0 = in_seq - tile_of_seq * w.cost(), left = w.cost() - c0, steps = left < u1 - u ? left : u1 - u;
-        const int j0 = (int)(c0 < kKvSegmentCost ? 0 : c0 - kKvSegmentCost), j1 = (int)(c0 + steps - kKvSegmentCost);
-        u += steps;
-        in_seq += steps;
-        if (j1 <= j0) continue;  // the share ends before the segment's first unit
-        const int head = tile_of_seq / w.tiles, row0 = (tile_of_seq - head * w.tiles) * 16 * MT;
-        KvState<D, MT> st;
-        int first_key[MT], last_key[MT];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            st.top[m] = -__builtin_inff();
-            st.sum[m] = 0.0f;
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) st.o[m][d] = f32x4{0, 0, 0, 0};
-            const int token = min((row0 + 16 * m + r) / a.group, w.span.rows - 1), pos = w.span.len - w.span.rows + token;
-            first_key[m] = a.window > 0 ? pos - a.window + 1 : 0;
-            last_key[m] = a.causal ? pos : w.span.len - 1;
-        }
-        // units between these need no mask
-        const int pos0 = w.span.len - w.span.rows + row0 / a.group;
-        const int pos1 = w.span.len - w.span.rows + min((row0 + 16 * MT - 1) / a.group, w.span.rows - 1);
-        const int clear_lo = a.window > 0 ? pos1 - a.window + 1 : 0;
-        const int clear_hi = a.causal ? pos0 + 1 : w.span.len;  // first token that some row does not see
-        const int end = a.causal ? pos1 + 1 : w.span.len;       // behind the last token that any row sees
-        const int upb = a.c.block / kKvGroup, unit0 = w.lo / kKvGroup;
-        int pages = -1;
-        auto fetch_pages = [&](int j) {  // pages of this wave's next 64 units
-            const int mine = j + kRowsWaves * lane;
-            pages = mine < j1 ? kv_page(a.s, a.c, seq, (unit0 + mine) / upb) : -1;
-        };
-        auto page_of = [&](int it) { return __builtin_amdgcn_readlane(pages, it & 63); };
-        const int n = (j1 - j0 - wave + kRowsWaves - 1) / kRowsWaves;  // units of this wave (may be none)
-        KvFrag<D, FMT> now, next;
-        int page_now = -1, page_next = -1;
-        auto request = [&](int it, KvFrag<D, FMT>& f) {
-            const int j = j0 + wave + kRowsWaves * it;
-            if ((it & 63) == 0) fetch_pages(j);
-            const int page = w.lo + j * kKvGroup >= end ? -1 : page_of(it);
-            load_unit<D, FMT>(f, a.c, head, page, ((unit0 + j) % upb) * kKvGroup, r, g);
-            return page;
-        };
-        if (n > 0) page_next = request(0, next);
+    // units between these need no mask
+    const int pos0 = w.span.len - w.span.rows + row0 / a.group;
+    const int pos1 = w.span.len - w.span.rows + min((row0 + 16 * MT - 1) / a.group, w.span.rows - 1);
+    const int clear_lo = a.window > 0 ? pos1 - a.window + 1 : 0;
+    const int clear_hi = a.causal ? pos0 + 1 : w.span.len;  // first token that some row does not see
+    const int end = a.causal ? pos1 + 1 : w.span.len;       // behind the last token that any row sees
+    const int upb = a.c.block / kKvGroup, unit0 = w.lo / kKvGroup;
+    int pages = -1;
+    auto fetch_pages = [&](int j) {  // pages of this wave's next 64 units
+        const int mine = j + NW * lane;
+        pages = mine < j1 ? kv_page(a.s, a.c, seq, (unit0 + mine) / upb) : -1;
+    };
+    auto page_of = [&](int it) { return __builtin_amdgcn_readlane(pages, it & 63); };
+    const int n = (j1 - j0 - wave + NW - 1) / NW;  // units of this wave (may be none)
+    KvFrag<D, FMT> f0, f1;  // a unit at work and the next on its way
+    int p0 = -1, p1 = -1;
+    // (without a condition: a wait behind a request that may not have been made is a wait for everything; the last unit comes again)
+    auto request = [&](int next, KvFrag<D, FMT>& f, int& page) {
+        const int it = min(next, n - 1), j = j0 + wave + NW * it;
+        if ((it & 63) == 0 && it == next) fetch_pages(j);
+        page = w.lo + j * kKvGroup >= end ? -1 : page_of(it);
+        load_unit<D, FMT>(f, a.c, head, page, ((unit0 + j) % upb) * kKvGroup, r, g);
+    };
+    if (n > 0) {
+        request(0, f0, p0);
         KvQueries<D, MT> Q;
         load_queries<D, MT>(Q, a, w.span, head, row0, r, g);
-        for (int it = 0; it < n; ++it) {
-            now = next;
-            page_now = page_next;
-            if (it + 1 < n) page_next = request(it + 1, next);
-            if (page_now < 0) continue;
-            const int token0 = w.lo + (j0 + wave + kRowsWaves * it) * kKvGroup;
-            take_unit<D, FMT, MT>(st, Q, now, a, token0 < clear_lo || token0 + kKvGroup > clear_hi, token0, w.span.len, first_key, last_key, g);
+        auto step = [&](int it, const KvFrag<D, FMT>& f, int page, KvFrag<D, FMT>& fill, int& fill_page) {
+            request(it + 1, fill, fill_page);
+            if (it >= n || page < 0) return;
+            const int token0 = w.lo + (j0 + wave + NW * it) * kKvGroup;
+            take_unit<D, FMT, MT>(st, Q, f, a, token0 < clear_lo || token0 + kKvGroup > clear_hi, token0, w.span.len, first_key, last_key, g);
+        };
+        for (int it = 0; it < n; it += 2) {
+            step(it, f0, p0, f1, p1);
+            step(it + 1, f1, p1, f0, p0);
         }
-        // ---- the four waves meet
-        const bool whole = j0 == 0 && j1 == w.units;
-        const size_t slot = 2 * (size_t)blockIdx.x + (j0 == 0 ? 1 : 0);
+    }
+    // ---- the four waves meet
+    const bool whole = n_chunks == 1;
+    const size_t part0 = ((size_t)blockIdx.x * a.chunks + chunk) * a.part_rows;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            st.sum[m] = quad_sum(st.sum[m]);
-            if (g == 0) {
-                ml[wave][16 * m + r][0] = st.top[m];
-                ml[wave][16 * m + r][1] = st.sum[m];
-            }
+    for (int m = 0; m < MT; ++m) {
+        st.sum[m] = quad_sum(st.sum[m]);
+        if (g == 0) {
+            ml[wave][16 * m + r][0] = st.top[m];
+            ml[wave][16 * m + r][1] = st.sum[m];
         }
-        __syncthreads();
+    }
+    __syncthreads();
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            float all_top = -__builtin_inff();
+    for (int m = 0; m < MT; ++m) {
+        float all_top = -__builtin_inff();
 #pragma unroll
-            for (int i = 0; i < kRowsWaves; ++i) all_top = fmaxf(all_top, ml[i][16 * m + r][0]);
-            const float f0 = weight_of(st.top[m], all_top);
-            if (m) __syncthreads();  // the slab of the tile before is read
+        for (int i = 0; i < NW; ++i) all_top = fmaxf(all_top, ml[i][16 * m + r][0]);
+        const float f0 = weight_of(st.top[m], all_top);
+        if (m) __syncthreads();  // the slab of the tile before is read
 #pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt) {
-                float* at = &slab[wave][r][32 * dt + 8 * g];
-                *reinterpret_cast<f32x4*>(at) = f32x4{st.o[m][2 * dt][0], st.o[m][2 * dt + 1][0], st.o[m][2 * dt][1], st.o[m][2 * dt + 1][1]} * f0;
-                *reinterpret_cast<f32x4*>(at + 4) = f32x4{st.o[m][2 * dt][2], st.o[m][2 * dt + 1][2], st.o[m][2 * dt][3], st.o[m][2 * dt + 1][3]} * f0;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) {
-                const int id = tid + 256 * i, row = id / (D / 4), d = (id - row * (D / 4)) * 4, rr = row0 + 16 * m + row;
-                if (rr >= w.span.rows * a.group) continue;
-                float top = -__builtin_inff(), l = 0.0f;
-                f32x4 o = {0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < kRowsWaves; ++k) top = fmaxf(top, ml[k][16 * m + row][0]);
-#pragma unroll
-                for (int k = 0; k < kRowsWaves; ++k) {
-                    l += ml[k][16 * m + row][1] * weight_of(ml[k][16 * m + row][0], top);
-                    o += *reinterpret_cast<const f32x4*>(&slab[k][row][d]);
-                }
-                if (whole) {
-                    const int token = rr / a.group;
-                    write_row4(a, D, w.span.row0 + token, head * a.group + rr - token * a.group, d, o, top, l);
-                } else {
-                    *reinterpret_cast<f32x4*>(a.part_o + ((slot * 16 * MT) + 16 * m + row) * D + d) = o;
-                    if (d == 0) {
-                        a.part_ml[(slot * 16 * MT + 16 * m + row) * 2] = top;
-                        a.part_ml[(slot * 16 * MT + 16 * m + row) * 2 + 1] = l;
-                    }
-                }
-            }
+        for (int dt = 0; dt < D / 32; ++dt) {
+            float* at = &slab[wave][r][32 * dt + 8 * g];
+            *reinterpret_cast<f32x4*>(at) = f32x4{st.o[m][2 * dt][0], st.o[m][2 * dt + 1][0], st.o[m][2 * dt][1], st.o[m][2 * dt + 1][1]} * f0;
+            *reinterpret_cast<f32x4*>(at + 4) = f32x4{st.o[m][2 * dt][2], st.o[m][2 * dt + 1][2], st.o[m][2 * dt][3], st.o[m][2 * dt + 1][3]} * f0;
         }
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            const int id = tid + 64 * NW * i, row = id / (D / 4), d = (id - row * (D / 4)) * 4, rr = row0 + 16 * m + row;
+            if (rr >= w.span.rows * a.group) continue;
+            float top = -__builtin_inff(), l = 0.0f;
+            f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < NW; ++k) top = fmaxf(top, ml[k][16 * m + row][0]);
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                l += ml[k][16 * m + row][1] * weight_of(ml[k][16 * m + row][0], top);
+                o += *reinterpret_cast<const f32x4*>(&slab[k][row][d]);
+            }
+            if (whole) {
+                const int token = rr / a.group;
+                write_row4(a, D, w.span.row0 + token, head * a.group + rr - token * a.group, d, o, top, l);
+            } else {
+                const size_t at = part0 + 16 * m + row;
+                *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = o;
+                if (d == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * at) = f32x2{top, l};
+            }
+        }
     }
 }
 
-// Joins the partial results of the rows whose units lay in several shares.  A workgroup takes one query row of one head; 256 / (D / 4)
-// pieces are read side by side.
+// Joins the partial results of the segments that have several chunks.  A workgroup takes one query row of one head; 256 / (D / 4)
+// chunks are read side by side.
 template <int D, int MT>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     constexpr int kLanes = D / 4, kSide = 256 / kLanes;
@@ -427,17 +352,16 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     const int seq = blockIdx.y, head_q = blockIdx.x % a.q_heads, token = blockIdx.x / a.q_heads;
     const KvUnits w = kv_units<MT>(a, seq);
     if (token >= w.span.rows) return;
+    const int n_chunks = kv_chunks(a, w.units);
+    if (n_chunks == 1) return;  // finished where it was formed
     const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / (16 * MT);
-    const int64_t share = a.plan[a.s.n_seqs + 1];
-    const int64_t from = a.plan[seq] + (head * w.tiles + tile) * w.cost() + kKvSegmentCost, to = from + w.units;  // of its units
-    const int64_t w0 = from / share, w1 = (to - 1) / share;
-    if (w0 == w1) return;  // one share had it all
+    const size_t first = (((size_t)seq * a.c.heads + head) * a.tiles + tile) * a.chunks;
     const int tid = threadIdx.x, lane = tid % kLanes, side = tid / kLanes, row = rr - tile * 16 * MT;
     float top = -__builtin_inff(), l = 0.0f;
     f32x4 o = {0, 0, 0, 0};
     if (side < kSide) {
-        for (int64_t p = w0 + side; p <= w1; p += kSide) {
-            const size_t at = (2 * (size_t)p + (p == w0 ? 1 : 0)) * 16 * MT + row;
+        for (int c = side; c < n_chunks; c += kSide) {
+            const size_t at = (first + c) * a.part_rows + row;
             const float t = a.part_ml[2 * at], s = a.part_ml[2 * at + 1];
             const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * lane);
             const float m = fmaxf(top, t), f0 = weight_of(top, m), f1 = weight_of(t, m);

@@ -6,33 +6,28 @@
 namespace floe {
 
 template <int FMT, int D, int MT>
-hipError_t kv_rows_instance(const KvAttnArgs& a, int workgroups, int rows, hipStream_t st) {
-    const dim3 wg(64 * kRowsWaves);
-    if (workgroups == 0) {
-        const int tiles = (rows * a.group + 16 * MT - 1) / (16 * MT);
-        kv_rows_kernel<D, FMT, MT, true><<<dim3(a.c.heads * tiles, a.s.n_seqs), wg, 0, st>>>(a, 0);
-    } else {
-        kv_rows_kernel<D, FMT, MT, false><<<dim3(workgroups), wg, 0, st>>>(a, kKvMinShare);
-    }
+hipError_t kv_rows_instance(const KvAttnArgs& a, hipStream_t st) {
+    const dim3 grid(a.s.n_seqs * a.c.heads * a.tiles, a.chunks);
+    kv_rows_kernel<D, FMT, MT><<<grid, dim3(64 * kRowsWaves), 0, st>>>(a);
     return hipGetLastError();
 }
 template <int FMT, int D>
-hipError_t kv_rows_tiles(const KvAttnArgs& a, int mt, int workgroups, int rows, hipStream_t st) {
+hipError_t kv_rows_tiles(const KvAttnArgs& a, int mt, hipStream_t st) {
     if constexpr (kv_rows_most_tiles(D) >= 4) {
-        if (mt == 4) return kv_rows_instance<FMT, D, 4>(a, workgroups, rows, st);
+        if (mt == 4) return kv_rows_instance<FMT, D, 4>(a, st);
     }
     if constexpr (kv_rows_most_tiles(D) >= 2) {
-        if (mt == 2) return kv_rows_instance<FMT, D, 2>(a, workgroups, rows, st);
+        if (mt == 2) return kv_rows_instance<FMT, D, 2>(a, st);
     }
-    return kv_rows_instance<FMT, D, 1>(a, workgroups, rows, st);
+    return kv_rows_instance<FMT, D, 1>(a, st);
 }
 template <int FMT>
-hipError_t kv_rows_dispatch(const KvAttnArgs& a, int mt, int workgroups, int rows, hipStream_t st) {
+hipError_t kv_rows_dispatch(const KvAttnArgs& a, int mt, hipStream_t st) {
     switch (a.c.dim) {
-        case 64: return kv_rows_tiles<FMT, 64>(a, mt, workgroups, rows, st);
-        case 128: return kv_rows_tiles<FMT, 128>(a, mt, workgroups, rows, st);
-        case 192: return kv_rows_tiles<FMT, 192>(a, mt, workgroups, rows, st);
-        default: return kv_rows_tiles<FMT, 256>(a, mt, workgroups, rows, st);
+        case 64: return kv_rows_tiles<FMT, 64>(a, mt, st);
+        case 128: return kv_rows_tiles<FMT, 128>(a, mt, st);
+        case 192: return kv_rows_tiles<FMT, 192>(a, mt, st);
+        default: return kv_rows_tiles<FMT, 256>(a, mt, st);
     }
 }
 
