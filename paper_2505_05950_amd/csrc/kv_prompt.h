@@ -167,19 +167,37 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
         if (it + 1 < n_tiles) request(it + 1);
         __syncthreads();
         if (!live_wave || t0 > w_hi || t0 + kPromptTokens <= w_lo || !(have[0] || have[1])) continue;
-        // ---- S^T
+        // ---- S^T: operands come from LDS four at a time, the next four on their way while these are multiplied; the two halves of the
+        // tile take turns, so that no product waits for the one before it
+        const uint4 *lk = &ldsK[buf][c32 * kChunks], *lv_ = &ldsV[buf][c32 * 8];
+        const int sw = c32 & 7;
         f32x16 s[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int j = 0; j < 16; ++j) s[0][j] = s[1][j] = 0.0f;
+        h16x8 kf[2][4];
+        auto load_k = [&](int group, h16x8* f) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[u][j] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const int t = 32 * u + c32;
-                const h16x8 kf = __builtin_bit_cast(h16x8, ldsK[buf][t * kChunks + ((2 * k + h) ^ (t & 7))]);
-                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, q[k], s[u], 0, 0, 0);
+            for (int i = 0; i < 4; ++i) {
+                const int k = 2 * group + (i >> 1), u = i & 1;
+                f[i] = __builtin_bit_cast(h16x8, lk[32 * u * kChunks + ((2 * k + h) ^ sw)]);
             }
+        };
+        load_k(0, kf[0]);
+#pragma unroll
+        for (int group = 0; group < D / 32; ++group) {
+            if (group + 1 < D / 32) load_k(group + 1, kf[(group + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[group & 1][i], q[2 * group + (i >> 1)], s[i & 1], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        h16x8 vf[2][D / 32];
+        auto load_v = [&](int k, h16x8* f) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) f[d] = __builtin_bit_cast(h16x8, lv_[32 * d * 8 + ((2 * k + h) ^ sw)]);
+        };
+        load_v(0, vf[0]);
         const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || !have[0] || !have[1];
         uint32_t unseen = 0;
         if (masked) {
@@ -233,7 +251,8 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             }
 #pragma unroll
             for (int j = 0; j < 16; ++j) part += s[u][j];
-            sum += part != 0.0f ? part * (1.0f / vs_now[u]) : 0.0f;
+            const float add = part * __builtin_amdgcn_rcpf(vs_now[u]);
+            sum += part != 0.0f ? add : 0.0f;  // (a block whose scale is NaN counts only where something of it is seen)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const h16x2 w = __builtin_convertvector(f32x2{s[u][2 * j], s[u][2 * j + 1]}, h16x2);
@@ -243,13 +262,13 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
         }
         // ---- O^T
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k) {
+            if (k + 1 < 4) load_v(k + 1, vf[(k + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
-                const int dim = 32 * d + c32;
-                const h16x8 vf = __builtin_bit_cast(h16x8, ldsV[buf][dim * 8 + ((2 * k + h) ^ (dim & 7))]);
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[k], o[d], 0, 0, 0);
-            }
+            for (int d = 0; d < D / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[k & 1][d], p[k], o[d], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     swap32(sum, ks[0], ks[1]);
     sum = ks[0] + ks[1];
