@@ -33,8 +33,11 @@ template <int D, int FMT, int NW>
 __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_prompt_kernel(KvAttnArgs a, int tiles_per_seq) {
     constexpr int kThreads = 64 * NW, kPieces = PromptStage<D, NW>::kPieces, kChunks = D / 8;
     static_assert(kPieces * kThreads == 4 * D, "a tile is dealt out evenly");
-    __shared__ uint4 ldsK[2][kPromptTokens * kChunks];  // [token][chunk ^ token % 8]: eight dims of a token
-    __shared__ uint4 ldsV[2][D * 8];                    // [dim][chunk ^ dim % 8]: chunk 2 s + h holds tokens 16 s + {4 h .. + 3, 8 + 4 h .. + 3}
+    // Pieces of sixteen bytes.  Where a piece of a row lies is turned by the row's number so that sixteen neighbouring rows, which sixteen
+    // lanes read at once, have it in sixteen different places of 256 bytes.
+    __shared__ uint4 ldsK[2][kPromptTokens * kChunks];  // [token][chunk ^ swizzle(token)]: eight dims of a token
+    __shared__ uint4 ldsV[2][D * 8];                    // [dim][chunk ^ (dim / 2) % 8]: chunk 2 s + h holds tokens 16 s + {4 h .. + 3, 8 + 4 h .. + 3}
+    auto swizzle = [](int t) { return kChunks % 16 == 0 ? t & 15 : (t >> 1) & 7; };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
     const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads;
     const int seq = rest % a.s.n_seqs, tile = tiles_per_seq - 1 - rest / a.s.n_seqs;  // the last rows of a prompt see most: they go first
@@ -132,8 +135,8 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             {
                 const int t = id / (D / 16), c = 2 * (id - t * (D / 16));
                 const uint4 w = next.k[i];
-                ldsK[buf][t * kChunks + (c ^ (t & 7))] = __builtin_bit_cast(uint4, codes_to_h8<FMT>(w.x, w.y));
-                ldsK[buf][t * kChunks + ((c + 1) ^ (t & 7))] = __builtin_bit_cast(uint4, codes_to_h8<FMT>(w.z, w.w));
+                ldsK[buf][t * kChunks + (c ^ swizzle(t))] = __builtin_bit_cast(uint4, codes_to_h8<FMT>(w.x, w.y));
+                ldsK[buf][t * kChunks + ((c + 1) ^ swizzle(t))] = __builtin_bit_cast(uint4, codes_to_h8<FMT>(w.z, w.w));
             }
             {
                 const int u = id / (2 * D), in = id - u * 2 * D, pair = in >> 2, g = in & 3;
@@ -152,7 +155,7 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         const int chunk = 2 * (2 * u + t) + (g & 1);
-                        row[2 * (chunk ^ (d & 7)) + (g >> 1)] = t ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y);
+                        row[2 * (chunk ^ ((d >> 1) & 7)) + (g >> 1)] = t ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y);
                     }
                 }
             }
@@ -170,7 +173,6 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
         // ---- S^T: operands come from LDS four at a time, the next four on their way while these are multiplied; the two halves of the
         // tile take turns, so that no product waits for the one before it
         const uint4 *lk = &ldsK[buf][c32 * kChunks], *lv_ = &ldsV[buf][c32 * 8];
-        const int sw = c32 & 7;
         f32x16 s[2];
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[0][j] = s[1][j] = 0.0f;
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = 2 * group + (i >> 1), u = i & 1;
-                f[i] = __builtin_bit_cast(h16x8, lk[32 * u * kChunks + ((2 * k + h) ^ sw)]);
+                f[i] = __builtin_bit_cast(h16x8, lk[32 * u * kChunks + ((2 * k + h) ^ swizzle(c32))]);
             }
         };
         load_k(0, kf[0]);
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
         h16x8 vf[2][D / 32];
         auto load_v = [&](int k, h16x8* f) {
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) f[d] = __builtin_bit_cast(h16x8, lv_[32 * d * 8 + ((2 * k + h) ^ sw)]);
+            for (int d = 0; d < D / 32; ++d) f[d] = __builtin_bit_cast(h16x8, lv_[32 * d * 8 + ((2 * k + h) ^ ((c32 >> 1) & 7))]);
         };
         load_v(0, vf[0]);
         const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || !have[0] || !have[1];
