@@ -94,6 +94,7 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[d][j] = 0.0f;
     float top = -__builtin_inff(), sum = 0.0f;
+    int page0 = -1, page1 = -1;  // of the tile at work
 
     const int upb = a.c.block / kKvGroup;
     int pages = -1;
@@ -105,20 +106,14 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
         return __builtin_amdgcn_readlane(pages, unit & 63);
     };
     PromptStage<D, NW> next;
-    int page[2] = {-1, -1};
-    float ks[2], vs[2];
-    auto request = [&](int it) {
+    auto request = [&](int it, const int* page) {  // codes of a tile
         const uint8_t *kp[2], *vp[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            page[u] = page_of(2 * it + u);
             const size_t slot = (size_t)max(page[u], 0) * a.c.heads + head;
-            const int unit = start / kKvGroup + 2 * it + u;
-            const size_t at = (slot * a.c.block + (unit % upb) * kKvGroup) * D;
+            const size_t at = (slot * a.c.block + ((start / kKvGroup + 2 * it + u) % upb) * kKvGroup) * D;
             kp[u] = scalar_ptr(a.c.k + at);
             vp[u] = scalar_ptr(a.c.v + at);
-            ks[u] = gloadf(a.c.k_scale + slot);
-            vs[u] = gloadf(a.c.v_scale + slot);
         }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
@@ -127,8 +122,33 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             next.v[i] = gload16((u ? vp[1] : vp[0]) + 16 * in);
         }
     };
-    auto convert = [&](int it, int buf) {
-        const int tokens_left = span.len - (start + it * kPromptTokens);  // of the tile
+    float ks[2], vs[2];
+    auto request_scales = [&](const int* page) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const size_t slot = (size_t)max(page[u], 0) * a.c.heads + head;
+            ks[u] = gloadf(a.c.k_scale + slot);
+            vs[u] = gloadf(a.c.v_scale + slot);
+        }
+    };
+    // Codes of V that no token of the sequence has (behind its end they are whatever the page held before, those of an absent page are
+    // nobody's) become zeros: bytes to keep of the two runs of four tokens in a piece, for either unit of the tile.
+    uint32_t keep[2][2] = {{~0u, ~0u}, {~0u, ~0u}};
+    auto set_keep = [&](int it, const int* page) {
+        const int g = tid & 3;  // (pieces of V: g is the fastest index, and a workgroup is a multiple of four threads)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int left = page[u] < 0 ? 0 : span.len - (start + it * kPromptTokens) - kKvGroup * u;
+            if (left >= kKvGroup) {
+                keep[u][0] = keep[u][1] = ~0u;
+            } else {
+                const int n0 = min(max(left - 4 * g, 0), 4), n1 = min(max(left - 16 - 4 * g, 0), 4);
+                keep[u][0] = n0 == 4 ? ~0u : (1u << (8 * n0)) - 1u;
+                keep[u][1] = n1 == 4 ? ~0u : (1u << (8 * n1)) - 1u;
+            }
+        }
+    };
+    auto convert = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int id = tid + i * kThreads;
@@ -140,13 +160,8 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             }
             {
                 const int u = id / (2 * D), in = id - u * 2 * D, pair = in >> 2, g = in & 3;
-                uint4 w = next.v[i];
-                const int left = (u ? page[1] : page[0]) < 0 ? 0 : tokens_left - 32 * u;
-                if (left < kKvGroup) {  // codes behind the last token are whatever the page held before, those of an absent page are nobody's
-                    const int n0 = min(max(left - 4 * g, 0), 4), n1 = min(max(left - 16 - 4 * g, 0), 4);
-                    const uint32_t m0 = n0 == 4 ? ~0u : (1u << (8 * n0)) - 1u, m1 = n1 == 4 ? ~0u : (1u << (8 * n1)) - 1u;
-                    w.x &= m0, w.y &= m1, w.z &= m0, w.w &= m1;
-                }
+                const uint32_t m0 = u ? keep[1][0] : keep[0][0], m1 = u ? keep[1][1] : keep[0][1];
+                const uint4 w = make_uint4(next.v[i].x & m0, next.v[i].y & m1, next.v[i].z & m0, next.v[i].w & m1);
 #pragma unroll
                 for (int par = 0; par < 2; ++par) {
                     const int d = 2 * pair + par;
@@ -161,70 +176,56 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             }
         }
     };
-    if (n_tiles > 0) request(0);
-    for (int it = 0; it < n_tiles; ++it) {
-        const int buf = it & 1, t0 = start + it * kPromptTokens;
-        convert(it, buf);
-        const float ks_now[2] = {ks[0], ks[1]}, vs_now[2] = {vs[0], vs[1]};
-        const bool have[2] = {page[0] >= 0, page[1] >= 0};
-        if (it + 1 < n_tiles) request(it + 1);
-        __syncthreads();
-        if (!live_wave || t0 > w_hi || t0 + kPromptTokens <= w_lo || !(have[0] || have[1])) continue;
-        // ---- S^T: operands come from LDS four at a time, the next four on their way while these are multiplied; the two halves of the
-        // tile take turns, so that no product waits for the one before it
-        const uint4 *lk = &ldsK[buf][c32 * kChunks], *lv_ = &ldsV[buf][c32 * 8];
-        f32x16 s[2];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[0][j] = s[1][j] = 0.0f;
-        h16x8 kf[2][4];
-        auto load_k = [&](int group, h16x8* f) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = 2 * group + (i >> 1), u = i & 1;
-                f[i] = __builtin_bit_cast(h16x8, lk[32 * u * kChunks + ((2 * k + h) ^ swizzle(c32))]);
-            }
-        };
-        load_k(0, kf[0]);
-#pragma unroll
-        for (int group = 0; group < D / 32; ++group) {
-            if (group + 1 < D / 32) load_k(group + 1, kf[(group + 1) & 1]);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[group & 1][i], q[2 * group + (i >> 1)], s[i & 1], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+    // One pass over a tile makes 4 D / 16 products per wave: S^T of its two units, then O^T of either.  Their operands come from LDS in
+    // that order, kAhead of them on the way.
+    constexpr int kStep = D / 16, kAhead = 4;
+    h16x8 ring[kAhead];
+    auto operand = [&](int buf, int i) {
+        if (i < 2 * kStep) {  // K: unit i / kStep, dims 16 (i % kStep) ..
+            const int u = i / kStep, k = i % kStep;
+            return __builtin_bit_cast(h16x8, ldsK[buf][(32 * u + c32) * kChunks + ((2 * k + h) ^ swizzle(c32))]);
         }
-        h16x8 vf[2][D / 32];
-        auto load_v = [&](int k, h16x8* f) {
+        const int j = i - 2 * kStep, k = j / (D / 32), d = j % (D / 32);  // V: tokens 16 k .., dims 32 d ..
+        return __builtin_bit_cast(h16x8, ldsV[buf][(32 * d + c32) * 8 + ((2 * k + h) ^ ((c32 >> 1) & 7))]);
+    };
+    f32x16 s[2];
+    h16x8 p[4];
+    float c[2], lv[2], rv[2];
+    // a fourth of the tile's products; what is written behind a call and needs none of them is put between them
+    auto products = [&](int buf, int part) {
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) f[d] = __builtin_bit_cast(h16x8, lv_[32 * d * 8 + ((2 * k + h) ^ ((c32 >> 1) & 7))]);
-        };
-        load_v(0, vf[0]);
-        const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || !have[0] || !have[1];
-        uint32_t unseen = 0;
+        for (int n = 0; n < kStep; ++n) {
+            const int i = part * kStep + n;
+            if (part < 2) s[part] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], q[n], s[part], 0, 0, 0);
+            else o[n % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], p[2 * (part - 2) + n / (D / 32)], o[n % (D / 32)], 0, 0, 0);
+            if (i + kAhead < 4 * kStep) ring[i % kAhead] = operand(buf, i + kAhead);
+        }
+    };
+    // mask and running maximum of the tile
+    auto maximum = [&](int t0, bool masked) {
         if (masked) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u) {
+                const bool poisoned = !(ks[u] == ks[u]) || !(vs[u] == vs[u]);  // a NaN scale: NaN for whoever sees a token, nothing for others
+                const float poison = poisoned ? __builtin_nanf("") : 0.0f;
+                const bool none = (u ? page1 : page0) < 0 || last_key < first_key;
+                const int lo = (none ? t0 + 2 * kPromptTokens : first_key) - (t0 + 32 * u + 4 * h);  // keys from here on, up to `more` behind, are seen
+                const uint32_t more = none ? 0 : last_key - first_key;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const int key = t0 + 32 * u + 8 * (j >> 2) + 4 * h + (j & 3);
-                    if (key < first_key || key > last_key || !have[u]) {
-                        s[u][j] = -__builtin_inff();
-                        unseen |= 1u << (16 * u + j);
-                    }
+                    const float x = s[u][j] + poison;
+                    s[u][j] = (uint32_t)(8 * (j >> 2) + (j & 3) - lo) > more ? -__builtin_inff() : x;
                 }
+                if (poisoned) c[u] = 1.0f, lv[u] = 0.0f, rv[u] = 1.0f;
+            }
         }
-        // ---- weights
-        float c[2], lv[2], mx = -__builtin_inff();
+        float mx = -__builtin_inff();
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float m = -__builtin_inff();
 #pragma unroll
             for (int j = 0; j < 16; ++j) m = fmaxf(m, s[u][j]);
-            c[u] = row_scale * ks_now[u];
-            lv[u] = __builtin_amdgcn_logf(vs_now[u]);
-            // (nothing seen: m is -inf, and must stay so whatever the scales are)
-            mx = fmaxf(mx, m == -__builtin_inff() ? m : __builtin_fmaf(m, c[u], lv[u]));
+            mx = fmaxf(mx, __builtin_fmaf(m, c[u], lv[u]));
         }
         float x0, x1;
         swap32(mx, x0, x1);
@@ -238,39 +239,68 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             for (int d = 0; d < D / 32; ++d) o[d] *= f;
             top = new_top;
         }
-        const float base = top == -__builtin_inff() ? 0.0f : top;
-        h16x8 p[4];
+    };
+    auto weights = [&](int u) {
+        const float off = lv[u] - (top == -__builtin_inff() ? 0.0f : top);
+        float part = 0.0f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float off = lv[u] - base;
-            float part = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) s[u][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][j], c[u], off));
-            if (masked) {  // (0 and NaN times -infinity are no weight either)
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (unseen & (1u << (16 * u + j))) s[u][j] = 0.0f;
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) part += s[u][j];
-            const float add = part * __builtin_amdgcn_rcpf(vs_now[u]);
-            sum += part != 0.0f ? add : 0.0f;  // (a block whose scale is NaN counts only where something of it is seen)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const h16x2 w = __builtin_convertvector(f32x2{s[u][2 * j], s[u][2 * j + 1]}, h16x2);
-                p[2 * u + (j >> 2)][2 * (j & 3)] = w.x;
-                p[2 * u + (j >> 2)][2 * (j & 3) + 1] = w.y;
-            }
+        for (int j = 0; j < 16; j += 2) {
+            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][j], c[u], off));
+            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][j + 1], c[u], off));
+            part += e0;
+            part += e1;
+            const h16x2 w = __builtin_convertvector(f32x2{e0, e1}, h16x2);
+            p[2 * u + (j >> 3)][j & 7] = w.x;
+            p[2 * u + (j >> 3)][(j & 7) + 1] = w.y;
         }
-        // ---- O^T
+        sum += part * rv[u];
+    };
+    int page_next[2], page_then[2];
+    if (n_tiles > 0) {
+        page0 = page_of(0), page1 = page_of(1);
+        const int now[2] = {page0, page1};
+        request(0, now);
+        request_scales(now);
+        set_keep(0, now);
+        convert(0);
+        page_next[0] = page_of(2), page_next[1] = page_of(3);
+        request(min(1, n_tiles - 1), page_next);
+        set_keep(1, page_next);
+    }
+    for (int it = 0; it < n_tiles; ++it) {
+        const int buf = it & 1, t0 = start + it * kPromptTokens;
+        page_then[0] = page_of(2 * it + 4), page_then[1] = page_of(2 * it + 5);
+        __syncthreads();  // this tile is in LDS, and nobody reads the one before it any more
+        {
+            const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || page0 < 0 || page1 < 0 || !(ks[0] * vs[0] + ks[1] * vs[1] > 0.0f);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (k + 1 < 4) load_v(k + 1, vf[(k + 1) & 1]);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < kAhead; ++i) ring[i] = operand(buf, i);
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[k & 1][d], p[k], o[d], 0, 0, 0);
+            for (int u = 0; u < 2; ++u) {
+                c[u] = fmaxf(row_scale * ks[u], 0x1p-126f);  // (-infinity times it has to stay that)
+                lv[u] = __builtin_amdgcn_logf(vs[u]);
+                rv[u] = __builtin_amdgcn_rcpf(vs[u]);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[u][j] = 0.0f;
+            }
             __builtin_amdgcn_sched_barrier(0);
+            products(buf, 0);
+            products(buf, 1);
+            convert(buf ^ 1);
+            __builtin_amdgcn_sched_barrier(0);
+            request(min(it + 2, n_tiles - 1), page_then);
+            maximum(t0, masked);
+            weights(0);
+            __builtin_amdgcn_sched_barrier(0);
+            products(buf, 2);
+            weights(1);
+            __builtin_amdgcn_sched_barrier(0);
+            request_scales(page_next);
+            products(buf, 3);
         }
+        set_keep(it + 2, page_then);
+        page0 = page_next[0], page1 = page_next[1];
+        page_next[0] = page_then[0], page_next[1] = page_then[1];
     }
     swap32(sum, ks[0], ks[1]);
     sum = ks[0] + ks[1];
