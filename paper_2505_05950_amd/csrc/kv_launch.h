@@ -57,9 +57,10 @@ inline int kv_rows_tiles_for(int dim, int rows) {
 constexpr int kv_rows_waves_per_simd(int dim, int mt) { return dim * mt <= 128 ? 3 : dim * mt <= 256 && dim < 256 ? 2 : 1; }
 hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, hipStream_t st);  // mt tiles of sixteen rows per workgroup
 hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, hipStream_t st);
-// prompt kernel (kv_prompt.h): waves of a workgroup, 32 query rows each, and how many of them a SIMD holds
-constexpr int kv_prompt_waves(int dim) { return dim == 128 ? 8 : 4; }
-constexpr int kv_prompt_waves_per_simd(int dim) { return dim <= 128 ? 2 : 1; }
+// prompt kernel (kv_prompt.h): waves of a workgroup, how many share 32 query rows, rows of a workgroup
+constexpr int kv_prompt_waves(int dim) { return dim == 64 ? 4 : 8; }
+constexpr int kv_prompt_split(int dim) { return dim == 256 ? 2 : 1; }
+constexpr int kv_prompt_rows(int dim) { return 32 * kv_prompt_waves(dim) / kv_prompt_split(dim); }
 hipError_t launch_kv_prompt_int8(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_prompt_e4m3(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_join(const KvAttnArgs& a, int mt, int rows, hipStream_t st);  // rows: at least those of any sequence it joins

@@ -20,32 +20,32 @@ constexpr int kPromptTokens = 64;             // of a tile: two units of 32, eac
 constexpr float kPromptBits = 7.0f;           // a row's largest weight is 2^7 when its base is set ...
 constexpr float kPromptTop = 15.0f;           // ... and may grow to 2^15 before it is set again
 
-// rows of a workgroup and workgroups that a sequence's rows make
-constexpr int kv_prompt_rows(int waves) { return 32 * waves; }
-
 template <int D, int NW>
 struct PromptStage {  // a thread's share of a tile on its way: 16-byte pieces of the codes
-    static constexpr int kPieces = 4 * D / (64 * NW);
+    static constexpr int kPieces = (4 * D + 64 * NW - 1) / (64 * NW);
     uint4 k[kPieces], v[kPieces];
 };
 
 template <int D, int FMT, int NW>
-__global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_prompt_kernel(KvAttnArgs a, int tiles_per_seq) {
+__global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a, int tiles_per_seq) {
+    // kSplit waves share 32 rows: each forms all of S^T and the weights, and a part of the dims of O^T (whose registers bound the waves)
     constexpr int kThreads = 64 * NW, kPieces = PromptStage<D, NW>::kPieces, kChunks = D / 8;
-    static_assert(kPieces * kThreads == 4 * D, "a tile is dealt out evenly");
+    constexpr int kSplit = kv_prompt_split(D), kRowWaves = NW / kSplit, kOut = D / 32 / kSplit;
+    constexpr bool kEven = kPieces * kThreads == 4 * D;
     // Pieces of sixteen bytes.  Where a piece of a row lies is turned by the row's number so that sixteen neighbouring rows, which sixteen
     // lanes read at once, have it in sixteen different places of 256 bytes.
     __shared__ uint4 ldsK[2][kPromptTokens * kChunks];  // [token][chunk ^ swizzle(token)]: eight dims of a token
     __shared__ uint4 ldsV[2][D * 8];                    // [dim][chunk ^ (dim / 2) % 8]: chunk 2 s + h holds tokens 16 s + {4 h .. + 3, 8 + 4 h .. + 3}
     auto swizzle = [](int t) { return kChunks % 16 == 0 ? t & 15 : (t >> 1) & 7; };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
+    const int row_wave = kSplit == 1 ? wave : wave % kRowWaves, out0 = kSplit == 1 ? 0 : wave / kRowWaves * kOut;  // this wave's rows and its first 32 dims of the output
     const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads;
     const int seq = rest % a.s.n_seqs, tile = tiles_per_seq - 1 - rest / a.s.n_seqs;  // the last rows of a prompt see most: they go first
     const KvSpan span = kv_span(a.s, seq);
-    const int all_rows = span.rows * a.group, row0 = tile * 32 * NW;
+    const int all_rows = span.rows * a.group, row0 = tile * 32 * kRowWaves;
     if (row0 >= all_rows || span.rows <= a.most_rows) return;
     // ---- queries of this wave
-    const int rr = row0 + 32 * wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.len - span.rows + token;
+    const int rr = row0 + 32 * row_wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.len - span.rows + token;
     const bool there = rr < all_rows;
     const int head_q = head * a.group + (there ? rr - token * a.group : 0);
     h16x8 q[D / 16];
@@ -78,19 +78,17 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
     // ---- tokens that the workgroup and this wave's rows see
     const int first_key = a.window > 0 ? pos - a.window + 1 : 0, last_key = a.causal ? pos : span.len - 1;
     const int base_pos = span.len - span.rows;
-    const int wg_last = base_pos + min((row0 + 32 * NW - 1) / a.group, span.rows - 1), wg_first = base_pos + row0 / a.group;
-    const int w_first = base_pos + min((row0 + 32 * wave) / a.group, span.rows - 1);
-    const int w_last = base_pos + min((row0 + 32 * wave + 31) / a.group, span.rows - 1);
+    const int wg_last = base_pos + min((row0 + 32 * kRowWaves - 1) / a.group, span.rows - 1), wg_first = base_pos + row0 / a.group;
+    const int w_first = base_pos + min((row0 + 32 * row_wave) / a.group, span.rows - 1);
+    const int w_last = base_pos + min((row0 + 32 * row_wave + 31) / a.group, span.rows - 1);
     const int end = a.causal ? wg_last + 1 : span.len;  // behind the last token that any row sees
     const int start = a.window > 0 ? max(0, wg_first - a.window + 1) & ~(kPromptTokens - 1) : 0;
     const int n_tiles = max(0, (end - start + kPromptTokens - 1) / kPromptTokens);
-    const int w_lo = a.window > 0 ? w_first - a.window + 1 : 0, w_hi = a.causal ? w_last : span.len - 1;     // any row sees
     const int w_clear_lo = a.window > 0 ? w_last - a.window + 1 : 0, w_clear_hi = a.causal ? w_first : span.len - 1;  // every row sees
-    const bool live_wave = row0 + 32 * wave < all_rows;
 
-    f32x16 o[D / 32];
+    f32x16 o[kOut];
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+    for (int d = 0; d < kOut; ++d)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[d][j] = 0.0f;
     float top = -__builtin_inff(), sum = 0.0f;
@@ -117,7 +115,8 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
         }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int id = tid + i * kThreads, u = id / (2 * D), in = id - u * 2 * D;  // (2 D is a multiple of the wave: u is the same in a wave)
+            const int id = kEven ? tid + i * kThreads : min(tid + i * kThreads, 4 * D - 1);
+            const int u = id / (2 * D), in = id - u * 2 * D;  // (2 D is a multiple of the wave: u is the same in a wave)
             next.k[i] = gload16((u ? kp[1] : kp[0]) + 16 * in);
             next.v[i] = gload16((u ? vp[1] : vp[0]) + 16 * in);
         }
@@ -152,6 +151,7 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int id = tid + i * kThreads;
+            if (!kEven && id >= 4 * D) break;  // (a whole wave)
             {
                 const int t = id / (D / 16), c = 2 * (id - t * (D / 16));
                 const uint4 w = next.k[i];
@@ -176,29 +176,31 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             }
         }
     };
-    // One pass over a tile makes 4 D / 16 products per wave: S^T of its two units, then O^T of either.  Their operands come from LDS in
+    // One pass over a tile makes 2 D / 16 + 4 kOut products per wave: S^T of its two units, then O^T of either.  Their operands come from LDS in
     // that order, kAhead of them on the way.
-    constexpr int kStep = D / 16, kAhead = 4;
+    constexpr int kStep = D / 16, kAhead = D == 192 ? 2 : 4;  // (four are more than the registers hold at D 192: 297 us, with two 285)
     h16x8 ring[kAhead];
     auto operand = [&](int buf, int i) {
         if (i < 2 * kStep) {  // K: unit i / kStep, dims 16 (i % kStep) ..
             const int u = i / kStep, k = i % kStep;
             return __builtin_bit_cast(h16x8, ldsK[buf][(32 * u + c32) * kChunks + ((2 * k + h) ^ swizzle(c32))]);
         }
-        const int j = i - 2 * kStep, k = j / (D / 32), d = j % (D / 32);  // V: tokens 16 k .., dims 32 d ..
+        const int j = i - 2 * kStep, k = j / kOut, d = out0 + j % kOut;  // V: tokens 16 k .., dims 32 d ..
         return __builtin_bit_cast(h16x8, ldsV[buf][(32 * d + c32) * 8 + ((2 * k + h) ^ ((c32 >> 1) & 7))]);
     };
     f32x16 s[2];
     h16x8 p[4];
     float c[2], lv[2], rv[2];
-    // a fourth of the tile's products; what is written behind a call and needs none of them is put between them
-    auto products = [&](int buf, int part) {
+    // those of one unit: S^T (parts 0 and 1) or O^T (2 and 3); what is written behind a call and needs none of them goes between them
+    auto products = [&](int buf, auto part_) {
+        constexpr int part = decltype(part_)::value, n_here = part < 2 ? kStep : 2 * kOut;
+        constexpr int first = part < 2 ? part * kStep : 2 * kStep + (part - 2) * 2 * kOut;
 #pragma unroll
-        for (int n = 0; n < kStep; ++n) {
-            const int i = part * kStep + n;
-            if (part < 2) s[part] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], q[n], s[part], 0, 0, 0);
-            else o[n % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], p[2 * (part - 2) + n / (D / 32)], o[n % (D / 32)], 0, 0, 0);
-            if (i + kAhead < 4 * kStep) ring[i % kAhead] = operand(buf, i + kAhead);
+        for (int n = 0; n < n_here; ++n) {
+            const int i = first + n;
+            if constexpr (part < 2) s[part] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], q[n], s[part], 0, 0, 0);
+            else o[n % kOut] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], p[2 * (part - 2) + n / kOut], o[n % kOut], 0, 0, 0);
+            if (i + kAhead < 2 * kStep + 4 * kOut) ring[i % kAhead] = operand(buf, i + kAhead);
         }
     };
     // mask and running maximum of the tile
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
             const float f = move ? __builtin_amdgcn_exp2f(top - new_top) : 1.0f;
             sum *= f;
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d) o[d] *= f;
+            for (int d = 0; d < kOut; ++d) o[d] *= f;
             top = new_top;
         }
     };
@@ -284,19 +286,19 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
                 for (int j = 0; j < 16; ++j) s[u][j] = 0.0f;
             }
             __builtin_amdgcn_sched_barrier(0);
-            products(buf, 0);
-            products(buf, 1);
+            products(buf, std::integral_constant<int, 0>());
+            products(buf, std::integral_constant<int, 1>());
             convert(buf ^ 1);
             __builtin_amdgcn_sched_barrier(0);
             request(min(it + 2, n_tiles - 1), page_then);
             maximum(t0, masked);
             weights(0);
             __builtin_amdgcn_sched_barrier(0);
-            products(buf, 2);
+            products(buf, std::integral_constant<int, 2>());
             weights(1);
             __builtin_amdgcn_sched_barrier(0);
             request_scales(page_next);
-            products(buf, 3);
+            products(buf, std::integral_constant<int, 3>());
         }
         set_keep(it + 2, page_then);
         page0 = page_next[0], page1 = page_next[1];
@@ -306,10 +308,10 @@ __global__ __launch_bounds__(64 * NW, kv_prompt_waves_per_simd(D)) void kv_promp
     sum = ks[0] + ks[1];
     if (!there) return;
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+    for (int d = 0; d < kOut; ++d)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            write_row4(a, D, span.row0 + token, head_q, 32 * d + 8 * j + 4 * h, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, top, sum);
+            write_row4(a, D, span.row0 + token, head_q, 32 * (out0 + d) + 8 * j + 4 * h, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, top, sum);
 }
 
 }  // namespace floe
