@@ -52,13 +52,14 @@ int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_at
     if ((int64_t)k.max_rows * a->q_heads > 0x7fffffff) return FLOE_EUNSUPPORTED;
     return FLOE_OK;
 }
-// Which kernels a call runs, and its workspace: [partial sums][their maxima and sums]
+// Which kernels a call runs, and its workspace: [partial sums][their bases and sums of weights] of the rows kernel, and of the prompt kernel
 struct AttnPlan {
     bool rows, prompt;
     int most_rows;  // sequences of up to so many rows are the rows kernel's
     int row_limit;  // at least the rows of any of those
     int mt, tiles, chunk, chunks, part_rows;
-    size_t ml_off, total;
+    int prompt_tiles, prompt_chunk, prompt_chunks;
+    size_t rows_off, ml_off, prompt_ml_off, total;  // (the prompt kernel's come first)
 };
 // How segments (sequence, KV head, tile of rows) of up to `units` units of 32 tokens are cut into chunks: as many as give every compute
 // unit one, of 8 to 128 units.  One chunk where that is nearly all of a segment, or little: a join costs about as much as 10 units.
@@ -76,11 +77,19 @@ void cut_segments(AttnPlan& w, int64_t segments, int64_t units) {
     w.chunk = (int)((units + chunks - 1) / chunks);
     w.chunks = (int)chunks;
 }
+// Tiles of rows that do not fill the card are cut into chunks of their tokens, of at least four tiles of 64.
+void cut_prompts(AttnPlan& w, int64_t segments, int64_t tiles) {
+    int64_t chunks = num_cus() / segments;
+    if (chunks > tiles / 4) chunks = tiles / 4;
+    if (chunks < 1) chunks = 1;
+    w.prompt_chunk = (int)((tiles + chunks - 1) / chunks);
+    w.prompt_chunks = (int)chunks;
+}
 AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
     AttnPlan w{};
     w.total = kAlign;  // (so that a workspace is a workspace whichever kernels run)
     const KvSeqs k = dev_seqs(s);
-    const int group = a->q_heads / c->kv_heads, most = kKvRowsLimit / group;
+    const int group = a->q_heads / c->kv_heads, most = kv_rows_limit(c->head_dim) / group;
     w.rows = true;
     w.most_rows = w.row_limit = k.max_rows;
     if (k.max_rows > most) {
@@ -90,17 +99,33 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
         w.most_rows = w.rows ? most : 0;
         w.row_limit = most;
     }
+    const int64_t max_keys = a->max_len;
+    if (w.prompt) {
+        const int64_t tile_rows = kv_prompt_rows(c->head_dim);
+        w.prompt_tiles = (int)(((int64_t)k.max_rows * group + tile_rows - 1) / tile_rows);
+        const int64_t keys = a->window > 0 && a->window + tile_rows < max_keys ? a->window + tile_rows : max_keys;
+        const int64_t segments = (int64_t)k.n_seqs * c->kv_heads * w.prompt_tiles;
+        cut_prompts(w, segments, (keys + 63) / 64 + 1);
+        if ((int64_t)a->q_heads * k.max_rows > kMaxGrid) w.prompt_chunks = 1;  // (more rows than a join has workgroups)
+        if (w.prompt_chunks > 1) {
+            const size_t parts = (size_t)segments * w.prompt_chunks * tile_rows;
+            w.prompt_ml_off = align_up(parts * c->head_dim * 4);
+            w.total = w.prompt_ml_off + align_up(parts * 8);
+        }
+    }
     if (!w.rows) return w;
     const int rows = w.row_limit * group;  // of a KV head
     w.mt = kv_rows_tiles_for(c->head_dim, rows);
     w.tiles = (rows + 16 * w.mt - 1) / (16 * w.mt);
     const int64_t segments = (int64_t)k.n_seqs * c->kv_heads * w.tiles;
-    const int64_t keys = a->window > 0 && a->window + (int64_t)w.row_limit < a->max_len ? a->window + (int64_t)w.row_limit : a->max_len;
+    const int64_t keys = a->window > 0 && a->window + (int64_t)w.row_limit < max_keys ? a->window + (int64_t)w.row_limit : max_keys;
     cut_segments(w, segments, (keys + kKvGroup - 1) / kKvGroup + 1);
     if (w.chunks > 1) {
         w.part_rows = rows < 16 * w.mt ? rows : 16 * w.mt;
         const size_t parts = (size_t)segments * w.chunks * w.part_rows;
-        w.ml_off = align_up(parts * c->head_dim * 4);
+        const size_t rows_off = w.total > kAlign ? w.total : 0;
+        w.rows_off = rows_off;
+        w.ml_off = rows_off + align_up(parts * c->head_dim * 4);
         w.total = w.ml_off + align_up(parts * 8);
     }
     return w;
@@ -205,15 +230,21 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     k.window = a->window;
     k.bf16 = c->dtype == FLOE_BF16;
     k.most_rows = w.most_rows;
-    k.part_o = reinterpret_cast<float*>(base);
-    k.part_ml = reinterpret_cast<float*>(base + w.ml_off);
+    k.parts = KvParts{reinterpret_cast<float*>(base + w.rows_off), reinterpret_cast<float*>(base + w.ml_off)};
+    k.prompt_parts = KvParts{reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + w.prompt_ml_off)};
+    k.prompt_tiles = w.prompt_tiles;
+    k.prompt_chunk = w.prompt_chunk;
+    k.prompt_chunks = w.prompt_chunks;
     k.tiles = w.tiles;
     k.chunk = w.chunk;
     k.chunks = w.chunks;
     k.part_rows = w.part_rows;
     hipStream_t st = (hipStream_t)stream;
     const bool int8 = c->format == FLOE_KV_INT8;
-    if (w.prompt) FLOE_LAUNCH(FLOE_KERNEL_KV_PROMPT, st, int8 ? launch_kv_prompt_int8(k, st) : launch_kv_prompt_e4m3(k, st));
+    if (w.prompt) {
+        FLOE_LAUNCH(FLOE_KERNEL_KV_PROMPT, st, int8 ? launch_kv_prompt_int8(k, st) : launch_kv_prompt_e4m3(k, st));
+        if (w.prompt_chunks > 1) FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_prompt_join(k, st));
+    }
     if (w.rows) {
         FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st, int8 ? launch_kv_rows_int8(k, w.mt, st) : launch_kv_rows_e4m3(k, w.mt, st));
         if (w.chunks > 1) FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, w.row_limit, st));

@@ -1,5 +1,5 @@
-// Joins what the shares of the rows kernel left (kv_rows.h).
-#include "kv_rows.h"
+// Joins what the chunks of the attention kernels left (kv_rows.h, kv_prompt.h).
+#include "kv_prompt.h"
 
 namespace floe {
 
@@ -24,6 +24,23 @@ hipError_t launch_kv_join(const KvAttnArgs& a, int mt, int rows, hipStream_t st)
         case 128: return join_tiles<128>(a, mt, rows, st);
         case 192: return join_tiles<192>(a, mt, rows, st);
         default: return join_tiles<256>(a, mt, rows, st);
+    }
+}
+
+namespace {
+template <int D>
+hipError_t prompt_join(const KvAttnArgs& a, hipStream_t st) {
+    kv_prompt_join_kernel<D><<<dim3(a.q_heads * a.s.max_rows, a.s.n_seqs), dim3(256), 0, st>>>(a);
+    return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_kv_prompt_join(const KvAttnArgs& a, hipStream_t st) {
+    switch (a.c.dim) {
+        case 64: return prompt_join<64>(a, st);
+        case 128: return prompt_join<128>(a, st);
+        case 192: return prompt_join<192>(a, st);
+        default: return prompt_join<256>(a, st);
     }
 }
 

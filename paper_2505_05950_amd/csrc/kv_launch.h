@@ -26,6 +26,12 @@ hipError_t launch_kv_append(const KvCache& c, const KvSeqs& s, const KvAppendArg
 hipError_t launch_kv_gather(const KvCache& c, const KvSeqs& s, uint16_t* k_out, uint16_t* v_out, int format, bool bf16, hipStream_t st);
 hipError_t launch_rope_table(float* table, int n_positions, int rot, double base, hipStream_t st);
 
+// partial results: sums of rows of `dim` values, and per row the exponent's base and the sum of the weights
+struct KvParts {
+    float* o;
+    float* ml;
+};
+
 struct KvAttnArgs {
     KvCache c;
     KvSeqs s;  // len: tokens of each sequence, the call's own among them
@@ -39,15 +45,21 @@ struct KvAttnArgs {
     bool bf16;
     int most_rows;  // sequences of up to so many rows are the rows kernel's, the others the prompt kernel's
     // rows kernel (kv_rows.h)
-    float* part_o;   // [n_seqs][heads][tiles][chunks][part_rows][dim]
-    float* part_ml;  // [...][part_rows][2]
-    int tiles;       // of 16 mt rows, per KV head
+    KvParts parts;      // [n_seqs][heads][tiles][chunks][part_rows]
+    int tiles;          // of 16 mt rows, per KV head
     int chunk, chunks;  // units of 32 tokens per chunk, chunks per segment
-    int part_rows;   // rows of a partial result
+    int part_rows;      // rows of a partial result
+    // prompt kernel (kv_prompt.h)
+    KvParts prompt_parts;  // [n_seqs][heads][prompt_tiles][prompt_chunks][rows of a tile]
+    int prompt_tiles;      // of kv_prompt_rows(dim) rows, per KV head
+    int prompt_chunk, prompt_chunks;  // tiles of 64 tokens per chunk, chunks per tile of rows
 };
 
 constexpr int64_t kKvMostParts = 65535;  // partial results of a call
-constexpr int kKvRowsLimit = 64;  // query rows per KV head up to which a sequence is the rows kernel's
+// Query rows per KV head up to which a sequence is the rows kernel's.  us, rows / prompt kernel, 32 / 8 heads of 128: 36 rows (9 tokens) of 1
+// sequence of 8000 16.4 / 22.2, 8 of 8000 51 / 88, 64 of 1000 52 / 86; 68 rows 23.3 / 23.6, 79 / 87, 74 / 90; 132 rows 30.8 / 27.4, 126 / 96,
+// 123 / 97 (1 of 1000: 13.8 / 22.2).  16 / 4 heads of 256, 4 of 3000: 68 rows 29.5 / 33.  8 / 8 heads of 64: 33 rows 16.8 / 18, 65 rows 22.1 / 20.2.
+constexpr int kv_rows_limit(int dim) { return dim == 64 ? 64 : 128; }
 // Tiles of sixteen rows that a workgroup of the rows kernel takes at once: as many as its registers hold beside two units of the cache
 constexpr int kv_rows_most_tiles(int dim) { return dim == 64 ? 4 : dim <= 192 ? 2 : 1; }
 inline int kv_rows_tiles_for(int dim, int rows) {
@@ -63,6 +75,7 @@ constexpr int kv_prompt_split(int dim) { return dim == 256 ? 2 : 1; }
 constexpr int kv_prompt_rows(int dim) { return 32 * kv_prompt_waves(dim) / kv_prompt_split(dim); }
 hipError_t launch_kv_prompt_int8(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_prompt_e4m3(const KvAttnArgs& a, hipStream_t st);
+hipError_t launch_kv_prompt_join(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_join(const KvAttnArgs& a, int mt, int rows, hipStream_t st);  // rows: at least those of any sequence it joins
 
 }  // namespace floe

@@ -26,8 +26,23 @@ struct PromptStage {  // a thread's share of a tile on its way: 16-byte pieces o
     uint4 k[kPieces], v[kPieces];
 };
 
+// The tokens that a tile of rows sees: `n` tiles of 64 from `start` on, cut into chunks as a.prompt_chunk says.
+struct PromptRange {
+    int start, n, chunks;
+};
+__device__ __forceinline__ PromptRange prompt_range(const KvAttnArgs& a, const KvSpan& span, int row0, int rows) {
+    const int first = span.len - span.rows + row0 / a.group, last = span.len - span.rows + min((row0 + rows - 1) / a.group, span.rows - 1);
+    const int end = a.causal ? last + 1 : span.len;  // behind the last token that any row sees
+    PromptRange r;
+    r.start = a.window > 0 ? max(0, first - a.window + 1) & ~(kPromptTokens - 1) : 0;
+    r.n = max(0, (end - r.start + kPromptTokens - 1) / kPromptTokens);
+    r.chunks = min(max(1, (r.n + a.prompt_chunk - 1) / a.prompt_chunk), a.prompt_chunks);
+    return r;
+}
+
+// blockIdx.x: KV head, sequence, tile of rows; blockIdx.y: chunk of the tokens (one, unless the card would not be filled)
 template <int D, int FMT, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a, int tiles_per_seq) {
+__global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
     // kSplit waves share 32 rows: each forms all of S^T and the weights, and a part of the dims of O^T (whose registers bound the waves)
     constexpr int kThreads = 64 * NW, kPieces = PromptStage<D, NW>::kPieces, kChunks = D / 8;
     constexpr int kSplit = kv_prompt_split(D), kRowWaves = NW / kSplit, kOut = D / 32 / kSplit;
@@ -40,10 +55,15 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a, int
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
     const int row_wave = kSplit == 1 ? wave : wave % kRowWaves, out0 = kSplit == 1 ? 0 : wave / kRowWaves * kOut;  // this wave's rows and its first 32 dims of the output
     const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads;
-    const int seq = rest % a.s.n_seqs, tile = tiles_per_seq - 1 - rest / a.s.n_seqs;  // the last rows of a prompt see most: they go first
+    const int seq = rest % a.s.n_seqs, tile = a.prompt_tiles - 1 - rest / a.s.n_seqs;  // the last rows of a prompt see most: they go first
     const KvSpan span = kv_span(a.s, seq);
     const int all_rows = span.rows * a.group, row0 = tile * 32 * kRowWaves;
     if (row0 >= all_rows || span.rows <= a.most_rows) return;
+    const PromptRange range = prompt_range(a, span, row0, 32 * kRowWaves);
+    const int chunk = blockIdx.y;
+    if (chunk >= range.chunks) return;
+    const int start = range.start + chunk * a.prompt_chunk * kPromptTokens;
+    const int n_tiles = chunk + 1 < range.chunks ? a.prompt_chunk : range.n - chunk * a.prompt_chunk;
     // ---- queries of this wave
     const int rr = row0 + 32 * row_wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.len - span.rows + token;
     const bool there = rr < all_rows;
@@ -78,12 +98,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a, int
     // ---- tokens that the workgroup and this wave's rows see
     const int first_key = a.window > 0 ? pos - a.window + 1 : 0, last_key = a.causal ? pos : span.len - 1;
     const int base_pos = span.len - span.rows;
-    const int wg_last = base_pos + min((row0 + 32 * kRowWaves - 1) / a.group, span.rows - 1), wg_first = base_pos + row0 / a.group;
     const int w_first = base_pos + min((row0 + 32 * row_wave) / a.group, span.rows - 1);
     const int w_last = base_pos + min((row0 + 32 * row_wave + 31) / a.group, span.rows - 1);
-    const int end = a.causal ? wg_last + 1 : span.len;  // behind the last token that any row sees
-    const int start = a.window > 0 ? max(0, wg_first - a.window + 1) & ~(kPromptTokens - 1) : 0;
-    const int n_tiles = max(0, (end - start + kPromptTokens - 1) / kPromptTokens);
     const int w_clear_lo = a.window > 0 ? w_last - a.window + 1 : 0, w_clear_hi = a.causal ? w_first : span.len - 1;  // every row sees
 
     f32x16 o[kOut];
@@ -126,8 +142,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a, int
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const size_t slot = (size_t)max(page[u], 0) * a.c.heads + head;
-            ks[u] = gloadf(a.c.k_scale + slot);
-            vs[u] = gloadf(a.c.v_scale + slot);
+            const float k = gloadf(a.c.k_scale + slot), v = gloadf(a.c.v_scale + slot);
+            ks[u] = page[u] < 0 ? 1.0f : k;  // (page 0 stands in for an absent one: what its scales hold is nobody's)
+            vs[u] = page[u] < 0 ? 1.0f : v;
         }
     };
     // Codes of V that no token of the sequence has (behind its end they are whatever the page held before, those of an absent page are
@@ -307,11 +324,35 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a, int
     swap32(sum, ks[0], ks[1]);
     sum = ks[0] + ks[1];
     if (!there) return;
+    if (range.chunks == 1) {
+#pragma unroll
+        for (int d = 0; d < kOut; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                write_row4(a, D, span.row0 + token, head_q, 32 * (out0 + d) + 8 * j + 4 * h, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, top, sum);
+        return;
+    }
+    const size_t segment = ((size_t)seq * a.c.heads + head) * a.prompt_tiles + tile;
+    const size_t at = (segment * a.prompt_chunks + chunk) * (32 * kRowWaves) + 32 * row_wave + c32;
 #pragma unroll
     for (int d = 0; d < kOut; ++d)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            write_row4(a, D, span.row0 + token, head_q, 32 * (out0 + d) + 8 * j + 4 * h, f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]}, top, sum);
+            *reinterpret_cast<f32x4*>(a.prompt_parts.o + at * D + 32 * (out0 + d) + 8 * j + 4 * h) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    if (out0 == 0 && h == 0) *reinterpret_cast<f32x2*>(a.prompt_parts.ml + 2 * at) = f32x2{top, sum};
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void kv_prompt_join_kernel(KvAttnArgs a) {
+    constexpr int kRows = kv_prompt_rows(D);
+    const int seq = blockIdx.y, head_q = blockIdx.x % a.q_heads, token = blockIdx.x / a.q_heads;
+    const KvSpan span = kv_span(a.s, seq);
+    if (token >= span.rows || span.rows <= a.most_rows) return;
+    const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / kRows;
+    const PromptRange range = prompt_range(a, span, tile * kRows, kRows);
+    if (range.chunks == 1) return;  // finished where it was formed
+    const size_t segment = ((size_t)seq * a.c.heads + head) * a.prompt_tiles + tile;
+    join_row<D>(a, a.prompt_parts, segment * a.prompt_chunks * kRows + rr - tile * kRows, kRows, range.chunks, span.row0 + token, head_q);
 }
 
 }  // namespace floe

@@ -7,9 +7,9 @@ namespace floe {
 
 template <int FMT, int D>
 hipError_t kv_prompt_instance(const KvAttnArgs& a, hipStream_t st) {
-    constexpr int kWaves = kv_prompt_waves(D), kRows = kv_prompt_rows(D);
-    const int tiles = (int)(((int64_t)a.s.max_rows * a.group + kRows - 1) / kRows);
-    kv_prompt_kernel<D, FMT, kWaves><<<dim3(tiles * a.s.n_seqs * a.c.heads), dim3(64 * kWaves), 0, st>>>(a, tiles);
+    constexpr int kWaves = kv_prompt_waves(D);
+    const dim3 grid(a.prompt_tiles * a.s.n_seqs * a.c.heads, a.prompt_chunks);
+    kv_prompt_kernel<D, FMT, kWaves><<<grid, dim3(64 * kWaves), 0, st>>>(a);
     return hipGetLastError();
 }
 template <int FMT>

@@ -343,35 +343,28 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
                 write_row4(a, D, w.span.row0 + token, head * a.group + rr - token * a.group, d, o, top, l);
             } else {
                 const size_t at = part0 + 16 * m + row;
-                *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = o;
-                if (d == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * at) = f32x2{top, l};
+                *reinterpret_cast<f32x4*>(a.parts.o + at * D + d) = o;
+                if (d == 0) *reinterpret_cast<f32x2*>(a.parts.ml + 2 * at) = f32x2{top, l};
             }
         }
     }
 }
 
-// Joins the partial results of the segments that have several chunks.  A workgroup takes one query row of one head; 256 / (D / 4)
-// chunks are read side by side.
-template <int D, int MT>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
+// Joins the `n` partial results of one query row of one head, which lie at `first`, first + step, ...: a workgroup of 256 threads, of
+// which 256 / (D / 4) partial results are read side by side.
+template <int D>
+__device__ __forceinline__ void join_row(const KvAttnArgs& a, const KvParts& parts, size_t first, int step, int n, size_t row, int head) {
     constexpr int kLanes = D / 4, kSide = 256 / kLanes;
     __shared__ f32x4 so[kSide][kLanes];
     __shared__ float sm[kSide], sl[kSide];
-    const int seq = blockIdx.y, head_q = blockIdx.x % a.q_heads, token = blockIdx.x / a.q_heads;
-    const KvUnits w = kv_units<MT>(a, seq);
-    if (token >= w.span.rows) return;
-    const int n_chunks = kv_chunks(a, w.units);
-    if (n_chunks == 1) return;  // finished where it was formed
-    const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / (16 * MT);
-    const size_t first = (((size_t)seq * a.c.heads + head) * a.tiles + tile) * a.chunks;
-    const int tid = threadIdx.x, lane = tid % kLanes, side = tid / kLanes, row = rr - tile * 16 * MT;
+    const int tid = threadIdx.x, lane = tid % kLanes, side = tid / kLanes;
     float top = -__builtin_inff(), l = 0.0f;
     f32x4 o = {0, 0, 0, 0};
     if (side < kSide) {
-        for (int c = side; c < n_chunks; c += kSide) {
-            const size_t at = (first + c) * a.part_rows + row;
-            const float t = a.part_ml[2 * at], s = a.part_ml[2 * at + 1];
-            const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * lane);
+        for (int c = side; c < n; c += kSide) {
+            const size_t at = first + (size_t)c * step;
+            const float t = parts.ml[2 * at], s = parts.ml[2 * at + 1];
+            const f32x4 x = *reinterpret_cast<const f32x4*>(parts.o + at * D + 4 * lane);
             const float m = fmaxf(top, t), f0 = weight_of(top, m), f1 = weight_of(t, m);
             o = o * f0 + x * f1;
             l = l * f0 + s * f1;
@@ -389,7 +382,19 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
         l = l * f0 + sl[i] * f1;
         top = m;
     }
-    write_row4(a, D, w.span.row0 + token, head_q, 4 * lane, o, top, l);
+    write_row4(a, D, row, head, 4 * lane, o, top, l);
+}
+// A workgroup per query row and head, of the segments that have several chunks.
+template <int D, int MT>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
+    const int seq = blockIdx.y, head_q = blockIdx.x % a.q_heads, token = blockIdx.x / a.q_heads;
+    const KvUnits w = kv_units<MT>(a, seq);
+    if (token >= w.span.rows) return;
+    const int n_chunks = kv_chunks(a, w.units);
+    if (n_chunks == 1) return;  // finished where it was formed
+    const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / (16 * MT);
+    const size_t segment = ((size_t)seq * a.c.heads + head) * a.tiles + tile;
+    join_row<D>(a, a.parts, segment * a.chunks * a.part_rows + rr - tile * 16 * MT, a.part_rows, n_chunks, w.span.row0 + token, head_q);
 }
 
 }  // namespace floe

@@ -87,6 +87,54 @@ def test_chunks_of_prompts(fmt, dtype, D, P, heads, qh, window):
     check(m, table, lens, n_q, qh, dtype, True, window, rng=rng)
 
 
+@pytest.mark.parametrize("D,heads,qh,P", [(64, 1, 2, 32), (128, 2, 8, 32), (192, 1, 3, 128), (256, 1, 2, 64)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 90), (False, 200)])
+def test_long_and_short_chunks_in_one_call(D, heads, qh, P, causal, window):
+    """Both kernels in one call; tiles of rows that are cut over their tokens, rows and tiles that are not full."""
+    rng = np.random.default_rng(D + window)
+    lens, n_q = [700, 90, 3, 0, 260, 130], [150, 90, 1, 0, 2, 129]
+    m, table = build(rng, lens, heads, D, P, "e4m3" if D % 128 else "int8", "fp16")
+    check(m, table, lens, n_q, qh, "fp16", causal, window, rng=rng)
+    check(m, table[:1], [700], [150], qh, "bf16", causal, window, rng=rng)
+    check(m, table[:1], [700], [150], qh, "fp16", causal, window, rng=rng, max_len=1, scale=-0.05)  # max_len only chooses
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_long_chunks_with_absent_pages_nan_blocks_and_extreme_scales(fmt):
+    rng = np.random.default_rng(21)
+    lens, n_q = [500, 330], [160, 200]
+    m, table = build(rng, lens, 1, 128, 32, fmt, "bf16", v_spread=6.0)
+    check(m, table, lens, n_q, 2, "bf16", rng=rng)
+    check(m, table, lens, n_q, 2, "bf16", scale=0.0, rng=rng)
+    table[0][2], table[1][0], table[1][9] = -1, 1 << 30, -7
+    check(m, table, lens, n_q, 2, "bf16", rng=rng)
+    check(m, [t[:5] for t in table], lens, n_q, 2, "bf16", rng=rng)
+    m.scale[0][table[0][11], 0] = np.nan
+    m.scale[1][table[1][4], 0] = np.nan
+    check(m, table, lens, n_q, 2, "bf16", rng=rng)
+    check(m, table, lens, n_q, 2, "bf16", window=40, rng=rng)
+    check(m, table, [100, 20], [160, 200], 2, "bf16", rng=rng)  # more rows than tokens
+
+
+@pytest.mark.parametrize("garbage", [0.0, -1.0, np.inf, np.nan, 1e-42])
+def test_pages_of_nobody_hold_anything(garbage):
+    """Codes and scales that no token has, page 0 among them, which an absent page's address falls on."""
+    rng = np.random.default_rng(4)
+    lens = [300, 200]
+    table, pages = tables(rng, lens, 32)
+    table = [[p + 1 if p >= 0 else p for p in t] for t in table]
+    m = R.Model(pages + 1, 1, 128, 32, "e4m3")
+    for s, n in enumerate(lens):
+        for which in (0, 1):
+            m.append(which, rng.normal(0, 1, (n, 1, 128)).astype(np.float32), 0, table[s])
+    unused = ~m.known.any(axis=1)
+    for scale in m.scale:
+        scale[unused] = garbage
+    table[0][4] = table[1][0] = table[1][1] = -1
+    check(m, table, lens, [1, 2], 4, "fp16", rng=rng)
+    check(m, table, lens, [150, 120], 2, "fp16", rng=rng)
+
+
 def test_more_rows_than_tokens_and_absent_pages():
     rng = np.random.default_rng(3)
     lens = [3, 100, 130, 96]
