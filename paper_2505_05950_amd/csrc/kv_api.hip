@@ -166,7 +166,7 @@ int floe_kv_append(const floe_kv_cache* c, const floe_kv_seqs* s, const void* k,
     if ((rc = check_arrays(s))) return rc;
     if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return FLOE_EINVAL;
     const KvSeqs ds = dev_seqs(s);
-    const int64_t q_groups = q ? (int64_t)ds.n_rows * ((q_heads * (c->head_dim / 16) + 255) / 256) : 0;
+    const int64_t q_groups = q ? ((int64_t)ds.n_rows + 3) / 4 : 0;
     if (block_tasks(c, ds) + q_groups > kMaxGrid) return FLOE_EUNSUPPORTED;
     KvAppendArgs a{};
     a.k = static_cast<const uint16_t*>(k);

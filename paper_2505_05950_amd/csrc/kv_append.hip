@@ -46,42 +46,44 @@ __device__ __forceinline__ PairUnit pair_unit(int p, int rot, bool interleaved) 
     u.b = half ? (rot >> 1) + 8 * p : 16 * p + 8;
     return u;
 }
-// Loads a unit of a row and turns it: x[0..8) and x[8..16) are the two halves.  A position outside the table gives NaN.
-template <bool BF16>
-__device__ __forceinline__ void load_turned(const uint16_t* row, const PairUnit& u, const KvRope& r, int pos, float* x) {
-    unpack8<BF16>(gload16(row + u.a), x);
-    unpack8<BF16>(gload16(row + u.b), x + 8);
-    if (!u.turns) return;
-    if ((unsigned)pos >= (unsigned)r.n_positions) {
+// The (cos, sin) pairs of a unit at a position: pairs of dims (a + j, b + j) in halves, (a + 2 j, a + 2 j + 1) over all sixteen when
+// interleaved.  A position outside the table gives NaN, a unit that does not turn (1, 0), which leaves it as it is.
+struct Turns {
+    float c[8], s[8];
+};
+__device__ __forceinline__ Turns load_turns(const PairUnit& u, const KvRope& r, int pos) {
+    Turns t;
+    const bool there = (unsigned)pos < (unsigned)r.n_positions;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = __builtin_nanf("");
-        return;
-    }
-    // the pairs of this unit: dims (a + j, b + j) in halves, (a + 2 j, a + 2 j + 1) over all sixteen when interleaved
-    const int first = r.interleaved ? u.a >> 1 : u.a;
-    const float* t = r.table + ((size_t)pos * (r.rot >> 1) + first) * 2;
-    float cs[16];
+    for (int j = 0; j < 8; ++j) t.c[j] = u.turns && !there ? __builtin_nanf("") : 1.0f, t.s[j] = 0.0f;
+    if (!u.turns || !there) return t;
+    const float* at = r.table + ((size_t)pos * (r.rot >> 1) + (r.interleaved ? u.a >> 1 : u.a)) * 2;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint4 q = gload16(t + 4 * j);
-        cs[4 * j] = __builtin_bit_cast(float, q.x);
-        cs[4 * j + 1] = __builtin_bit_cast(float, q.y);
-        cs[4 * j + 2] = __builtin_bit_cast(float, q.z);
-        cs[4 * j + 3] = __builtin_bit_cast(float, q.w);
+        const uint4 q = gload16(at + 4 * j);
+        t.c[2 * j] = __builtin_bit_cast(float, q.x);
+        t.s[2 * j] = __builtin_bit_cast(float, q.y);
+        t.c[2 * j + 1] = __builtin_bit_cast(float, q.z);
+        t.s[2 * j + 1] = __builtin_bit_cast(float, q.w);
     }
-    if (r.interleaved) {
+    return t;
+}
+// x[0..8) and x[8..16): the two halves of a unit
+__device__ __forceinline__ void turn(const PairUnit& u, bool interleaved, const Turns& t, float* x) {
+    if (!u.turns) return;  // (an infinity times the 0 above would not stay one)
+    if (interleaved) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float p = x[2 * j], q = x[2 * j + 1], c = cs[2 * j], s = cs[2 * j + 1];
-            x[2 * j] = p * c - q * s;
-            x[2 * j + 1] = q * c + p * s;
+            const float p = x[2 * j], q = x[2 * j + 1];
+            x[2 * j] = p * t.c[j] - q * t.s[j];
+            x[2 * j + 1] = q * t.c[j] + p * t.s[j];
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float p = x[j], q = x[8 + j], c = cs[2 * j], s = cs[2 * j + 1];
-            x[j] = p * c - q * s;
-            x[8 + j] = q * c + p * s;
+            const float p = x[j], q = x[8 + j];
+            x[j] = p * t.c[j] - q * t.s[j];
+            x[8 + j] = q * t.c[j] + p * t.s[j];
         }
     }
 }
@@ -128,35 +130,49 @@ __device__ __forceinline__ uint32_t workgroup_max(uint32_t x, uint32_t* lds) {
 // (they stay in registers between the maximum and the codes).  NU units of sixteen codes per thread hold a block.  A unit of V is the
 // sixteen bytes that lie next to each other in the cache (eight tokens x two dims): neighbouring lanes take the four token groups
 // and then the next pair of dims, so a wave writes 1 KiB in one piece and reads 64 bytes of each row.  The workgroups behind the last
-// task turn the queries.
+// task turn the queries, a row per wave.
 template <int NU, int FMT, bool BF16>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvAppendArgs a) {
     __shared__ uint32_t lds_max[4];
     const int tid = threadIdx.x, D = c.dim;
-    if ((int)blockIdx.x >= a.tasks) {  // queries: 256 pair units of one row
-        const int id = blockIdx.x - a.tasks, row = id / a.q_chunks;
-        int seq = 0, upto = 0;
+    if ((int)blockIdx.x >= a.tasks) {  // queries: a wave takes a row, its lanes the units of a few heads at a time, with the same turns
+        const int lane = tid & 63, row = (blockIdx.x - a.tasks) * 4 + (tid >> 6);
+        if (row >= s.n_rows) return;
+        int upto = 0;
         for (int i = 0; i < s.n_seqs; i += kWave) {  // sequences that begin at or before this row
-            const int j = i + (tid & 63);
+            const int j = i + lane;
             upto += __popcll(__ballot(j < s.n_seqs && s.cu[min(j, s.n_seqs)] <= row));
         }
-        seq = upto - 1;
-        if (seq < 0) return;
-        const KvSpan span = kv_span(s, seq);
+        if (upto == 0) return;
+        const KvSpan span = kv_span(s, upto - 1);
         if (row - span.row0 >= span.rows) return;
-        const int unit = (id % a.q_chunks) * 256 + tid, per_head = D >> 4;
-        if (unit >= a.q_heads * per_head) return;
-        const int head = unit / per_head;
-        const PairUnit u = pair_unit(unit - head * per_head, a.rope.rot, a.rope.interleaved);
-        const int pos = a.rope.positions ? a.rope.positions[row] : span.len + row - span.row0;
-        float x[16];
-        load_turned<BF16>(a.q + row * a.q_stride + head * D, u, a.rope, pos, x);
-        uint16_t* out = a.q_out + ((size_t)row * a.q_heads + head) * D;
-        uint4 w;
-        w = make_uint4(pack16<BF16>(x[0], x[1]), pack16<BF16>(x[2], x[3]), pack16<BF16>(x[4], x[5]), pack16<BF16>(x[6], x[7]));
-        *reinterpret_cast<uint4*>(out + u.a) = w;
-        w = make_uint4(pack16<BF16>(x[8], x[9]), pack16<BF16>(x[10], x[11]), pack16<BF16>(x[12], x[13]), pack16<BF16>(x[14], x[15]));
-        *reinterpret_cast<uint4*>(out + u.b) = w;
+        const int per_head = D >> 4, heads = kWave / per_head, first = lane / per_head;
+        if (first >= heads) return;  // (D 192: 60 lanes)
+        const PairUnit u = pair_unit(lane - first * per_head, a.rope.rot, a.rope.interleaved);
+        const Turns t = load_turns(u, a.rope, a.rope.positions ? a.rope.positions[row] : span.len + row - span.row0);
+        const uint16_t* in = a.q + row * a.q_stride;
+        uint16_t* out = a.q_out + (size_t)row * a.q_heads * D;
+        constexpr int kSide = 4;  // heads of a lane on their way
+        for (int h0 = first; h0 < a.q_heads; h0 += kSide * heads) {
+            uint4 raw[kSide][2];
+#pragma unroll
+            for (int k = 0; k < kSide; ++k) {
+                const uint16_t* at = in + min(h0 + k * heads, a.q_heads - 1) * D;
+                raw[k][0] = gload16(at + u.a);
+                raw[k][1] = gload16(at + u.b);
+            }
+#pragma unroll
+            for (int k = 0; k < kSide; ++k) {
+                if (h0 + k * heads >= a.q_heads) break;
+                uint16_t* at = out + (h0 + k * heads) * D;
+                float x[16];
+                unpack8<BF16>(raw[k][0], x);
+                unpack8<BF16>(raw[k][1], x + 8);
+                turn(u, a.rope.interleaved, t, x);
+                *reinterpret_cast<uint4*>(at + u.a) = make_uint4(pack16<BF16>(x[0], x[1]), pack16<BF16>(x[2], x[3]), pack16<BF16>(x[4], x[5]), pack16<BF16>(x[6], x[7]));
+                *reinterpret_cast<uint4*>(at + u.b) = make_uint4(pack16<BF16>(x[8], x[9]), pack16<BF16>(x[10], x[11]), pack16<BF16>(x[12], x[13]), pack16<BF16>(x[14], x[15]));
+            }
+        }
         return;
     }
     const BlockTask t = block_task(s, c, blockIdx.x, a.blocks_per_seq);
@@ -181,7 +197,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
                 const int o = id / per_row, row = row_of_0 + lo + o;
                 const PairUnit u = pair_unit(id - o * per_row, a.rope.rot, a.rope.interleaved);
                 const int pos = a.rope.positions ? a.rope.positions[row] : t.first + lo + o;
-                load_turned<BF16>(a.k + row * a.k_stride + t.head * D, u, a.rope, pos, x[n]);
+                const uint16_t* in = a.k + row * a.k_stride + t.head * D;
+                const uint4 r0 = gload16(in + u.a), r1 = gload16(in + u.b);
+                const Turns turns = load_turns(u, a.rope, pos);
+                unpack8<BF16>(r0, x[n]);
+                unpack8<BF16>(r1, x[n] + 8);
+                turn(u, a.rope.interleaved, turns, x[n]);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) amax = max(amax, __builtin_bit_cast(uint32_t, x[n][j]) & 0x7fffffffu);
             }
@@ -310,18 +331,21 @@ __global__ __launch_bounds__(256) void kv_gather_kernel(KvCache c, KvSeqs s, int
         }
         return;
     }
-    for (int id = tid; id < (c.block * D) >> 4; id += 256) {
-        const int g = id & 3, ap = id >> 2, group = ap / (D >> 1), pair = ap - group * (D >> 1);
+    // a thread takes two neighbouring pairs of dims, so that sixteen lanes write a whole line of a token
+    for (int id = tid; id < (c.block * D) >> 5; id += 256) {
+        const int g = id & 3, ap = id >> 2, group = ap / (D >> 2), quad = ap - group * (D >> 2);
         const int t0 = kKvGroup * group + 4 * g;
         if (t0 + 20 <= lo || t0 >= hi) continue;
-        float x[16];
-        codes_to_f32<FMT>(there ? gload16(codes + id) : make_uint4(0, 0, 0, 0), x);
+        const uint4* at = codes + (group * (D >> 1) + 2 * quad) * 4 + g;
+        float x[16], y[16];
+        codes_to_f32<FMT>(there ? gload16(at) : make_uint4(0, 0, 0, 0), x);
+        codes_to_f32<FMT>(there ? gload16(at + 4) : make_uint4(0, 0, 0, 0), y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int o = t0 + 16 * (j >> 2) + (j & 3);
             if (o >= lo && o < hi)
-                *reinterpret_cast<uint32_t*>(v_out + (row_of_0 + o) * out_stride + t.head * D + 2 * pair) =
-                    there ? pack16<BF16>(x[j] * scale, x[8 + j] * scale) : 0u;
+                *reinterpret_cast<uint2*>(v_out + (row_of_0 + o) * out_stride + t.head * D + 4 * quad) =
+                    there ? make_uint2(pack16<BF16>(x[j] * scale, x[8 + j] * scale), pack16<BF16>(y[j] * scale, y[8 + j] * scale)) : make_uint2(0, 0);
         }
     }
 }
@@ -353,8 +377,7 @@ hipError_t launch_kv_append(const KvCache& c, const KvSeqs& s, const KvAppendArg
     KvAppendArgs a = args;
     a.blocks_per_seq = kv_blocks_per_seq(s.max_rows, c.block);
     a.tasks = s.n_seqs * a.blocks_per_seq * c.heads * 2;
-    a.q_chunks = a.q ? (a.q_heads * (c.dim / 16) + 255) / 256 : 0;
-    const int grid = a.tasks + s.n_rows * a.q_chunks;
+    const int grid = a.tasks + (a.q ? (s.n_rows + 3) / 4 : 0);
     if (format == kKvInt8) return bf16 ? append_nu<kKvInt8, true>(c, s, a, grid, st) : append_nu<kKvInt8, false>(c, s, a, grid, st);
     return bf16 ? append_nu<kKvE4m3, true>(c, s, a, grid, st) : append_nu<kKvE4m3, false>(c, s, a, grid, st);
 }
