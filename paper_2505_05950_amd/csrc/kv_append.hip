@@ -130,13 +130,13 @@ __device__ __forceinline__ uint32_t workgroup_max(uint32_t x, uint32_t* lds) {
 // (they stay in registers between the maximum and the codes).  NU units of sixteen codes per thread hold a block.  A unit of V is the
 // sixteen bytes that lie next to each other in the cache (eight tokens x two dims): neighbouring lanes take the four token groups
 // and then the next pair of dims, so a wave writes 1 KiB in one piece and reads 64 bytes of each row.  The workgroups behind the last
-// task turn the queries, a row per wave.
+// task turn the queries.
 template <int NU, int FMT, bool BF16>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvAppendArgs a) {
     __shared__ uint32_t lds_max[4];
     const int tid = threadIdx.x, D = c.dim;
-    if ((int)blockIdx.x >= a.tasks) {  // queries: a wave takes a row, its lanes the units of a few heads at a time, with the same turns
-        const int lane = tid & 63, row = (blockIdx.x - a.tasks) * 4 + (tid >> 6);
+    if ((int)blockIdx.x >= a.tasks) {  // queries: a wave takes a row (or a part of its heads), its lanes the units of a few heads at a time, with the same turns
+        const int lane = tid & 63, id = (blockIdx.x - a.tasks) * 4 + (tid >> 6), row = id / a.q_split, part = id - row * a.q_split;
         if (row >= s.n_rows) return;
         int upto = 0;
         for (int i = 0; i < s.n_seqs; i += kWave) {  // sequences that begin at or before this row
@@ -153,18 +153,19 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
         const uint16_t* in = a.q + row * a.q_stride;
         uint16_t* out = a.q_out + (size_t)row * a.q_heads * D;
         constexpr int kSide = 4;  // heads of a lane on their way
-        for (int h0 = first; h0 < a.q_heads; h0 += kSide * heads) {
+        const int step = a.q_split * heads;
+        for (int h0 = part * heads + first; h0 < a.q_heads; h0 += kSide * step) {
             uint4 raw[kSide][2];
 #pragma unroll
             for (int k = 0; k < kSide; ++k) {
-                const uint16_t* at = in + min(h0 + k * heads, a.q_heads - 1) * D;
+                const uint16_t* at = in + min(h0 + k * step, a.q_heads - 1) * D;
                 raw[k][0] = gload16(at + u.a);
                 raw[k][1] = gload16(at + u.b);
             }
 #pragma unroll
             for (int k = 0; k < kSide; ++k) {
-                if (h0 + k * heads >= a.q_heads) break;
-                uint16_t* at = out + (h0 + k * heads) * D;
+                if (h0 + k * step >= a.q_heads) break;
+                uint16_t* at = out + (h0 + k * step) * D;
                 float x[16];
                 unpack8<BF16>(raw[k][0], x);
                 unpack8<BF16>(raw[k][1], x + 8);
@@ -240,6 +241,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
         }
         return;
     }
+    uint4 was[NU];
     // V: unit = ((group of 32 tokens) * D / 2 + pair of dims) * 4 + g; token 32 group + 16 tile + 4 g + i is byte 8 (dim % 2) + 4 tile + i
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
@@ -254,6 +256,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
                 x[n][j] = from16<BF16>(w);
                 x[n][8 + j] = from16<BF16>(w >> 16);
             }
+            // the codes beside new tokens, asked for before the scale is known
+            const int t0 = kKvGroup * group + 4 * g;
+            was[n] = make_uint4(0, 0, 0, 0);
+            if (t0 < lo && t0 + 20 > lo) was[n] = gload16(codes + 16 * id);
 #pragma unroll
             for (int j = 0; j < 16; ++j) amax = max(amax, __builtin_bit_cast(uint32_t, x[n][j]) & 0x7fffffffu);
         }
@@ -279,11 +285,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
         uint4* at = reinterpret_cast<uint4*>(codes) + id;
         uint32_t w[4] = {0, 0, 0, 0};
         if (older) {
-            const uint4 was = *at;
-            w[0] = was.x, w[1] = was.y, w[2] = was.z, w[3] = was.w;
+            const uint4 old = t0 + 20 > lo ? was[n] : *at;
+            w[0] = old.x, w[1] = old.y, w[2] = old.z, w[3] = old.w;
             if (b.grows) {  // (codes behind the block's tokens are nobody's)
                 float y[16];
-                codes_to_f32<FMT>(was, y);
+                codes_to_f32<FMT>(old, y);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     w[j] = codes_of<FMT>(y[4 * j] * b.shrink, y[4 * j + 1] * b.shrink, y[4 * j + 2] * b.shrink, y[4 * j + 3] * b.shrink);
@@ -377,7 +383,10 @@ hipError_t launch_kv_append(const KvCache& c, const KvSeqs& s, const KvAppendArg
     KvAppendArgs a = args;
     a.blocks_per_seq = kv_blocks_per_seq(s.max_rows, c.block);
     a.tasks = s.n_seqs * a.blocks_per_seq * c.heads * 2;
-    const int grid = a.tasks + (a.q ? (s.n_rows + 3) / 4 : 0);
+    // a wave per row of queries, or several where rows are few: then the way to the first of them is what there is to save
+    const int passes = a.q ? (a.q_heads + kWave / (c.dim / 16) - 1) / (kWave / (c.dim / 16)) : 1;
+    a.q_split = s.n_rows >= 1024 ? 1 : (1024 / s.n_rows < passes ? 1024 / s.n_rows : passes);
+    const int grid = a.tasks + (a.q ? (int)(((int64_t)s.n_rows * a.q_split + 3) / 4) : 0);
     if (format == kKvInt8) return bf16 ? append_nu<kKvInt8, true>(c, s, a, grid, st) : append_nu<kKvInt8, false>(c, s, a, grid, st);
     return bf16 ? append_nu<kKvE4m3, true>(c, s, a, grid, st) : append_nu<kKvE4m3, false>(c, s, a, grid, st);
 }

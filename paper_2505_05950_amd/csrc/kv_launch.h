@@ -18,7 +18,7 @@ struct KvAppendArgs {
     uint16_t* q_out;
     int q_heads;
     KvRope rope;
-    int blocks_per_seq, tasks;  // set by the launcher
+    int blocks_per_seq, tasks, q_split;  // set by the launcher
 };
 // blocks that `rows` consecutive tokens can touch
 inline int kv_blocks_per_seq(int rows, int block) { return (rows + block - 2) / block + 1; }
