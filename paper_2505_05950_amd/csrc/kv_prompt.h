@@ -7,7 +7,6 @@
 // 32-token tile) are the operand of O^T = V^T P^T when the tokens of V lie in LDS in that order, so the weights stay in registers.
 // Two LDS buffers: a wave converts the next tile's codes while others still multiply, one barrier per tile, and the tile after next is on
 // its way from memory.
-// The exponent's base of a row is moved only when a weight would leave fp16 (2^15): after the first tiles it hardly ever is.
 #pragma once
 
 #include "kv_rows.h"
@@ -17,9 +16,6 @@ namespace floe {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kPromptTokens = 64;             // of a tile: two units of 32, each inside one page
-constexpr float kPromptBits = 7.0f;           // a row's largest weight is 2^7 when its base is set ...
-constexpr float kPromptTop = 15.0f;           // ... and may grow to 2^15 before it is set again
-
 template <int D, int NW>
 struct PromptStage {  // a thread's share of a tile on its way: 16-byte pieces of the codes
     static constexpr int kPieces = (4 * D + 64 * NW - 1) / (64 * NW);
@@ -249,9 +245,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
         float x0, x1;
         swap32(mx, x0, x1);
         mx = fmaxf(x0, x1);
-        const bool move = mx > top + kPromptTop;
+        const bool move = mx > top + kTopBits;
         if (__ballot(move)) {
-            const float new_top = move ? mx - kPromptBits : top;
+            const float new_top = move ? mx - kBaseBits : top;
             const float f = move ? __builtin_amdgcn_exp2f(top - new_top) : 1.0f;
             sum *= f;
 #pragma unroll

@@ -4,8 +4,8 @@
 //   t_rj = scale * log2(e) * (q_r . kcode_j) * kscale_j + log2(vscale_j)      o_r = sum_j 2^t_rj vcode_j / sum_j 2^(t_rj) / vscale_j
 // i.e. the softmax with the scale of V inside the exponent: codes go to the matrix cores as they are (int8 and e4m3 are exact in
 // fp16), no product with a scale is formed per element, and the largest weight that V is multiplied with is a fixed power of two
-// whatever the scales are.  The running maximum M is that of t, lowered by 14 so that the fp16 weights use the type's range (a weight
-// of 2^-38 of the largest still counts).  Queries in bf16 are scaled per row by a power of two into fp16's range.
+// whatever the scales are.  The exponent's base of a row is set so that its largest weight is 2^7, and set again only when a weight would
+// pass 2^15 (after the first tokens it hardly ever is): fp16 holds the weights, down to 2^-31 of the largest.  Queries in bf16 are scaled per row by a power of two into fp16's range.
 //
 // S^T = K Q^T and O^T = V^T P^T, both as v_mfma_f32_16x16x32_f16: a column is a query row, so its maximum and sum live in the four
 // lanes that hold the column, and the rows of S^T that a lane holds (tokens 4 g + i of two tiles) are exactly the operand of the
@@ -22,7 +22,7 @@
 namespace floe {
 
 constexpr int kRowsWaves = 4;
-constexpr float kWeightBits = 14.0f;
+constexpr float kBaseBits = 7.0f, kTopBits = 15.0f;  // a row's largest weight is 2^7 when its base is set, and may grow to 2^15
 
 // Units of one sequence: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on for each.
 struct KvUnits {
@@ -161,7 +161,7 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
                 s[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, Q.q[m][2 * kk + 1], s[m][t], 0, 0, 0);
             }
         }
-    const float lv = __builtin_amdgcn_logf(f.vs), rv = 1.0f / f.vs;
+    const float lv = __builtin_amdgcn_logf(f.vs), rv = __builtin_amdgcn_rcpf(f.vs);
     h16x8 p[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -170,23 +170,24 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(s[m][j >> 2][j & 3], c, lv);
         if (mask) {
+            const bool none = last_key[m] < first_key[m];
+            const int lo = (none ? token0 + 2 * kKvGroup : first_key[m]) - (token0 + 4 * g);  // keys from here on, up to `more` behind, are seen
+            const uint32_t more = none ? 0 : last_key[m] - first_key[m];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int key = token0 + 16 * (j >> 2) + 4 * g + (j & 3);
-                if (key < first_key[m] || key > last_key[m]) x[j] = -__builtin_inff();
-            }
+            for (int j = 0; j < 8; ++j) x[j] = (uint32_t)(16 * (j >> 2) + (j & 3) - lo) > more ? -__builtin_inff() : x[j];
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) mx = fmaxf(mx, x[j]);
-        mx = quad_max(mx) - kWeightBits;
-        const float top = fmaxf(st.top[m], mx), base = top == -__builtin_inff() ? 0.0f : top;
-        if (__ballot(top != st.top[m])) {
-            const float shrink = __builtin_amdgcn_exp2f(st.top[m] - base);
+        mx = quad_max(mx);
+        const bool move = mx > st.top[m] + kTopBits;
+        if (__ballot(move)) {
+            const float top = move ? mx - kBaseBits : st.top[m], shrink = move ? __builtin_amdgcn_exp2f(st.top[m] - top) : 1.0f;
             st.sum[m] *= shrink;
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) st.o[m][d] *= shrink;
             st.top[m] = top;
         }
+        const float base = st.top[m] == -__builtin_inff() ? 0.0f : st.top[m];
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -194,7 +195,8 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
             sum += x[j];
         }
         // (a block whose scale is NaN counts only where something of it is seen)
-        st.sum[m] += sum != 0.0f ? sum * rv : 0.0f;
+        const float add = sum * rv;
+        st.sum[m] += sum != 0.0f ? add : 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const h16x2 p2 = __builtin_convertvector(f32x2{x[2 * j], x[2 * j + 1]}, h16x2);
