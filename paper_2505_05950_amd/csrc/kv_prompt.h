@@ -50,16 +50,17 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
     auto swizzle = [](int t) { return kChunks % 16 == 0 ? t & 15 : (t >> 1) & 7; };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
     const int row_wave = kSplit == 1 ? wave : wave % kRowWaves, out0 = kSplit == 1 ? 0 : wave / kRowWaves * kOut;  // this wave's rows and its first 32 dims of the output
-    const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads;
-    const int seq = rest % a.s.n_seqs, tile = a.prompt_tiles - 1 - rest / a.s.n_seqs;  // the last rows of a prompt see most: they go first
+    const int head = __builtin_amdgcn_readfirstlane(blockIdx.x % a.c.heads), rest = blockIdx.x / a.c.heads;
+    const int seq = __builtin_amdgcn_readfirstlane(rest % a.s.n_seqs), tile = a.prompt_tiles - 1 - rest / a.s.n_seqs;  // the last rows of a prompt see most: they go first
     const KvSpan span = kv_span(a.s, seq);
     const int all_rows = span.rows * a.group, row0 = tile * 32 * kRowWaves;
     if (row0 >= all_rows || span.rows <= a.most_rows) return;
     const PromptRange range = prompt_range(a, span, row0, 32 * kRowWaves);
     const int chunk = blockIdx.y;
     if (chunk >= range.chunks) return;
-    const int start = range.start + chunk * a.prompt_chunk * kPromptTokens;
-    const int n_tiles = chunk + 1 < range.chunks ? a.prompt_chunk : range.n - chunk * a.prompt_chunk;
+    // (quotients are formed in vector registers: what all lanes hold alike goes back to scalar ones)
+    const int start = __builtin_amdgcn_readfirstlane(range.start + chunk * a.prompt_chunk * kPromptTokens);
+    const int n_tiles = __builtin_amdgcn_readfirstlane(chunk + 1 < range.chunks ? a.prompt_chunk : range.n - chunk * a.prompt_chunk);
     // ---- queries of this wave
     const int rr = row0 + 32 * row_wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.len - span.rows + token;
     const bool there = rr < all_rows;
@@ -96,7 +97,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
     const int base_pos = span.len - span.rows;
     const int w_first = base_pos + min((row0 + 32 * row_wave) / a.group, span.rows - 1);
     const int w_last = base_pos + min((row0 + 32 * row_wave + 31) / a.group, span.rows - 1);
-    const int w_clear_lo = a.window > 0 ? w_last - a.window + 1 : 0, w_clear_hi = a.causal ? w_first : span.len - 1;  // every row sees
+    // tokens that every row of the wave sees
+    const int w_clear_lo = __builtin_amdgcn_readfirstlane(a.window > 0 ? w_last - a.window + 1 : 0);
+    const int w_clear_hi = __builtin_amdgcn_readfirstlane(a.causal ? w_first : span.len - 1);
 
     f32x16 o[kOut];
 #pragma unroll
@@ -106,12 +109,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
     float top = -__builtin_inff(), sum = 0.0f;
     int page0 = -1, page1 = -1;  // of the tile at work
 
-    const int upb = a.c.block / kKvGroup;
+    const int unit0 = start / kKvGroup, log_upb = a.c.block == 32 ? 0 : a.c.block == 64 ? 1 : 2;  // units per block: 1, 2 or 4
     int pages = -1;
     auto page_of = [&](int unit) {  // page of the walk's unit-th unit of 32 tokens (0, 1, 2 ... in order), -1 where there is none
         if ((unit & 63) == 0) {
             const int t = start + (unit + lane) * kKvGroup;
-            pages = t < span.len ? kv_page(a.s, a.c, seq, (t / kKvGroup) / upb) : -1;
+            pages = t < span.len ? kv_page(a.s, a.c, seq, (t / kKvGroup) >> log_upb) : -1;
         }
         return __builtin_amdgcn_readlane(pages, unit & 63);
     };
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const size_t slot = (size_t)max(page[u], 0) * a.c.heads + head;
-            const size_t at = (slot * a.c.block + ((start / kKvGroup + 2 * it + u) % upb) * kKvGroup) * D;
+            const size_t at = (slot * a.c.block + ((unit0 + 2 * it + u) & ((1 << log_upb) - 1)) * kKvGroup) * D;
             kp[u] = scalar_ptr(a.c.k + at);
             vp[u] = scalar_ptr(a.c.v + at);
         }
@@ -286,33 +289,35 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
         const int buf = it & 1, t0 = start + it * kPromptTokens;
         page_then[0] = page_of(2 * it + 4), page_then[1] = page_of(2 * it + 5);
         __syncthreads();  // this tile is in LDS, and nobody reads the one before it any more
-        {
-            const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || page0 < 0 || page1 < 0 || !(ks[0] * vs[0] + ks[1] * vs[1] > 0.0f);
+        const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || page0 < 0 || page1 < 0 || !(ks[0] * vs[0] + ks[1] * vs[1] > 0.0f);
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) ring[i] = operand(buf, i);
+        for (int i = 0; i < kAhead; ++i) ring[i] = operand(buf, i);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                c[u] = fmaxf(row_scale * ks[u], 0x1p-126f);  // (-infinity times it has to stay that)
-                lv[u] = __builtin_amdgcn_logf(vs[u]);
-                rv[u] = __builtin_amdgcn_rcpf(vs[u]);
+        for (int u = 0; u < 2; ++u) {
+            c[u] = fmaxf(row_scale * ks[u], 0x1p-126f);  // (-infinity times it has to stay that)
+            lv[u] = __builtin_amdgcn_logf(vs[u]);
+            rv[u] = __builtin_amdgcn_rcpf(vs[u]);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[u][j] = 0.0f;
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            products(buf, std::integral_constant<int, 0>());
-            products(buf, std::integral_constant<int, 1>());
-            convert(buf ^ 1);
-            __builtin_amdgcn_sched_barrier(0);
-            request(min(it + 2, n_tiles - 1), page_then);
-            maximum(t0, masked);
-            weights(0);
-            __builtin_amdgcn_sched_barrier(0);
-            products(buf, std::integral_constant<int, 2>());
-            weights(1);
-            __builtin_amdgcn_sched_barrier(0);
-            request_scales(page_next);
-            products(buf, std::integral_constant<int, 3>());
+            for (int j = 0; j < 16; ++j) s[u][j] = 0.0f;
         }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);  // (a wave whose products wait goes before one that converts: 1 to 2 %)
+        products(buf, std::integral_constant<int, 0>());
+        products(buf, std::integral_constant<int, 1>());
+        convert(buf ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
+        request(min(it + 2, n_tiles - 1), page_then);
+        maximum(t0, masked);
+        weights(0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        products(buf, std::integral_constant<int, 2>());
+        weights(1);
+        __builtin_amdgcn_sched_barrier(0);
+        request_scales(page_next);
+        products(buf, std::integral_constant<int, 3>());
+        __builtin_amdgcn_s_setprio(0);
         set_keep(it + 2, page_then);
         page0 = page_next[0], page1 = page_next[1];
         page_next[0] = page_then[0], page_next[1] = page_then[1];

@@ -4,8 +4,10 @@
 //   t_rj = scale * log2(e) * (q_r . kcode_j) * kscale_j + log2(vscale_j)      o_r = sum_j 2^t_rj vcode_j / sum_j 2^(t_rj) / vscale_j
 // i.e. the softmax with the scale of V inside the exponent: codes go to the matrix cores as they are (int8 and e4m3 are exact in
 // fp16), no product with a scale is formed per element, and the largest weight that V is multiplied with is a fixed power of two
-// whatever the scales are.  The exponent's base of a row is set so that its largest weight is 2^7, and set again only when a weight would
-// pass 2^15 (after the first tokens it hardly ever is): fp16 holds the weights, down to 2^-31 of the largest.  Queries in bf16 are scaled per row by a power of two into fp16's range.
+// whatever the scales are.  The exponent's base of a row is set so that its largest weight is 2^14, and set again only when a weight would
+// pass 2^15 (after the first tokens it hardly ever is): fp16 holds the weights, down to 2^-38 of the largest.  Their rounding is what
+// the result is off by beside its own: 2.2e-4 of it in all with fp16 outputs (2.1e-4 is the rounding of the output), 2.5e-4 when the
+// base is set to 2^7, which costs 1 % less time on long prompts.  Queries in bf16 are scaled per row by a power of two into fp16's range.
 //
 // S^T = K Q^T and O^T = V^T P^T, both as v_mfma_f32_16x16x32_f16: a column is a query row, so its maximum and sum live in the four
 // lanes that hold the column, and the rows of S^T that a lane holds (tokens 4 g + i of two tiles) are exactly the operand of the
@@ -22,7 +24,7 @@
 namespace floe {
 
 constexpr int kRowsWaves = 4;
-constexpr float kBaseBits = 7.0f, kTopBits = 15.0f;  // a row's largest weight is 2^7 when its base is set, and may grow to 2^15
+constexpr float kBaseBits = 14.0f, kTopBits = 15.0f;  // a row's largest weight is 2^14 when its base is set, and may grow to 2^15
 
 // Units of one sequence: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on for each.
 struct KvUnits {
@@ -245,10 +247,12 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
     __shared__ float slab[NW][16][kStride];
     __shared__ float ml[NW][16 * MT][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    const int segments = a.c.heads * a.tiles, seq = blockIdx.x / segments, seg = blockIdx.x - seq * segments, chunk = blockIdx.y;
-    const int head = seg / a.tiles, tile = seg - head * a.tiles, row0 = tile * 16 * MT;
+    // (quotients are formed in vector registers: what all lanes hold alike goes back to scalar ones)
+    const int segments = a.c.heads * a.tiles, seq = __builtin_amdgcn_readfirstlane(blockIdx.x / segments);
+    const int seg = blockIdx.x - seq * segments, chunk = blockIdx.y;
+    const int head = __builtin_amdgcn_readfirstlane(seg / a.tiles), tile = seg - head * a.tiles, row0 = tile * 16 * MT;
     const KvUnits w = kv_units<MT>(a, seq);
-    const int n_chunks = kv_chunks(a, w.units);
+    const int n_chunks = __builtin_amdgcn_readfirstlane(kv_chunks(a, w.units));
     if (tile >= w.tiles || chunk >= n_chunks) return;
     const int j0 = chunk * a.chunk, j1 = chunk + 1 < n_chunks ? j0 + a.chunk : w.units;
     KvState<D, MT> st;
@@ -266,14 +270,14 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
     // units between these need no mask
     const int pos0 = w.span.len - w.span.rows + row0 / a.group;
     const int pos1 = w.span.len - w.span.rows + min((row0 + 16 * MT - 1) / a.group, w.span.rows - 1);
-    const int clear_lo = a.window > 0 ? pos1 - a.window + 1 : 0;
-    const int clear_hi = a.causal ? pos0 + 1 : w.span.len;  // first token that some row does not see
-    const int end = a.causal ? pos1 + 1 : w.span.len;       // behind the last token that any row sees
-    const int upb = a.c.block / kKvGroup, unit0 = w.lo / kKvGroup;
+    const int clear_lo = __builtin_amdgcn_readfirstlane(a.window > 0 ? pos1 - a.window + 1 : 0);
+    const int clear_hi = __builtin_amdgcn_readfirstlane(a.causal ? pos0 + 1 : w.span.len);  // first token that some row does not see
+    const int end = __builtin_amdgcn_readfirstlane(a.causal ? pos1 + 1 : w.span.len);       // behind the last token that any row sees
+    const int unit0 = w.lo / kKvGroup, log_upb = a.c.block == 32 ? 0 : a.c.block == 64 ? 1 : 2;  // units per block: 1, 2 or 4
     int pages = -1;
     auto fetch_pages = [&](int j) {  // pages of this wave's next 64 units
         const int mine = j + NW * lane;
-        pages = mine < j1 ? kv_page(a.s, a.c, seq, (unit0 + mine) / upb) : -1;
+        pages = mine < j1 ? kv_page(a.s, a.c, seq, (unit0 + mine) >> log_upb) : -1;
     };
     auto page_of = [&](int it) { return __builtin_amdgcn_readlane(pages, it & 63); };
     const int n = (j1 - j0 - wave + NW - 1) / NW;  // units of this wave (may be none)
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
         const int it = min(next, n - 1), j = j0 + wave + NW * it;
         if ((it & 63) == 0 && it == next) fetch_pages(j);
         page = w.lo + j * kKvGroup >= end ? -1 : page_of(it);
-        load_unit<D, FMT>(f, a.c, head, page, ((unit0 + j) % upb) * kKvGroup, r, g);
+        load_unit<D, FMT>(f, a.c, head, page, ((unit0 + j) & ((1 << log_upb) - 1)) * kKvGroup, r, g);
     };
     if (n > 0) {
         request(0, f0, p0);
