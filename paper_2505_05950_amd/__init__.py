@@ -1,5 +1,6 @@
 """MI355X-native FloE decode path: compressed sparse expert FFN (quantized up GEMV, threshold
-selection, gathered gate/down GEMVs, top-k combine) behind a C ABI (include/floe.h).
+selection, gathered gate/down GEMVs, top-k combine) behind a C ABI (include/floe.h), and in front of it attention over a
+paged cache in 8 bits.
 
 `paper_2505_05950_amd.binding` marshals torch tensors into that ABI; every step runs in the HIP
 library.  There is no host fallback: loading fails loudly when the library has not been built.
