@@ -77,13 +77,20 @@ void cut_segments(AttnPlan& w, int64_t segments, int64_t units) {
     w.chunk = (int)((units + chunks - 1) / chunks);
     w.chunks = (int)chunks;
 }
-// Tiles of rows that do not fill the card are cut into chunks of their tokens, of at least four tiles of 64.
-void cut_prompts(AttnPlan& w, int64_t segments, int64_t tiles) {
-    int64_t chunks = num_cus() / segments;
-    if (chunks > tiles / 4) chunks = tiles / 4;
-    if (chunks < 1) chunks = 1;
+// Chunks of the prompt kernel's tiles of rows: what costs least in tiles of 64 tokens (about 2.4 us each at 128 dims), the last round's
+// compute units standing idle among it, two tiles' worth for every round's start, and the partial results' way to memory and back.
+void cut_prompts(AttnPlan& w, int dim, int64_t segments, int64_t tiles) {
+    const int64_t slots = (int64_t)num_cus() * (dim == 64 ? 2 : 1);  // workgroups at a time
+    const double part = kv_prompt_rows(dim) * 8.0 * 128 / 5.0e6 / 2.4;
+    double best = 0;
+    int64_t chunks = 1;
+    for (int64_t c = 1; c <= 32 && c <= tiles && (c == 1 || segments * c <= 8 * slots); ++c) {
+        const int64_t rounds = (segments * c + slots - 1) / slots;
+        const double cost = rounds * ((tiles + c - 1) / c + 2.0) + (c > 1 ? 2.0 + segments * c * part : 0.0);
+        if (c == 1 || cost < best) best = cost, chunks = c;
+    }
     w.prompt_chunk = (int)((tiles + chunks - 1) / chunks);
-    w.prompt_chunks = (int)chunks;
+    w.prompt_chunks = (int)((tiles + w.prompt_chunk - 1) / w.prompt_chunk);
 }
 AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
     AttnPlan w{};
@@ -93,9 +100,12 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
     w.rows = true;
     w.most_rows = w.row_limit = k.max_rows;
     if (k.max_rows > most) {
-        // where no sequence can have few rows (n_rows are too many for that) the rows kernel has nothing to look for
+        // Sequences with few rows are the rows kernel's, unless there can be none (n_rows are too many for that) or the prompt kernel has
+        // room for their tiles beside the others': then a launch costs more than it saves.
+        const int64_t tile_rows = kv_prompt_rows(c->head_dim);
+        const int64_t tiles = k.n_seqs * ((k.max_rows * (int64_t)group + tile_rows - 1) / tile_rows) * c->kv_heads;
         w.prompt = true;
-        w.rows = most > 0 && k.n_rows - (int64_t)(k.n_seqs - 1) * k.max_rows <= most;
+        w.rows = most > 0 && k.n_rows - (int64_t)(k.n_seqs - 1) * k.max_rows <= most && tiles > num_cus();
         w.most_rows = w.rows ? most : 0;
         w.row_limit = most;
     }
@@ -105,7 +115,7 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
         w.prompt_tiles = (int)(((int64_t)k.max_rows * group + tile_rows - 1) / tile_rows);
         const int64_t keys = a->window > 0 && a->window + tile_rows < max_keys ? a->window + tile_rows : max_keys;
         const int64_t segments = (int64_t)k.n_seqs * c->kv_heads * w.prompt_tiles;
-        cut_prompts(w, segments, (keys + 63) / 64 + 1);
+        cut_prompts(w, c->head_dim, segments, (keys + 63) / 64 + 1);
         if ((int64_t)a->q_heads * k.max_rows > kMaxGrid) w.prompt_chunks = 1;  // (more rows than a join has workgroups)
         if (w.prompt_chunks > 1) {
             const size_t parts = (size_t)segments * w.prompt_chunks * tile_rows;

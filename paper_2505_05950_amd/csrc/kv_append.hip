@@ -116,6 +116,19 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits, bool opens
     }
     return r;
 }
+// the first `n` pieces of sixteen codes of a block, all of older tokens
+template <int FMT>
+__device__ __forceinline__ void recode(uint8_t* codes, int n, float shrink) {
+    for (int id = threadIdx.x; id < n; id += 256) {
+        uint4* at = reinterpret_cast<uint4*>(codes) + id;
+        float y[16];
+        codes_to_f32<FMT>(*at, y);
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = codes_of<FMT>(y[4 * j] * shrink, y[4 * j + 1] * shrink, y[4 * j + 2] * shrink, y[4 * j + 3] * shrink);
+        *at = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
 __device__ __forceinline__ uint32_t workgroup_max(uint32_t x, uint32_t* lds) {
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o, kWave));
@@ -127,7 +140,7 @@ __device__ __forceinline__ uint32_t workgroup_max(uint32_t x, uint32_t* lds) {
 }  // namespace
 
 // A workgroup owns one block x head of K or of V, so nobody else touches its codes and its scale: no atomics, one pass over the rows
-// (they stay in registers between the maximum and the codes).  NU units of sixteen codes per thread hold a block.  A unit of V is the
+// (they stay in registers between the maximum and the codes).  NU units of sixteen codes per thread hold what a call can bring to a block.  A unit of V is the
 // sixteen bytes that lie next to each other in the cache (eight tokens x two dims): neighbouring lanes take the four token groups
 // and then the next pair of dims, so a wave writes 1 KiB in one piece and reads 64 bytes of each row.  The workgroups behind the last
 // task turn the queries.
@@ -186,7 +199,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
     float* scale_at = (t.is_v ? c.v_scale : c.k_scale) + slot;
     const float old_scale = opens ? 1.0f : *scale_at;
     uint8_t* codes = (t.is_v ? c.v : c.k) + slot * c.block * D;
-    const int units = (c.block * D) >> 4;
     float x[NU][16];
     uint32_t amax = 0;
     if (!t.is_v) {
@@ -227,26 +239,40 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
                 *reinterpret_cast<uint2*>(at + u.b) = make_uint2(w[2], w[3]);
             }
         }
+        if (b.grows) recode<FMT>(codes, lo * per_row, b.shrink);
+        return;
+    }
+    if (hi - lo == 1) {  // one token: a thread takes a pair of dims and writes its two bytes, the codes beside them stay unread
+        const int pair = tid;  // (dim is at most 256)
+        float y[2] = {0.0f, 0.0f};
+        if (2 * pair < D) {
+            const uint32_t w = gload4(a.v + (row_of_0 + lo) * a.v_stride + t.head * D + 2 * pair);
+            y[0] = from16<BF16>(w);
+            y[1] = from16<BF16>(w >> 16);
+            amax = max(__builtin_bit_cast(uint32_t, y[0]) & 0x7fffffffu, __builtin_bit_cast(uint32_t, y[1]) & 0x7fffffffu);
+        }
+        const BlockScale b = block_scale(workgroup_max(amax, lds_max), opens, old_scale, qmax);
+        if (tid == 0) *scale_at = b.scale;
         if (b.grows) {
-            for (int id = tid; id < lo * per_row; id += 256) {
-                uint4* at = reinterpret_cast<uint4*>(codes) + id;
-                float y[16];
-                codes_to_f32<FMT>(*at, y);
-                uint32_t w[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    w[j] = codes_of<FMT>(y[4 * j] * b.shrink, y[4 * j + 1] * b.shrink, y[4 * j + 2] * b.shrink, y[4 * j + 3] * b.shrink);
-                *at = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            recode<FMT>(codes, (lo / kKvGroup + 1) * 2 * D, b.shrink);
+            __syncthreads();  // the new bytes come behind those of their pieces
+        }
+        if (2 * pair < D) {
+            const int token = lo % kKvGroup;
+            uint8_t* at = codes + ((lo / kKvGroup * (D >> 1) + pair) * 4 + ((token >> 2) & 3)) * 16 + (token >> 4) * 4 + (token & 3);
+            const uint32_t w = b.finite ? codes_of<FMT>(y[0] / b.scale, y[1] / b.scale, 0.0f, 0.0f) : 0u;
+            at[0] = (uint8_t)w;
+            at[8] = (uint8_t)(w >> 8);
         }
         return;
     }
     uint4 was[NU];
+    const int unit0 = lo / kKvGroup * 2 * D, unit1 = ((hi - 1) / kKvGroup + 1) * 2 * D;  // units of the groups that get tokens
     // V: unit = ((group of 32 tokens) * D / 2 + pair of dims) * 4 + g; token 32 group + 16 tile + 4 g + i is byte 8 (dim % 2) + 4 tile + i
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
-        const int id = tid + n * 256;
-        if (id < units) {
+        const int id = unit0 + tid + n * 256;
+        if (id < unit1) {
             const int g = id & 3, ap = id >> 2, group = ap / (D >> 1), pair = ap - group * (D >> 1);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -268,8 +294,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
     if (tid == 0) *scale_at = b.scale;
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
-        const int id = tid + n * 256;
-        if (id >= units) continue;
+        const int id = unit0 + tid + n * 256;
+        if (id >= unit1) continue;
         const int g = id & 3, group = (id >> 2) / (D >> 1);
         const int t0 = kKvGroup * group + 4 * g;  // its tokens: t0 .. t0 + 4 and t0 + 16 .. t0 + 20
         uint32_t fresh[2] = {0, 0};  // bytes of new tokens
@@ -306,6 +332,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
         }
         *at = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    if (b.grows) recode<FMT>(codes, unit0, b.shrink);
 }
 
 // value = code * scale, rounded once to 16 bits; the same split and the same units as above.  Rows of absent pages are zero.
@@ -370,7 +397,10 @@ __global__ __launch_bounds__(256) void rope_table_kernel(float2* __restrict__ ta
 namespace {
 template <int FMT, bool BF16>
 hipError_t append_nu(const KvCache& c, const KvSeqs& s, const KvAppendArgs& a, int grid, hipStream_t st) {
-    const int per_thread = (c.block * c.dim + 4095) / 4096;
+    // pieces of sixteen codes per thread: of the 32-token groups of a block that max_rows rows can touch (the registers of a whole block
+    // would let a compute unit hold two workgroups)
+    const int groups = (s.max_rows + 2 * kKvGroup - 2) / kKvGroup, all = c.block / kKvGroup;
+    const int per_thread = s.max_rows == 1 ? 1 : ((groups < all ? groups : all) * 2 * c.dim + 255) / 256;
     if (per_thread <= 1) kv_append_kernel<1, FMT, BF16><<<dim3(grid), dim3(256), 0, st>>>(c, s, a);
     else if (per_thread <= 2) kv_append_kernel<2, FMT, BF16><<<dim3(grid), dim3(256), 0, st>>>(c, s, a);
     else if (per_thread <= 4) kv_append_kernel<4, FMT, BF16><<<dim3(grid), dim3(256), 0, st>>>(c, s, a);
