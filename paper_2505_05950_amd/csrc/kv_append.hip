@@ -116,10 +116,10 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t amax_bits, bool opens
     }
     return r;
 }
-// the first `n` pieces of sixteen codes of a block, all of older tokens
+// the first `n` pieces of sixteen codes of a block
 template <int FMT>
-__device__ __forceinline__ void recode(uint8_t* codes, int n, float shrink) {
-    for (int id = threadIdx.x; id < n; id += 256) {
+__device__ __forceinline__ void recode(uint8_t* codes, int n, float shrink, int first, int step) {
+    for (int id = first; id < n; id += step) {
         uint4* at = reinterpret_cast<uint4*>(codes) + id;
         float y[16];
         codes_to_f32<FMT>(*at, y);
@@ -129,12 +129,59 @@ __device__ __forceinline__ void recode(uint8_t* codes, int n, float shrink) {
         *at = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
-__device__ __forceinline__ uint32_t workgroup_max(uint32_t x, uint32_t* lds) {
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o, kWave));
+    return x;
+}
+__device__ __forceinline__ uint32_t workgroup_max(uint32_t x, uint32_t* lds) {
+    x = wave_max(x);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     return max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+}
+
+// The queries: a wave takes a row (or a part of its heads), its lanes the units of a few heads at a time, with the same turns.
+template <bool BF16>
+__device__ __forceinline__ void turn_queries(const KvCache& c, const KvSeqs& s, const KvAppendArgs& a, int id) {
+    const int lane = threadIdx.x & 63, D = c.dim, row = id / a.q_split, part = id - row * a.q_split;
+    if (row >= s.n_rows) return;
+    int upto = 0;
+    for (int i = 0; i < s.n_seqs; i += kWave) {  // sequences that begin at or before this row
+        const int j = i + lane;
+        upto += __popcll(__ballot(j < s.n_seqs && s.cu[min(j, s.n_seqs)] <= row));
+    }
+    if (upto == 0) return;
+    const KvSpan span = kv_span(s, upto - 1);
+    if (row - span.row0 >= span.rows) return;
+    const int per_head = D >> 4, heads = kWave / per_head, first = lane / per_head;
+    if (first >= heads) return;  // (D 192: 60 lanes)
+    const PairUnit u = pair_unit(lane - first * per_head, a.rope.rot, a.rope.interleaved);
+    const Turns t = load_turns(u, a.rope, a.rope.positions ? a.rope.positions[row] : span.len + row - span.row0);
+    const uint16_t* in = a.q + row * a.q_stride;
+    uint16_t* out = a.q_out + (size_t)row * a.q_heads * D;
+    constexpr int kSide = 4;  // heads of a lane on their way
+    const int step = a.q_split * heads;
+    for (int h0 = part * heads + first; h0 < a.q_heads; h0 += kSide * step) {
+        uint4 raw[kSide][2];
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) {
+            const uint16_t* at = in + min(h0 + k * step, a.q_heads - 1) * D;
+            raw[k][0] = gload16(at + u.a);
+            raw[k][1] = gload16(at + u.b);
+        }
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) {
+            if (h0 + k * step >= a.q_heads) break;
+            uint16_t* at = out + (h0 + k * step) * D;
+            float x[16];
+            unpack8<BF16>(raw[k][0], x);
+            unpack8<BF16>(raw[k][1], x + 8);
+            turn(u, a.rope.interleaved, t, x);
+            *reinterpret_cast<uint4*>(at + u.a) = make_uint4(pack16<BF16>(x[0], x[1]), pack16<BF16>(x[2], x[3]), pack16<BF16>(x[4], x[5]), pack16<BF16>(x[6], x[7]));
+            *reinterpret_cast<uint4*>(at + u.b) = make_uint4(pack16<BF16>(x[8], x[9]), pack16<BF16>(x[10], x[11]), pack16<BF16>(x[12], x[13]), pack16<BF16>(x[14], x[15]));
+        }
+    }
 }
 
 }  // namespace
@@ -148,47 +195,7 @@ template <int NU, int FMT, bool BF16>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvAppendArgs a) {
     __shared__ uint32_t lds_max[4];
     const int tid = threadIdx.x, D = c.dim;
-    if ((int)blockIdx.x >= a.tasks) {  // queries: a wave takes a row (or a part of its heads), its lanes the units of a few heads at a time, with the same turns
-        const int lane = tid & 63, id = (blockIdx.x - a.tasks) * 4 + (tid >> 6), row = id / a.q_split, part = id - row * a.q_split;
-        if (row >= s.n_rows) return;
-        int upto = 0;
-        for (int i = 0; i < s.n_seqs; i += kWave) {  // sequences that begin at or before this row
-            const int j = i + lane;
-            upto += __popcll(__ballot(j < s.n_seqs && s.cu[min(j, s.n_seqs)] <= row));
-        }
-        if (upto == 0) return;
-        const KvSpan span = kv_span(s, upto - 1);
-        if (row - span.row0 >= span.rows) return;
-        const int per_head = D >> 4, heads = kWave / per_head, first = lane / per_head;
-        if (first >= heads) return;  // (D 192: 60 lanes)
-        const PairUnit u = pair_unit(lane - first * per_head, a.rope.rot, a.rope.interleaved);
-        const Turns t = load_turns(u, a.rope, a.rope.positions ? a.rope.positions[row] : span.len + row - span.row0);
-        const uint16_t* in = a.q + row * a.q_stride;
-        uint16_t* out = a.q_out + (size_t)row * a.q_heads * D;
-        constexpr int kSide = 4;  // heads of a lane on their way
-        const int step = a.q_split * heads;
-        for (int h0 = part * heads + first; h0 < a.q_heads; h0 += kSide * step) {
-            uint4 raw[kSide][2];
-#pragma unroll
-            for (int k = 0; k < kSide; ++k) {
-                const uint16_t* at = in + min(h0 + k * step, a.q_heads - 1) * D;
-                raw[k][0] = gload16(at + u.a);
-                raw[k][1] = gload16(at + u.b);
-            }
-#pragma unroll
-            for (int k = 0; k < kSide; ++k) {
-                if (h0 + k * step >= a.q_heads) break;
-                uint16_t* at = out + (h0 + k * step) * D;
-                float x[16];
-                unpack8<BF16>(raw[k][0], x);
-                unpack8<BF16>(raw[k][1], x + 8);
-                turn(u, a.rope.interleaved, t, x);
-                *reinterpret_cast<uint4*>(at + u.a) = make_uint4(pack16<BF16>(x[0], x[1]), pack16<BF16>(x[2], x[3]), pack16<BF16>(x[4], x[5]), pack16<BF16>(x[6], x[7]));
-                *reinterpret_cast<uint4*>(at + u.b) = make_uint4(pack16<BF16>(x[8], x[9]), pack16<BF16>(x[10], x[11]), pack16<BF16>(x[12], x[13]), pack16<BF16>(x[14], x[15]));
-            }
-        }
-        return;
-    }
+    if ((int)blockIdx.x >= a.tasks) return turn_queries<BF16>(c, s, a, (blockIdx.x - a.tasks) * 4 + (tid >> 6));
     const BlockTask t = block_task(s, c, blockIdx.x, a.blocks_per_seq);
     if (t.page < 0) return;  // the whole workgroup
     const size_t slot = (size_t)t.page * c.heads + t.head;
@@ -239,31 +246,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
                 *reinterpret_cast<uint2*>(at + u.b) = make_uint2(w[2], w[3]);
             }
         }
-        if (b.grows) recode<FMT>(codes, lo * per_row, b.shrink);
-        return;
-    }
-    if (hi - lo == 1) {  // one token: a thread takes a pair of dims and writes its two bytes, the codes beside them stay unread
-        const int pair = tid;  // (dim is at most 256)
-        float y[2] = {0.0f, 0.0f};
-        if (2 * pair < D) {
-            const uint32_t w = gload4(a.v + (row_of_0 + lo) * a.v_stride + t.head * D + 2 * pair);
-            y[0] = from16<BF16>(w);
-            y[1] = from16<BF16>(w >> 16);
-            amax = max(__builtin_bit_cast(uint32_t, y[0]) & 0x7fffffffu, __builtin_bit_cast(uint32_t, y[1]) & 0x7fffffffu);
-        }
-        const BlockScale b = block_scale(workgroup_max(amax, lds_max), opens, old_scale, qmax);
-        if (tid == 0) *scale_at = b.scale;
-        if (b.grows) {
-            recode<FMT>(codes, (lo / kKvGroup + 1) * 2 * D, b.shrink);
-            __syncthreads();  // the new bytes come behind those of their pieces
-        }
-        if (2 * pair < D) {
-            const int token = lo % kKvGroup;
-            uint8_t* at = codes + ((lo / kKvGroup * (D >> 1) + pair) * 4 + ((token >> 2) & 3)) * 16 + (token >> 4) * 4 + (token & 3);
-            const uint32_t w = b.finite ? codes_of<FMT>(y[0] / b.scale, y[1] / b.scale, 0.0f, 0.0f) : 0u;
-            at[0] = (uint8_t)w;
-            at[8] = (uint8_t)(w >> 8);
-        }
+        if (b.grows) recode<FMT>(codes, lo * per_row, b.shrink, tid, 256);
         return;
     }
     uint4 was[NU];
@@ -332,7 +315,81 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
         }
         *at = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    if (b.grows) recode<FMT>(codes, unit0, b.shrink);
+    if (b.grows) recode<FMT>(codes, unit0, b.shrink, tid, 256);
+}
+
+// One token per sequence: a wave owns the block x head.  The block's maximum is a wave's, V's token is two bytes per pair of dims, and
+// what lies beside them is read only where the scale grows.
+template <int FMT, bool BF16>
+__global__ __launch_bounds__(256) void kv_append_one_kernel(KvCache c, KvSeqs s, KvAppendArgs a) {
+    const int lane = threadIdx.x & 63, D = c.dim, id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (id >= a.tasks) {
+        if (a.q) turn_queries<BF16>(c, s, a, id - a.tasks);
+        return;
+    }
+    const BlockTask t = block_task(s, c, id, 1);
+    if (t.page < 0) return;
+    const size_t slot = (size_t)t.page * c.heads + t.head;
+    const int o = t.lo - t.first, row = t.span.row0;
+    const bool opens = o == 0;
+    const float qmax = FMT == kKvInt8 ? 127.0f : 448.0f;
+    float* scale_at = (t.is_v ? c.v_scale : c.k_scale) + slot;
+    const float old_scale = opens ? 1.0f : *scale_at;
+    uint8_t* codes = (t.is_v ? c.v : c.k) + slot * c.block * D;
+    if (!t.is_v) {
+        const int per_row = D >> 4;
+        const PairUnit u = pair_unit(min(lane, per_row - 1), a.rope.rot, a.rope.interleaved);  // lanes behind the row double its last unit
+        const uint16_t* in = a.k + row * a.k_stride + t.head * D;
+        const uint4 r0 = gload16(in + u.a), r1 = gload16(in + u.b);
+        const Turns turns = load_turns(u, a.rope, a.rope.positions ? a.rope.positions[row] : t.lo);
+        float x[16];
+        unpack8<BF16>(r0, x);
+        unpack8<BF16>(r1, x + 8);
+        turn(u, a.rope.interleaved, turns, x);
+        uint32_t amax = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) amax = max(amax, __builtin_bit_cast(uint32_t, x[j]) & 0x7fffffffu);
+        const BlockScale b = block_scale(wave_max(amax), opens, old_scale, qmax);
+        if (lane == 0) *scale_at = b.scale;
+        if (b.grows) recode<FMT>(codes, o * per_row, b.shrink, lane, kWave);
+        if (lane >= per_row) return;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (b.finite) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = codes_of<FMT>(x[4 * j] / b.scale, x[4 * j + 1] / b.scale, x[4 * j + 2] / b.scale, x[4 * j + 3] / b.scale);
+        }
+        uint8_t* at = codes + (size_t)o * D;
+        *reinterpret_cast<uint2*>(at + u.a) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(at + u.b) = make_uint2(w[2], w[3]);
+        return;
+    }
+    constexpr int kPairs = 2;  // of dims per lane: head dims go up to 256
+    float y[kPairs][2];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int n = 0; n < kPairs; ++n) {
+        const int pair = min(lane + n * kWave, (D >> 1) - 1);  // as above
+        const uint32_t w = gload4(a.v + row * a.v_stride + t.head * D + 2 * pair);
+        y[n][0] = from16<BF16>(w);
+        y[n][1] = from16<BF16>(w >> 16);
+        amax = max(amax, max(__builtin_bit_cast(uint32_t, y[n][0]) & 0x7fffffffu, __builtin_bit_cast(uint32_t, y[n][1]) & 0x7fffffffu));
+    }
+    const BlockScale b = block_scale(wave_max(amax), opens, old_scale, qmax);
+    if (lane == 0) *scale_at = b.scale;
+    const int group = o / kKvGroup, token = o % kKvGroup;
+    if (b.grows) {
+        recode<FMT>(codes, (group + 1) * 2 * D, b.shrink, lane, kWave);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the new bytes come behind the pieces that other lanes wrote around them
+    }
+    uint8_t* at = codes + group * kKvGroup * D + ((token >> 2) & 3) * 16 + (token >> 4) * 4 + (token & 3);
+#pragma unroll
+    for (int n = 0; n < kPairs; ++n) {
+        const int pair = lane + n * kWave;
+        if (2 * pair >= D) break;
+        const uint32_t w = b.finite ? codes_of<FMT>(y[n][0] / b.scale, y[n][1] / b.scale, 0.0f, 0.0f) : 0u;
+        at[pair * 64] = (uint8_t)w;
+        at[pair * 64 + 8] = (uint8_t)(w >> 8);
+    }
 }
 
 // value = code * scale, rounded once to 16 bits; the same split and the same units as above.  Rows of absent pages are zero.
@@ -396,11 +453,17 @@ __global__ __launch_bounds__(256) void rope_table_kernel(float2* __restrict__ ta
 
 namespace {
 template <int FMT, bool BF16>
-hipError_t append_nu(const KvCache& c, const KvSeqs& s, const KvAppendArgs& a, int grid, hipStream_t st) {
+hipError_t append_nu(const KvCache& c, const KvSeqs& s, const KvAppendArgs& a, hipStream_t st) {
+    const int64_t turns = a.q ? (int64_t)s.n_rows * a.q_split : 0;  // waves for the queries
+    if (s.max_rows == 1) {
+        kv_append_one_kernel<FMT, BF16><<<dim3((unsigned)((a.tasks + turns + 3) / 4)), dim3(256), 0, st>>>(c, s, a);
+        return hipGetLastError();
+    }
+    const int grid = a.tasks + (int)((turns + 3) / 4);
     // pieces of sixteen codes per thread: of the 32-token groups of a block that max_rows rows can touch (the registers of a whole block
     // would let a compute unit hold two workgroups)
     const int groups = (s.max_rows + 2 * kKvGroup - 2) / kKvGroup, all = c.block / kKvGroup;
-    const int per_thread = s.max_rows == 1 ? 1 : ((groups < all ? groups : all) * 2 * c.dim + 255) / 256;
+    const int per_thread = ((groups < all ? groups : all) * 2 * c.dim + 255) / 256;
     if (per_thread <= 1) kv_append_kernel<1, FMT, BF16><<<dim3(grid), dim3(256), 0, st>>>(c, s, a);
     else if (per_thread <= 2) kv_append_kernel<2, FMT, BF16><<<dim3(grid), dim3(256), 0, st>>>(c, s, a);
     else if (per_thread <= 4) kv_append_kernel<4, FMT, BF16><<<dim3(grid), dim3(256), 0, st>>>(c, s, a);
@@ -416,9 +479,8 @@ hipError_t launch_kv_append(const KvCache& c, const KvSeqs& s, const KvAppendArg
     // a wave per row of queries, or several where rows are few: then the way to the first of them is what there is to save
     const int passes = a.q ? (a.q_heads + kWave / (c.dim / 16) - 1) / (kWave / (c.dim / 16)) : 1;
     a.q_split = s.n_rows >= 1024 ? 1 : (1024 / s.n_rows < passes ? 1024 / s.n_rows : passes);
-    const int grid = a.tasks + (a.q ? (int)(((int64_t)s.n_rows * a.q_split + 3) / 4) : 0);
-    if (format == kKvInt8) return bf16 ? append_nu<kKvInt8, true>(c, s, a, grid, st) : append_nu<kKvInt8, false>(c, s, a, grid, st);
-    return bf16 ? append_nu<kKvE4m3, true>(c, s, a, grid, st) : append_nu<kKvE4m3, false>(c, s, a, grid, st);
+    if (format == kKvInt8) return bf16 ? append_nu<kKvInt8, true>(c, s, a, st) : append_nu<kKvInt8, false>(c, s, a, st);
+    return bf16 ? append_nu<kKvE4m3, true>(c, s, a, st) : append_nu<kKvE4m3, false>(c, s, a, st);
 }
 
 hipError_t launch_kv_gather(const KvCache& c, const KvSeqs& s, uint16_t* k_out, uint16_t* v_out, int format, bool bf16, hipStream_t st) {

@@ -117,6 +117,31 @@ def test_append_is_the_definition_bit_for_bit(fmt, dtype, D, P, heads, qh, rot, 
         at += m
 
 
+@pytest.mark.parametrize("fmt,dtype,D,P,heads,rot,inter", [
+    ("int8", "fp16", 64, 32, 1, 64, False), ("e4m3", "bf16", 128, 64, 3, 64, True), ("int8", "bf16", 192, 128, 2, 32, False),
+    ("e4m3", "fp16", 256, 128, 1, 256, False)])
+def test_single_tokens_into_every_place_of_a_block(fmt, dtype, D, P, heads, rot, inter):
+    # one sequence from nothing through a whole block into the next, one behind a prompt, one that rests in most calls
+    steps = [[1, 1, int(i % 7 == 0)] for i in range(P + 3)]
+    test_append_is_the_definition_bit_for_bit(fmt, dtype, D, P, heads, 2, rot, inter, [[0, P // 2 + 5, 1]] + steps)
+
+
+def test_a_single_token_that_is_not_finite_says_so_until_its_block_is_opened_again():
+    cache = F.KVCache(3, 2, 128, 32, F.KV_INT8, torch.bfloat16, DEV)
+    x = torch.ones((1, 2, 128), dtype=torch.bfloat16, device=DEV)
+    table = i32([[2, 0]])
+    for i in range(6):
+        y = x * (1.0 + i)
+        if i == 3:
+            y[0, 1, 127] = float("inf")
+        F.floe_kv_append(cache, x, y, cu_of([1]), i32([i]), table, 1)
+    k, v = F.floe_kv_gather(cache, i32([0]), cu_of([6]), table, 6, 6)
+    assert torch.isnan(v[:, 1]).all() and torch.isfinite(v[:, 0]).all() and torch.isfinite(k).all()
+    F.floe_kv_append(cache, x, x, cu_of([1]), i32([0]), table, 1)
+    k, v = F.floe_kv_gather(cache, i32([0]), cu_of([1]), table, 1, 1)
+    assert torch.isfinite(v).all()
+
+
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 def test_a_block_that_takes_a_value_that_is_not_finite_says_so_until_it_is_opened_again(fmt, bad):
