@@ -549,17 +549,21 @@ class KVCache:
                               (self.k_scale, n, torch.float32), (self.v_scale, n, torch.float32)):
             if t.numel() != size or t.dtype != kind or not t.is_contiguous():
                 raise ValueError(f"KVCache: expected a contiguous {kind} tensor of {size} elements, got {t.dtype} {tuple(t.shape)}")
+        self._device = self.k.get_device()  # (-1 for tensors of the host; a look at t.device costs twice as much)
+        if any(t.get_device() != self._device for t in tensors):
+            raise ValueError("KVCache: the four arrays are on one device")
         self._c = _KvCache(self.n_pages, self.kv_heads, self.head_dim, self.block, self.fmt, _KV_DTYPES[dtype], self.k.data_ptr(),
                            self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
         self._at = C.addressof(self._c)
         self._ws = {}
 
     def workspace(self, nbytes: int, stream: int):
-        """(address, bytes) of scratch for the attention calls on a stream: an array per stream, since the calls on one are ordered."""
+        """(address, bytes) of scratch for the attention calls on a stream: an array per stream, since the calls on one are ordered.
+        An array that was too small stays (a captured graph may hold its address); each is twice the one before or more."""
         ws = self._ws.get(stream)
         if ws is None or ws[2] < nbytes:
-            array = _workspace(nbytes, self.k.device)
-            ws = self._ws[stream] = (array, *_aligned_ptr(array))
+            array = _workspace(max(nbytes, 2 * ws[2]) if ws else nbytes, self.k.device)
+            ws = self._ws[stream] = (array, *_aligned_ptr(array), ws)
         return ws[1], ws[2]
 
 
@@ -604,14 +608,16 @@ def _kv_calls():
     return _kv_functions
 
 
-def _kv_seqs(cu_rows, length, block_table, n_rows, max_rows) -> bytes:
-    n, i32 = cu_rows.shape[0] - 1, torch.int32
+def _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows) -> bytes:
+    device, n, i32 = cache._device, cu_rows.shape[0] - 1, torch.int32
     shape = block_table.shape
     if not (cu_rows.dtype is i32 and length.dtype is i32 and block_table.dtype is i32 and cu_rows.is_contiguous() and length.is_contiguous()
             and block_table.is_contiguous()):
         raise ValueError("cu_rows, lengths and block_table are contiguous int32 tensors")
     if length.shape[0] != n or len(shape) != 2 or shape[0] != n:
         raise ValueError(f"{n} sequences in cu_rows, {tuple(length.shape)} lengths, block_table {tuple(shape)}")
+    if cu_rows.get_device() != device or length.get_device() != device or block_table.get_device() != device or device < 0:
+        raise ValueError("cu_rows, lengths and block_table are on the cache's GPU")
     return _SEQS_FIELDS.pack(n, n_rows, max_rows, shape[1], cu_rows.data_ptr(), length.data_ptr(), block_table.data_ptr())
 
 
@@ -621,13 +627,15 @@ def _kv_wrong(t, cache, heads, n_rows, name):
         raise ValueError(f"{name}: expected {cache.dtype} [rows][{heads}][{cache.head_dim}], got {t.dtype} {shape}")
     if shape[0] != n_rows:
         raise ValueError(f"{name}: {shape[0]} rows, expected {n_rows}")
+    if t.get_device() != cache._device:
+        raise ValueError(f"{name}: on {t.device}, the cache is on {cache.k.device}")
     raise ValueError(f"{name}: the heads of a row lie one behind the other (strides {t.stride()})")
 
 
 def _kv_rows(t, cache: KVCache, heads, n_rows, name: str):
     """Row stride of a 16-bit tensor [n_rows][heads][head_dim] whose rows may lie anywhere."""
     shape, D = t.shape, cache.head_dim
-    if t.dtype is not cache.dtype or len(shape) != 3 or shape[2] != D or shape[1] != heads or shape[0] != n_rows:
+    if t.dtype is not cache.dtype or len(shape) != 3 or shape[2] != D or shape[1] != heads or shape[0] != n_rows or t.get_device() != cache._device:
         _kv_wrong(t, cache, heads, n_rows, name)
     stride = t.stride()
     if (stride[2] != 1 or (stride[1] != D and heads > 1)) and n_rows:
@@ -639,8 +647,8 @@ def _kv_out(t, cache, shape, dtype, device, name):
     """An output tensor: the caller's, if it fits, or a new one."""
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or t.get_device() != cache._device:
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
 
 
@@ -657,9 +665,12 @@ def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows:
         qs, q_at = _kv_rows(q, cache, heads, n_rows, "q"), q.data_ptr()
         q_out = _kv_out(q_out, cache, shape, cache.dtype, q.device, "q_out")
         q_out_at = q_out.data_ptr()
-    if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n_rows,) or not positions.is_contiguous()):
-        raise ValueError(f"positions: expected contiguous int32 [{n_rows}]")
-    rc = _kv_calls()[0](cache._at, _kv_seqs(cu_rows, length, block_table, n_rows, max_rows), k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs,
+    if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n_rows,) or not positions.is_contiguous()
+                                  or positions.get_device() != cache._device):
+        raise ValueError(f"positions: expected contiguous int32 [{n_rows}] on {cache.k.device}")
+    if rope is not None and rope.table.get_device() != cache._device:
+        raise ValueError(f"rope: its table is on {rope.table.device}, the cache on {cache.k.device}")
+    rc = _kv_calls()[0](cache._at, _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows), k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs,
                         heads, q_out_at, None if rope is None else rope._packed(positions), _stream(stream))
     if rc:
         _check(rc, "floe_kv_append")
@@ -671,7 +682,7 @@ def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max
     shape, device = (n_rows, cache.kv_heads, cache.head_dim), cache.k.device
     k_out = _kv_out(k_out, cache, shape, cache.dtype, device, "k_out")
     v_out = _kv_out(v_out, cache, shape, cache.dtype, device, "v_out")
-    rc = _kv_calls()[1](cache._at, _kv_seqs(cu_rows, first, block_table, n_rows, max_rows), k_out.data_ptr(), v_out.data_ptr(), _stream(stream))
+    rc = _kv_calls()[1](cache._at, _kv_seqs(cache, cu_rows, first, block_table, n_rows, max_rows), k_out.data_ptr(), v_out.data_ptr(), _stream(stream))
     if rc:
         _check(rc, "floe_kv_gather")
     return k_out, v_out
@@ -680,7 +691,8 @@ def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max
 def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows: int, max_len: int, scale: float = None,
                       causal: bool = True, window: int = 0, want_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
     """Attention of q [rows][q_heads][head_dim] over the cache; length[s] counts the rows' own tokens.  Returns out, or (out, lse) with
-    want_lse.  scale: 1 / sqrt(head_dim) by default.  workspace: the cache's own (one per stream) unless handed over."""
+    want_lse.  scale: 1 / sqrt(head_dim) by default.  workspace: the cache's own (one per stream) unless handed over; a captured call
+    keeps the one of the stream it was captured on, so graphs that run side by side are captured on different streams or bring theirs."""
     shape, device = q.shape, q.device
     n_rows, heads = shape[0], shape[1] if len(shape) == 3 else 0
     qs = _kv_rows(q, cache, heads, n_rows, "q")
@@ -688,8 +700,10 @@ def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows:
     if want_lse or lse is not None:
         lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, device, "lse")
     call, need = _kv_calls()[2:]
-    s = _kv_seqs(cu_rows, length, block_table, n_rows, max_rows)
+    s = _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows)
     a = _ATTENTION_FIELDS.pack(heads, causal, window, max_len, cache.head_dim ** -0.5 if scale is None else scale)
+    if workspace is not None and workspace.get_device() != cache._device:
+        raise ValueError(f"workspace: on {workspace.device}, the cache is on {cache.k.device}")
     st = _stream(stream)
     at, size = cache.workspace(256, st) if workspace is None else _aligned_ptr(workspace)
     args = cache._at, s, a, q.data_ptr(), qs, out.data_ptr(), None if lse is None else lse.data_ptr()

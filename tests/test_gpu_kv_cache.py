@@ -242,3 +242,22 @@ def test_a_cache_whose_offsets_pass_32_bits():
         w = p @ v[:, h2 // 2].double().cpu()
         size = p @ v[:, h2 // 2].double().cpu().abs()  # weights rounded to fp16, K and V read back in fp16, one rounding at the end
         assert ((o[0, h2].double().cpu() - w).abs() <= 2.0 ** -9 * size).all()
+
+
+def test_tensors_that_are_not_on_the_caches_device_are_refused():
+    c = F.KVCache(2, 2, 64, 32, device=DEV)
+    cu, n, table = cu_of([3]), i32([0]), i32([[0, 1]])
+    x = torch.zeros((3, 2, 64), dtype=torch.float16, device=DEV)
+    rope = F.Rope(torch.zeros((8, 32, 2), dtype=torch.float32))
+    for args, more in (((x.cpu(), x, cu, n, table), {}), ((x, x.cpu(), cu, n, table), {}), ((x, x, cu.cpu(), n, table), {}),
+                       ((x, x, cu, n.cpu(), table), {}), ((x, x, cu, n, table.cpu()), {}), ((x, x, cu, n, table), dict(rope=rope)),
+                       ((x, x, cu, n, table), dict(positions=torch.zeros(3, dtype=torch.int32)))):
+        with pytest.raises(ValueError):
+            F.floe_kv_append(c, *args, 3, **more)
+    for q, more in ((x.cpu(), {}), (x, dict(out=x.cpu())), (x, dict(lse=torch.zeros((3, 2)))), (x, dict(workspace=torch.zeros(1 << 20, dtype=torch.uint8)))):
+        with pytest.raises(ValueError):
+            F.floe_kv_attention(c, q, cu, i32([3]), table, 3, 3, **more)
+    with pytest.raises(ValueError):
+        F.floe_kv_gather(c, n, cu, table, 3, 3, k_out=x.cpu())
+    with pytest.raises(ValueError):
+        F.KVCache(2, 2, 64, 32, device=DEV, tensors=(c.k, c.v, c.k_scale.cpu(), c.v_scale))

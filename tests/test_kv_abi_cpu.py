@@ -2,6 +2,7 @@
 are made up and never followed), and the binding refuses tensors that do not fit."""
 import ctypes as C
 import os
+import weakref
 
 import pytest
 import torch
@@ -121,3 +122,23 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         F.KVCache(2, 2, 64, 32, device="cpu", tensors=(c.k, c.v, c.k_scale, c.v_scale[:1]))
     with pytest.raises(ValueError):
         F.Rope(torch.zeros((4, 8), dtype=torch.float32))
+
+
+def test_the_binding_refuses_tensors_of_the_host_before_the_library_sees_them():
+    c = F.KVCache(2, 2, 64, 32, device="cpu")
+    cu, n, table = torch.tensor([0, 3], dtype=torch.int32), torch.tensor([3], dtype=torch.int32), torch.zeros((1, 2), dtype=torch.int32)
+    x = torch.zeros((3, 2, 64), dtype=torch.float16)
+    for call in (lambda: F.floe_kv_append(c, x, x, cu, n, table, 3), lambda: F.floe_kv_attention(c, x, cu, n, table, 3, 3, workspace=c.k),
+                 lambda: F.floe_kv_gather(c, n, cu, table, 3, 3)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
+def test_a_workspace_that_was_outgrown_stays_for_the_graphs_that_hold_its_address():
+    c = F.KVCache(1, 1, 64, 32, device="cpu")
+    at, size = c.workspace(256, 7)
+    assert c.workspace(size, 7) == (at, size)
+    small = weakref.ref(c._ws[7][0])
+    larger, more = c.workspace(size + 1, 7)
+    assert larger != at and more >= 2 * size and c.workspace(256, 7) == (larger, more)
+    assert small() is not None and small().data_ptr() <= at
