@@ -58,7 +58,7 @@ struct AttnPlan {
     int most_rows;  // sequences of up to so many rows are the rows kernel's
     int row_limit;  // at least the rows of any of those
     int mt, tiles, chunk, chunks, part_rows;
-    int prompt_tiles, prompt_chunk, prompt_chunks;
+    int prompt_waves, prompt_rows, prompt_tiles, prompt_chunk, prompt_chunks;
     size_t rows_off, ml_off, prompt_ml_off, total;  // (the prompt kernel's come first)
 };
 // How segments (sequence, KV head, tile of rows) of up to `units` units of 32 tokens are cut into chunks: as many as give every compute
@@ -77,19 +77,41 @@ void cut_segments(AttnPlan& w, int64_t segments, int64_t units) {
     w.chunk = (int)((units + chunks - 1) / chunks);
     w.chunks = (int)chunks;
 }
-// Chunks of the prompt kernel's tiles of rows: what costs least in tiles of 64 tokens (about 2.4 us each at 128 dims), the last round's
-// compute units standing idle among it, two tiles' worth for every round's start, and the partial results' way to memory and back.
-void cut_prompts(AttnPlan& w, int dim, int64_t segments, int64_t tiles) {
-    const int64_t slots = (int64_t)num_cus() * (dim == 64 ? 2 : 1);  // workgroups at a time
-    const double part = kv_prompt_rows(dim) * 8.0 * 128 / 5.0e6 / 2.4;
-    double best = 0;
-    int64_t chunks = 1;
-    for (int64_t c = 1; c <= 32 && c <= tiles && (c == 1 || segments * c <= 8 * slots); ++c) {
-        const int64_t rounds = (segments * c + slots - 1) / slots;
-        const double cost = rounds * ((tiles + c - 1) / c + 2.0) + (c > 1 ? 2.0 + segments * c * part : 0.0);
-        if (c == 1 || cost < best) best = cost, chunks = c;
+// The prompt kernel's tiles of rows and their chunks: what costs least.  us, measured with n workgroups (8 heads of 256 rows, and 256 of
+// them) over 1024 and 2048 tokens: the start and end of a workgroup, a tile of 64 tokens while it has the card to itself, and with all taken.
+struct PromptCost {
+    int waves;
+    double start, alone, full;
+    int slots;  // workgroups of a compute unit at a time
+};
+PromptCost prompt_cost(int dim, bool half) {
+    if (dim == 64) return {4, 6.0, 1.15, 1.9, 2};
+    if (dim == 128) return half ? PromptCost{4, 8.0, 1.5, 2.85, 2} : PromptCost{8, 11.0, 1.9, 2.7, 1};
+    if (dim == 192) return half ? PromptCost{4, 10.0, 2.3, 2.4, 1} : PromptCost{8, 13.5, 2.9, 3.9, 1};
+    return {8, 8.5, 3.0, 3.6, 1};
+}
+// Four waves leave fewer compute units idle where rows are few, eight read the cache half as often.  us, 32 / 8 heads of 128, 8 / 4 waves:
+// 6 sequences of 466 with one KV head 30.9 / 19.9, 12 of 446 with 16 / 8 heads 34.6 / 30.4, 2 x 2048 rows behind 4000 tokens 343 / 365;
+// 40 / 5 heads of 192, 2224 rows with a window of 155: 93 / 115.
+void cut_prompts(AttnPlan& w, int dim, int64_t heads, int64_t rows, int64_t tiles) {
+    double best = -1;
+    for (int half = 0; half < (dim == 128 || dim == 192 ? 2 : 1); ++half) {
+        const PromptCost t = prompt_cost(dim, half);
+        const int64_t tile_rows = kv_prompt_rows(dim, t.waves), row_tiles = (rows + tile_rows - 1) / tile_rows, segments = heads * row_tiles;
+        const int64_t cus = num_cus(), slots = cus * t.slots;
+        for (int64_t c = 1; c <= 32 && c <= tiles && (c == 1 || segments * c <= 8 * slots); ++c) {
+            const int64_t groups = segments * c, rounds = (groups + slots - 1) / slots;
+            const double tile = groups <= (t.slots == 1 ? cus / 2 : cus) ? t.alone : t.full;
+            // (a join costs its launch and the partial results' way to memory and back)
+            const double cost = rounds * ((tiles + c - 1) / c * tile + t.start) + (c > 1 ? 5.0 + groups * tile_rows * dim * 8.0 / 5.0e6 : 0.0);
+            if (best >= 0 && cost >= best) continue;
+            best = cost;
+            w.prompt_waves = t.waves;
+            w.prompt_rows = (int)tile_rows;
+            w.prompt_tiles = (int)row_tiles;
+            w.prompt_chunk = (int)((tiles + c - 1) / c);
+        }
     }
-    w.prompt_chunk = (int)((tiles + chunks - 1) / chunks);
     w.prompt_chunks = (int)((tiles + w.prompt_chunk - 1) / w.prompt_chunk);
 }
 AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
@@ -102,7 +124,7 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
     if (k.max_rows > most) {
         // Sequences with few rows are the rows kernel's, unless there can be none (n_rows are too many for that) or the prompt kernel has
         // room for their tiles beside the others': then a launch costs more than it saves.
-        const int64_t tile_rows = kv_prompt_rows(c->head_dim);
+        const int64_t tile_rows = kv_prompt_rows(c->head_dim, prompt_cost(c->head_dim, false).waves);
         const int64_t tiles = k.n_seqs * ((k.max_rows * (int64_t)group + tile_rows - 1) / tile_rows) * c->kv_heads;
         w.prompt = true;
         w.rows = most > 0 && k.n_rows - (int64_t)(k.n_seqs - 1) * k.max_rows <= most && tiles > num_cus();
@@ -111,14 +133,12 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
     }
     const int64_t max_keys = a->max_len;
     if (w.prompt) {
-        const int64_t tile_rows = kv_prompt_rows(c->head_dim);
-        w.prompt_tiles = (int)(((int64_t)k.max_rows * group + tile_rows - 1) / tile_rows);
-        const int64_t keys = a->window > 0 && a->window + tile_rows < max_keys ? a->window + tile_rows : max_keys;
-        const int64_t segments = (int64_t)k.n_seqs * c->kv_heads * w.prompt_tiles;
-        cut_prompts(w, c->head_dim, segments, (keys + 63) / 64 + 1);
+        const int64_t seen = a->window + (int64_t)k.max_rows;  // (a tile of rows sees less where they are many)
+        const int64_t keys = a->window > 0 && seen < max_keys ? seen : max_keys;
+        cut_prompts(w, c->head_dim, (int64_t)k.n_seqs * c->kv_heads, (int64_t)k.max_rows * group, (keys + 63) / 64 + 1);
         if ((int64_t)a->q_heads * k.max_rows > kMaxGrid) w.prompt_chunks = 1;  // (more rows than a join has workgroups)
         if (w.prompt_chunks > 1) {
-            const size_t parts = (size_t)segments * w.prompt_chunks * tile_rows;
+            const size_t parts = (size_t)k.n_seqs * c->kv_heads * w.prompt_tiles * w.prompt_chunks * w.prompt_rows;
             w.prompt_ml_off = align_up(parts * c->head_dim * 4);
             w.total = w.prompt_ml_off + align_up(parts * 8);
         }
@@ -242,6 +262,8 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     k.most_rows = w.most_rows;
     k.parts = KvParts{reinterpret_cast<float*>(base + w.rows_off), reinterpret_cast<float*>(base + w.ml_off)};
     k.prompt_parts = KvParts{reinterpret_cast<float*>(base), reinterpret_cast<float*>(base + w.prompt_ml_off)};
+    k.prompt_waves = w.prompt_waves;
+    k.prompt_rows = w.prompt_rows;
     k.prompt_tiles = w.prompt_tiles;
     k.prompt_chunk = w.prompt_chunk;
     k.prompt_chunks = w.prompt_chunks;

@@ -50,8 +50,10 @@ struct KvAttnArgs {
     int chunk, chunks;  // units of 32 tokens per chunk, chunks per segment
     int part_rows;      // rows of a partial result
     // prompt kernel (kv_prompt.h)
-    KvParts prompt_parts;  // [n_seqs][heads][prompt_tiles][prompt_chunks][rows of a tile]
-    int prompt_tiles;      // of kv_prompt_rows(dim) rows, per KV head
+    KvParts prompt_parts;  // [n_seqs][heads][prompt_tiles][prompt_chunks][prompt_rows]
+    int prompt_waves;      // of a workgroup: 4 or 8
+    int prompt_rows;       // kv_prompt_rows(dim, prompt_waves)
+    int prompt_tiles;      // of prompt_rows rows, per KV head
     int prompt_chunk, prompt_chunks;  // tiles of 64 tokens per chunk, chunks per tile of rows
 };
 
@@ -69,10 +71,9 @@ inline int kv_rows_tiles_for(int dim, int rows) {
 constexpr int kv_rows_waves_per_simd(int dim, int mt) { return dim * mt <= 128 ? 3 : dim * mt <= 256 && dim < 256 ? 2 : 1; }
 hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, hipStream_t st);  // mt tiles of sixteen rows per workgroup
 hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, hipStream_t st);
-// prompt kernel (kv_prompt.h): waves of a workgroup, how many share 32 query rows, rows of a workgroup
-constexpr int kv_prompt_waves(int dim) { return dim == 64 ? 4 : 8; }
+// prompt kernel (kv_prompt.h): how many waves share 32 query rows, rows of a workgroup
 constexpr int kv_prompt_split(int dim) { return dim == 256 ? 2 : 1; }
-constexpr int kv_prompt_rows(int dim) { return 32 * kv_prompt_waves(dim) / kv_prompt_split(dim); }
+constexpr int kv_prompt_rows(int dim, int waves) { return 32 * waves / kv_prompt_split(dim); }
 hipError_t launch_kv_prompt_int8(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_prompt_e4m3(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_prompt_join(const KvAttnArgs& a, hipStream_t st);

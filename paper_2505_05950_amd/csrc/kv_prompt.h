@@ -38,7 +38,7 @@ __device__ __forceinline__ PromptRange prompt_range(const KvAttnArgs& a, const K
 
 // blockIdx.x: KV head, sequence, tile of rows; blockIdx.y: chunk of the tokens (one, unless the card would not be filled)
 template <int D, int FMT, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(64 * NW, D == 192 && NW == 4 ? 1 : 2) void kv_prompt_kernel(KvAttnArgs a) {
     // kSplit waves share 32 rows: each forms all of S^T and the weights, and a part of the dims of O^T (whose registers bound the waves)
     constexpr int kThreads = 64 * NW, kPieces = PromptStage<D, NW>::kPieces, kChunks = D / 8;
     constexpr int kSplit = kv_prompt_split(D), kRowWaves = NW / kSplit, kOut = D / 32 / kSplit;
@@ -345,15 +345,14 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_prompt_kernel(KvAttnArgs a) {
 
 template <int D>
 __global__ __launch_bounds__(256) void kv_prompt_join_kernel(KvAttnArgs a) {
-    constexpr int kRows = kv_prompt_rows(D);
     const int seq = blockIdx.y, head_q = blockIdx.x % a.q_heads, token = blockIdx.x / a.q_heads;
     const KvSpan span = kv_span(a.s, seq);
     if (token >= span.rows || span.rows <= a.most_rows) return;
-    const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / kRows;
-    const PromptRange range = prompt_range(a, span, tile * kRows, kRows);
+    const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / a.prompt_rows;
+    const PromptRange range = prompt_range(a, span, tile * a.prompt_rows, a.prompt_rows);
     if (range.chunks == 1) return;  // finished where it was formed
     const size_t segment = ((size_t)seq * a.c.heads + head) * a.prompt_tiles + tile;
-    join_row<D>(a, a.prompt_parts, segment * a.prompt_chunks * kRows + rr - tile * kRows, kRows, range.chunks, span.row0 + token, head_q);
+    join_row<D>(a, a.prompt_parts, segment * a.prompt_chunks * a.prompt_rows + rr - tile * a.prompt_rows, a.prompt_rows, range.chunks, span.row0 + token, head_q);
 }
 
 }  // namespace floe

@@ -291,3 +291,23 @@ def test_calls_on_a_stream_of_their_own():
     s.synchronize()
     assert torch.equal(got, want)
 
+
+@pytest.mark.parametrize("D,fmt,dtype,heads,n,context", [
+    (128, "int8", "fp16", 4, 2048, 2048), (128, "e4m3", "bf16", 2, 1600, 6000), (192, "e4m3", "fp16", 4, 1600, 1600), (192, "int8", "bf16", 2, 1600, 6000),
+    (192, "int8", "fp16", 4, 1600, 2500)])
+def test_prompts_that_fill_the_card(D, fmt, dtype, heads, n, context):
+    # enough rows for the larger workgroups, with the context whole and cut; rows at the ends of their tiles and some between
+    rng = np.random.default_rng(D + context)
+    m, table = build(rng, [context], heads, D, 64, fmt, dtype)
+    q = to16(rng.normal(0, 2.0, (n, 8 * heads, D)).astype(np.float32), dtype)
+    out, lse = F.floe_kv_attention(m.device(dtype, DEV, 0x7f), q.to(DEV), cu_of([n]), i32([context]), i32(table), n, context, want_lse=True)
+    torch.cuda.synchronize()
+    k, there = m.value(0, context, table[0])
+    v, _ = m.value(1, context, table[0])
+    for i in [0, 1, 15, 16, 31, 32, 33, 63, 64, n // 2, n // 2 + 7, n - 33, n - 32, n - 2, n - 1]:
+        seen = context - n + i + 1
+        want, want_lse, size = R.attention(q[i:i + 1].double().numpy(), k[:seen], v[:seen], there[:seen], seen, True, 0, D ** -0.5)
+        off = np.abs(out[i].double().cpu().numpy() - want[0])
+        bar = R.HALF_STEP[dtype] * np.abs(want[0]) + (2.0 ** -11 + 1e-4) * size[0] + 2.0 ** -25
+        assert (off <= bar).all(), (i, float((off / bar).max()))
+        assert (np.abs(lse[i].double().cpu().numpy() - want_lse[0]) <= 1e-4 + 1e-6 * np.abs(want_lse[0])).all(), i
