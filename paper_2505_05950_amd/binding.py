@@ -643,12 +643,14 @@ def _kv_rows(t, cache: KVCache, heads, n_rows, name: str):
     return stride[0] if n_rows > 1 else heads * D
 
 
-def _kv_out(t, cache, shape, dtype, device, name):
-    """An output tensor: the caller's, if it fits, or a new one."""
+def _kv_out(t, cache, shape, dtype, like, name):
+    """An output tensor: the caller's, if it fits, or a new one beside `like` (which saves 1 us where it has the same form)."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        if like.dtype is dtype and like.shape == shape and like.is_contiguous():
+            return torch.empty_like(like)
+        return like.new_empty(shape, dtype=dtype)
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or t.get_device() != cache._device:
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
 
 
@@ -663,7 +665,7 @@ def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows:
         shape = q.shape
         heads = shape[1] if len(shape) == 3 else 0
         qs, q_at = _kv_rows(q, cache, heads, n_rows, "q"), q.data_ptr()
-        q_out = _kv_out(q_out, cache, shape, cache.dtype, q.device, "q_out")
+        q_out = _kv_out(q_out, cache, shape, cache.dtype, q, "q_out")
         q_out_at = q_out.data_ptr()
     if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n_rows,) or not positions.is_contiguous()
                                   or positions.get_device() != cache._device):
@@ -679,9 +681,9 @@ def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows:
 
 def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max_rows: int, k_out=None, v_out=None, stream=None):
     """Rows cu_rows[s] .. cu_rows[s + 1) are tokens first[s], first[s] + 1, ... of sequence s: (k, v) 16-bit [n_rows][kv_heads][head_dim]."""
-    shape, device = (n_rows, cache.kv_heads, cache.head_dim), cache.k.device
-    k_out = _kv_out(k_out, cache, shape, cache.dtype, device, "k_out")
-    v_out = _kv_out(v_out, cache, shape, cache.dtype, device, "v_out")
+    shape = (n_rows, cache.kv_heads, cache.head_dim)
+    k_out = _kv_out(k_out, cache, shape, cache.dtype, cache.k, "k_out")
+    v_out = _kv_out(v_out, cache, shape, cache.dtype, k_out, "v_out")
     rc = _kv_calls()[1](cache._at, _kv_seqs(cache, cu_rows, first, block_table, n_rows, max_rows), k_out.data_ptr(), v_out.data_ptr(), _stream(stream))
     if rc:
         _check(rc, "floe_kv_gather")
@@ -693,12 +695,12 @@ def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows:
     """Attention of q [rows][q_heads][head_dim] over the cache; length[s] counts the rows' own tokens.  Returns out, or (out, lse) with
     want_lse.  scale: 1 / sqrt(head_dim) by default.  workspace: the cache's own (one per stream) unless handed over; a captured call
     keeps the one of the stream it was captured on, so graphs that run side by side are captured on different streams or bring theirs."""
-    shape, device = q.shape, q.device
+    shape = q.shape
     n_rows, heads = shape[0], shape[1] if len(shape) == 3 else 0
     qs = _kv_rows(q, cache, heads, n_rows, "q")
-    out = _kv_out(out, cache, shape, cache.dtype, device, "out")
+    out = _kv_out(out, cache, shape, cache.dtype, q, "out")
     if want_lse or lse is not None:
-        lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, device, "lse")
+        lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, q, "lse")
     call, need = _kv_calls()[2:]
     s = _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows)
     a = _ATTENTION_FIELDS.pack(heads, causal, window, max_len, cache.head_dim ** -0.5 if scale is None else scale)
