@@ -187,10 +187,10 @@ __device__ __forceinline__ void turn_queries(const KvCache& c, const KvSeqs& s, 
 }  // namespace
 
 // A workgroup owns one block x head of K or of V, so nobody else touches its codes and its scale: no atomics, one pass over the rows
-// (they stay in registers between the maximum and the codes).  NU units of sixteen codes per thread hold what a call can bring to a block.  A unit of V is the
-// sixteen bytes that lie next to each other in the cache (eight tokens x two dims): neighbouring lanes take the four token groups
-// and then the next pair of dims, so a wave writes 1 KiB in one piece and reads 64 bytes of each row.  The workgroups behind the last
-// task turn the queries.
+// (they stay in registers between the maximum and the codes).  NU units of sixteen codes per thread hold what a call can bring to a
+// block.  A unit of V is the sixteen bytes that lie next to each other in the cache (eight tokens x two dims): neighbouring lanes take
+// the four token groups and then the next pair of dims, so a wave writes 1 KiB in one piece and reads 64 bytes of each row.  The
+// workgroups behind the last task turn the queries.
 template <int NU, int FMT, bool BF16>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvAppendArgs a) {
     __shared__ uint32_t lds_max[4];
@@ -319,7 +319,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvCache c, KvSeqs s, KvA
 }
 
 // One token per sequence: a wave owns the block x head.  The block's maximum is a wave's, V's token is two bytes per pair of dims, and
-// what lies beside them is read only where the scale grows.
+// what lies beside them is read only where the scale grows.  What bounds it is the way from lengths to pages to scale and rows (4.4 us for
+// one sequence), and the number of such ways: 98 sequences, 16 heads of 192 with the attention 29.9 us when a workgroup took each, 26.3 so.
 template <int FMT, bool BF16>
 __global__ __launch_bounds__(256) void kv_append_one_kernel(KvCache c, KvSeqs s, KvAppendArgs a) {
     const int lane = threadIdx.x & 63, D = c.dim, id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
