@@ -46,7 +46,7 @@ int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_at
     if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0) return FLOE_EINVAL;
     if (a->q_heads % c->kv_heads != 0) return FLOE_ESHAPE;
     if (a->q_heads > 1024 || a->window > kKvMaxLen) return FLOE_EUNSUPPORTED;
-    // (the widest grid: a workgroup per 128 query rows of a KV head, or per row where there are few)
+    // (the widest grid that has to do: a workgroup per 128 query rows of a KV head, or per row where there are few)
     const KvSeqs k = dev_seqs(s);
     if (((int64_t)k.max_rows * (a->q_heads / c->kv_heads) / 128 + 4) * k.n_seqs * c->kv_heads > kMaxGrid) return FLOE_EUNSUPPORTED;
     if ((int64_t)k.max_rows * a->q_heads > 0x7fffffff) return FLOE_EUNSUPPORTED;
@@ -88,16 +88,18 @@ PromptCost prompt_cost(int dim, bool half) {
     if (dim == 64) return {4, 6.0, 1.15, 1.9, 2};
     if (dim == 128) return half ? PromptCost{4, 8.0, 1.5, 2.85, 2} : PromptCost{8, 11.0, 1.9, 2.7, 1};
     if (dim == 192) return half ? PromptCost{4, 10.0, 2.3, 2.4, 1} : PromptCost{8, 13.5, 2.9, 3.9, 1};
-    return {8, 8.5, 3.0, 3.6, 1};
+    return half ? PromptCost{4, 8.5, 2.35, 2.65, 1} : PromptCost{8, 8.5, 3.0, 3.8, 1};
 }
 // Four waves leave fewer compute units idle where rows are few, eight read the cache half as often.  us, 32 / 8 heads of 128, 8 / 4 waves:
 // 6 sequences of 466 with one KV head 30.9 / 19.9, 12 of 446 with 16 / 8 heads 34.6 / 30.4, 2 x 2048 rows behind 4000 tokens 343 / 365;
-// 40 / 5 heads of 192, 2224 rows with a window of 155: 93 / 115.
+// 40 / 5 heads of 192, 2224 rows with a window of 155: 93 / 115;
+// 16 / 4 heads of 256, one prompt of 500 35.5 / 28.1, 6 of 1500 with a window of 700 140 / 204.
 void cut_prompts(AttnPlan& w, int dim, int64_t heads, int64_t rows, int64_t tiles) {
     double best = -1;
-    for (int half = 0; half < (dim == 128 || dim == 192 ? 2 : 1); ++half) {
+    for (int half = 0; half < (dim == 64 ? 1 : 2); ++half) {
         const PromptCost t = prompt_cost(dim, half);
         const int64_t tile_rows = kv_prompt_rows(dim, t.waves), row_tiles = (rows + tile_rows - 1) / tile_rows, segments = heads * row_tiles;
+        if (half && segments > kMaxGrid) break;
         const int64_t cus = num_cus(), slots = cus * t.slots;
         for (int64_t c = 1; c <= 32 && c <= tiles && (c == 1 || segments * c <= 8 * slots); ++c) {
             const int64_t groups = segments * c, rounds = (groups + slots - 1) / slots;

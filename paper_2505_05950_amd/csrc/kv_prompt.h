@@ -38,7 +38,7 @@ __device__ __forceinline__ PromptRange prompt_range(const KvAttnArgs& a, const K
 
 // blockIdx.x: KV head, sequence, tile of rows; blockIdx.y: chunk of the tokens (one, unless the card would not be filled)
 template <int D, int FMT, int NW>
-__global__ __launch_bounds__(64 * NW, D == 192 && NW == 4 ? 1 : 2) void kv_prompt_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_prompt_kernel(KvAttnArgs a) {
     // kSplit waves share 32 rows: each forms all of S^T and the weights, and a part of the dims of O^T (whose registers bound the waves)
     constexpr int kThreads = 64 * NW, kPieces = PromptStage<D, NW>::kPieces, kChunks = D / 8;
     constexpr int kSplit = kv_prompt_split(D), kRowWaves = NW / kSplit, kOut = D / 32 / kSplit;

@@ -16,7 +16,7 @@ hipError_t kv_prompt_dispatch(const KvAttnArgs& a, hipStream_t st) {
         case 64: return kv_prompt_instance<FMT, 64, 4>(a, st);
         case 128: return a.prompt_waves == 4 ? kv_prompt_instance<FMT, 128, 4>(a, st) : kv_prompt_instance<FMT, 128, 8>(a, st);
         case 192: return a.prompt_waves == 4 ? kv_prompt_instance<FMT, 192, 4>(a, st) : kv_prompt_instance<FMT, 192, 8>(a, st);
-        default: return kv_prompt_instance<FMT, 256, 8>(a, st);
+        default: return a.prompt_waves == 4 ? kv_prompt_instance<FMT, 256, 4>(a, st) : kv_prompt_instance<FMT, 256, 8>(a, st);
     }
 }
 

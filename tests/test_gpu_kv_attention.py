@@ -294,7 +294,7 @@ def test_calls_on_a_stream_of_their_own():
 
 @pytest.mark.parametrize("D,fmt,dtype,heads,n,context", [
     (128, "int8", "fp16", 4, 2048, 2048), (128, "e4m3", "bf16", 2, 1600, 6000), (192, "e4m3", "fp16", 4, 1600, 1600), (192, "int8", "bf16", 2, 1600, 6000),
-    (192, "int8", "fp16", 4, 1600, 2500)])
+    (192, "int8", "fp16", 4, 1600, 2500), (256, "int8", "bf16", 4, 1000, 1000), (256, "e4m3", "fp16", 2, 1000, 4100), (256, "int8", "fp16", 1, 500, 3000)])
 def test_prompts_that_fill_the_card(D, fmt, dtype, heads, n, context):
     # enough rows for the larger workgroups, with the context whole and cut; rows at the ends of their tiles and some between
     rng = np.random.default_rng(D + context)
