@@ -120,7 +120,7 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
     AttnPlan w{};
     w.total = kAlign;  // (so that a workspace is a workspace whichever kernels run)
     const KvSeqs k = dev_seqs(s);
-    const int group = a->q_heads / c->kv_heads, most = kv_rows_limit(c->head_dim) / group;
+    const int group = a->q_heads / c->kv_heads, most = kKvRowsLimit / group;
     w.rows = true;
     w.most_rows = w.row_limit = k.max_rows;
     if (k.max_rows > most) {

@@ -311,3 +311,12 @@ def test_prompts_that_fill_the_card(D, fmt, dtype, heads, n, context):
         bar = R.HALF_STEP[dtype] * np.abs(want[0]) + (2.0 ** -11 + 1e-4) * size[0] + 2.0 ** -25
         assert (off <= bar).all(), (i, float((off / bar).max()))
         assert (np.abs(lse[i].double().cpu().numpy() - want_lse[0]) <= 1e-4 + 1e-6 * np.abs(want_lse[0])).all(), i
+
+
+@pytest.mark.parametrize("D,heads,qh", [(128, 1, 128), (64, 2, 130), (256, 1, 80)])
+def test_groups_of_more_heads_than_the_rows_kernel_takes(D, heads, qh):
+    rng = np.random.default_rng(qh)
+    lens = [1, 0, 33, 64, 200, 700]
+    m, table = build(rng, lens, heads, D, 32, "int8", "fp16")
+    check(m, table, lens, [1, 0, 1, 1, 1, 1], qh, "fp16", rng=rng)
+    check(m, table, lens, [1, 0, 2, 1, 3, 0], qh, "fp16", rng=rng)
