@@ -481,7 +481,8 @@ int floe_kv_gather(const floe_kv_cache* c, const floe_kv_seqs* s, void* k_out, v
  *   keys j <= its position (causal) or all j < len[s];  with window > 0 only j > position - window
  * Query head h reads KV head h / (q_heads / kv_heads).  out[row][h] = softmax(scale q.K) V, fp32 statistics and sums, rounded once;
  * lse[row][h] (dev float, or NULL) = log of the sum of exp(scale q.K).  A row that sees no key: out 0, lse -infinity.
- * Rows that belong to no sequence, and those of a sequence behind max_rows, are left as they are.
+ * Rows that belong to no sequence, and those of a sequence behind its first max_rows, are left as they are (n counts those too: the
+ * rows before them keep their positions).
  * q dev 16-bit, q_stride elements from row to row (a multiple of 8), heads contiguous; out dev [n_rows][q_heads][head_dim]; both 16-byte
  * aligned.  max_len: at least every len (host side).  It only chooses between kernels: results agree to rounding whatever it says.
  * workspace: dev, 256-byte aligned, floe_kv_attention_workspace_bytes(); contents are scratch.

@@ -139,15 +139,18 @@ __device__ __forceinline__ float quad_sum(float x) {
 }
 
 // A sequence's rows and length as a kernel may use them, whatever the arrays hold: rows inside [0, n_rows], at most max_rows of them.
+// Where they are fewer than cu_rows says, they are its first ones: pos0 counts all of them.
 struct KvSpan {
     int row0, rows, len;
+    int pos0;  // where the first row sits if the sequence's rows are the last ones of its len tokens; at least -kKvMaxLen
 };
 __device__ __forceinline__ KvSpan kv_span(const KvSeqs& s, int seq) {
-    const int a = s.cu[seq], b = s.cu[seq + 1];
+    const int a = max(s.cu[seq], 0), b = min(max(s.cu[seq + 1], 0), kKvMaxLen);
     KvSpan r;
-    r.row0 = min(max(a, 0), s.n_rows);
+    r.row0 = min(a, s.n_rows);
     r.rows = min(max(min(b, s.n_rows) - r.row0, 0), s.max_rows);
     r.len = min(max(s.len[seq], 0), kKvMaxLen);
+    r.pos0 = r.len - max(b - a, 0);
     return r;
 }
 // page of a sequence's block, or -1 where the table names none

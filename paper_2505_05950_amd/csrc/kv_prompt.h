@@ -27,7 +27,7 @@ struct PromptRange {
     int start, n, chunks;
 };
 __device__ __forceinline__ PromptRange prompt_range(const KvAttnArgs& a, const KvSpan& span, int row0, int rows) {
-    const int first = span.len - span.rows + row0 / a.group, last = span.len - span.rows + min((row0 + rows - 1) / a.group, span.rows - 1);
+    const int first = span.pos0 + row0 / a.group, last = span.pos0 + min((row0 + rows - 1) / a.group, span.rows - 1);
     const int end = a.causal ? last + 1 : span.len;  // behind the last token that any row sees
     PromptRange r;
     r.start = a.window > 0 ? max(0, first - a.window + 1) & ~(kPromptTokens - 1) : 0;
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     const int start = __builtin_amdgcn_readfirstlane(range.start + chunk * a.prompt_chunk * kPromptTokens);
     const int n_tiles = __builtin_amdgcn_readfirstlane(chunk + 1 < range.chunks ? a.prompt_chunk : range.n - chunk * a.prompt_chunk);
     // ---- queries of this wave
-    const int rr = row0 + 32 * row_wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.len - span.rows + token;
+    const int rr = row0 + 32 * row_wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.pos0 + token;
     const bool there = rr < all_rows;
     const int head_q = head * a.group + (there ? rr - token * a.group : 0);
     h16x8 q[D / 16];
@@ -93,10 +93,9 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     }
     const float row_scale = fabsf(a.scale_log2) * unscale;
     // ---- tokens that the workgroup and this wave's rows see
-    const int first_key = a.window > 0 ? pos - a.window + 1 : 0, last_key = a.causal ? pos : span.len - 1;
-    const int base_pos = span.len - span.rows;
-    const int w_first = base_pos + min((row0 + 32 * row_wave) / a.group, span.rows - 1);
-    const int w_last = base_pos + min((row0 + 32 * row_wave + 31) / a.group, span.rows - 1);
+    const int first_key = a.window > 0 ? max(0, pos - a.window + 1) : 0, last_key = a.causal ? pos : span.len - 1;
+    const int w_first = span.pos0 + min((row0 + 32 * row_wave) / a.group, span.rows - 1);
+    const int w_last = span.pos0 + min((row0 + 32 * row_wave + 31) / a.group, span.rows - 1);
     // tokens that every row of the wave sees
     const int w_clear_lo = __builtin_amdgcn_readfirstlane(a.window > 0 ? w_last - a.window + 1 : 0);
     const int w_clear_hi = __builtin_amdgcn_readfirstlane(a.causal ? w_first : span.len - 1);

@@ -37,8 +37,9 @@ __device__ __forceinline__ KvUnits kv_units(const KvAttnArgs& a, int seq) {
     u.span = kv_span(a.s, seq);
     if (u.span.rows > a.most_rows) u.span.rows = 0;  // the prompt kernel's
     u.tiles = (u.span.rows * a.group + 16 * MT - 1) / (16 * MT);
-    u.lo = a.window > 0 ? max(0, u.span.len - u.span.rows - a.window + 1) & ~(kKvGroup - 1) : 0;
-    u.units = (u.span.len - u.lo + kKvGroup - 1) / kKvGroup;
+    u.lo = a.window > 0 ? max(0, u.span.pos0 - a.window + 1) & ~(kKvGroup - 1) : 0;
+    const int end = a.causal ? max(0, u.span.pos0 + u.span.rows) : u.span.len;  // behind the last token that any row sees
+    u.units = max(0, end - u.lo + kKvGroup - 1) / kKvGroup;
     return u;
 }
 // Chunks of a segment: a.chunk units each; the last of the a.chunks that the launch has takes whatever is left.
@@ -263,13 +264,13 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
         st.sum[m] = 0.0f;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) st.o[m][d] = f32x4{0, 0, 0, 0};
-        const int token = min((row0 + 16 * m + r) / a.group, w.span.rows - 1), pos = w.span.len - w.span.rows + token;
-        first_key[m] = a.window > 0 ? pos - a.window + 1 : 0;
+        const int token = min((row0 + 16 * m + r) / a.group, w.span.rows - 1), pos = w.span.pos0 + token;
+        first_key[m] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
         last_key[m] = a.causal ? pos : w.span.len - 1;
     }
     // units between these need no mask
-    const int pos0 = w.span.len - w.span.rows + row0 / a.group;
-    const int pos1 = w.span.len - w.span.rows + min((row0 + 16 * MT - 1) / a.group, w.span.rows - 1);
+    const int pos0 = w.span.pos0 + row0 / a.group;
+    const int pos1 = w.span.pos0 + min((row0 + 16 * MT - 1) / a.group, w.span.rows - 1);
     const int clear_lo = __builtin_amdgcn_readfirstlane(a.window > 0 ? pos1 - a.window + 1 : 0);
     const int clear_hi = __builtin_amdgcn_readfirstlane(a.causal ? pos0 + 1 : w.span.len);  // first token that some row does not see
     const int end = __builtin_amdgcn_readfirstlane(a.causal ? pos1 + 1 : w.span.len);       // behind the last token that any row sees
