@@ -481,6 +481,9 @@ int floe_kv_gather(const floe_kv_cache* c, const floe_kv_seqs* s, void* k_out, v
  *   keys j <= its position (causal) or all j < len[s];  with window > 0 only j > position - window
  * Query head h reads KV head h / (q_heads / kv_heads).  out[row][h] = softmax(scale q.K) V, fp32 statistics and sums, rounded once;
  * lse[row][h] (dev float, or NULL) = log of the sum of exp(scale q.K).  A row that sees no key: out 0, lse -infinity.
+ * Every token counts in the denominator and in lse, whatever the sizes of V are.  What it adds to out is a code times a fp16 weight that
+ * holds V's scale: of tokens whose weight times scale is below 2^-28 of the row's largest bits are lost, below 2^-38 all of them.  In
+ * attention, scales of V below 2^-60 (an append writes none) count as 2^-60.
  * Rows that belong to no sequence, and those of a sequence behind its first max_rows, are left as they are (n counts those too: the
  * rows before them keep their positions).
  * q dev 16-bit, q_stride elements from row to row (a multiple of 8), heads contiguous; out dev [n_rows][q_heads][head_dim]; both 16-byte

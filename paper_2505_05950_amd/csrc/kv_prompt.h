@@ -142,7 +142,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
             const size_t slot = (size_t)max(page[u], 0) * a.c.heads + head;
             const float k = gloadf(a.c.k_scale + slot), v = gloadf(a.c.v_scale + slot);
             ks[u] = page[u] < 0 ? 1.0f : k;  // (page 0 stands in for an absent one: what its scales hold is nobody's)
-            vs[u] = page[u] < 0 ? 1.0f : v;
+            vs[u] = page[u] < 0 ? 1.0f : v_scale_of(v);
         }
     };
     // Codes of V that no token of the sequence has (behind its end they are whatever the page held before, those of an absent page are
@@ -206,6 +206,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     f32x16 s[2];
     h16x8 p[4];
     float c[2], lv[2], rv[2];
+    KvSpread spread;  // of V's scales (kv_rows.h)
     // those of one unit: S^T (parts 0 and 1) or O^T (2 and 3); what is written behind a call and needs none of them goes between them
     auto products = [&](int buf, auto part_) {
         constexpr int part = decltype(part_)::value, n_here = part < 2 ? kStep : 2 * kOut;
@@ -295,7 +296,8 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
         for (int u = 0; u < 2; ++u) {
             c[u] = fmaxf(row_scale * ks[u], 0x1p-126f);  // (-infinity times it has to stay that)
             lv[u] = __builtin_amdgcn_logf(vs[u]);
-            rv[u] = __builtin_amdgcn_rcpf(vs[u]);
+            rv[u] = __builtin_amdgcn_rcpf(vs[u]) * kSumUnit;
+            spread.take(vs[u]);
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[u][j] = 0.0f;
         }
@@ -320,6 +322,35 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
         set_keep(it + 2, page_then);
         page0 = page_next[0], page1 = page_next[1];
         page_next[0] = page_then[0], page_next[1] = page_then[1];
+    }
+    if (spread.wide()) {  // the sum of weights once more, without V's scales; a wave by itself, its codes from memory
+        const float off = kSumBits - (top == -__builtin_inff() ? 0.0f : top);
+        sum = 0.0f;
+        for (int unit = 0; unit < 2 * n_tiles; ++unit) {
+            const int page = page_of(unit);
+            if (page < 0) continue;
+            const size_t slot = (size_t)page * a.c.heads + head;
+            const uint8_t* k = a.c.k + (slot * a.c.block + ((unit0 + unit) & ((1 << log_upb) - 1)) * kKvGroup + c32) * D + 8 * h;
+            f32x16 x;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] = 0.0f;
+#pragma unroll
+            for (int n = 0; n < kStep; ++n) {
+                const uint2 w = gload8(k + 16 * n);
+                x = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_h8<FMT>(w.x, w.y), q[n], x, 0, 0, 0);
+            }
+            const float k_scale = gloadf(a.c.k_scale + slot), v_scale = gloadf(a.c.v_scale + slot);
+            const bool poisoned = !(k_scale == k_scale) || !(v_scale == v_scale);
+            const float by = fmaxf(row_scale * k_scale, 0x1p-126f), from = poisoned ? __builtin_nanf("") : off;
+            const bool none = last_key < first_key;
+            const int lo = (none ? start + 2 * (unit + 2) * kKvGroup : first_key) - (start + unit * kKvGroup + 4 * h);
+            const uint32_t more = none ? 0 : last_key - first_key;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], by, from));
+                sum += (uint32_t)(8 * (j >> 2) + (j & 3) - lo) > more ? 0.0f : e;
+            }
+        }
     }
     swap32(sum, ks[0], ks[1]);
     sum = ks[0] + ks[1];

@@ -9,6 +9,13 @@
 // the result is off by beside its own: 2.2e-4 of it in all with fp16 outputs (2.1e-4 is the rounding of the output), 2.5e-4 when the
 // base is set to 2^7, which costs 1 % less time on long prompts.  Queries in bf16 are scaled per row by a power of two into fp16's range.
 //
+// The sum below the line does without V's scale, and the scales of a sequence can lie 181 powers of two apart (2^-60 is an append's least
+// one, a block of the largest bf16 values has 2^121): a token whose weight times scale binary32 no longer holds can have all of the
+// softmax.  Who has walked over scales that lie further apart than 2^80 forms its sum once more, without them and with the base that the
+// rows ended with; below that, what is lost is less than 2^-44 of a row's sum.  (A branch for it in the walk costs prompts 4 %, this 0 to
+// 1, at 192 dims 3.)  Sums are kept times 2^20, which puts the largest weight of a row between 2^-88 and 2^95, and two of them meet on one
+// base in two steps.
+//
 // S^T = K Q^T and O^T = V^T P^T, both as v_mfma_f32_16x16x32_f16: a column is a query row, so its maximum and sum live in the four
 // lanes that hold the column, and the rows of S^T that a lane holds (tokens 4 g + i of two tiles) are exactly the operand of the
 // second product when V is stored in that order: the weights never leave their lane.
@@ -25,6 +32,20 @@ namespace floe {
 
 constexpr int kRowsWaves = 4;
 constexpr float kBaseBits = 14.0f, kTopBits = 15.0f;  // a row's largest weight is 2^14 when its base is set, and may grow to 2^15
+constexpr float kSumBits = 20.0f, kSumUnit = 0x1p20f;  // sums of weights are kept times 2^20
+
+// V's scale as the attention uses it: an append writes no smaller one, and 0 (of an array that was filled in another way) has no logarithm.
+__device__ __forceinline__ float v_scale_of(float scale) { return scale < kKvFloor ? kKvFloor : scale; }  // (a NaN stays one)
+// The least and the largest scale of V that a wave has walked over, as bits in scalar registers (they are positive; a NaN is a large one).
+struct KvSpread {
+    int least = 0x7f800000, most = 0;
+    __device__ __forceinline__ void take(float scale) {
+        const int bits = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, scale));
+        least = min(least, bits);
+        most = max(most, bits);
+    }
+    __device__ __forceinline__ bool wide() const { return most - least > 80 << 23; }
+};
 
 // Units of one sequence: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on for each.
 struct KvUnits {
@@ -60,7 +81,7 @@ struct KvFrag {  // one unit in registers
     float ks, vs;
 };
 
-template <int D, int FMT>
+template <int D, int FMT, bool WITH_V = true>
 __device__ __forceinline__ void load_unit(KvFrag<D, FMT>& f, const KvCache& c, int head, int page, int token_in_page, int r, int g) {
     const size_t slot = (size_t)max(page, 0) * c.heads + head;
     const size_t base = (slot * c.block + token_in_page) * D;  // the same in every lane
@@ -70,8 +91,10 @@ __device__ __forceinline__ void load_unit(KvFrag<D, FMT>& f, const KvCache& c, i
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int kk = 0; kk < D / 64; ++kk) f.k[t * (D / 64) + kk] = gload16(k + (k_lane + t * 16 * D + kk * 64));
+    if constexpr (WITH_V) {
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) f.v[dt] = gload16_once(v + (v_lane + dt * 1024));
+        for (int dt = 0; dt < D / 32; ++dt) f.v[dt] = gload16_once(v + (v_lane + dt * 1024));
+    }
     f.ks = gloadf(c.k_scale + slot);
     f.vs = gloadf(c.v_scale + slot);
 }
@@ -144,12 +167,12 @@ template <int D, int MT>
 struct KvState {
     f32x4 o[MT][D / 16];  // O^T: tile dt, parity e: dims 32 dt + 8 g + 2 i + e in o[2 dt + e][i]
     float top[MT], sum[MT];
+    KvSpread spread;
 };
 
+// S^T of a unit: row r of tile m in s[m][t][i], token 16 t + 4 g + i
 template <int D, int FMT, int MT>
-__device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D, MT>& Q, const KvFrag<D, FMT>& f, const KvAttnArgs& a,
-                                          bool mask, int token0, int len, const int* first_key, const int* last_key, int g) {
-    f32x4 s[MT][2];
+__device__ __forceinline__ void unit_scores(f32x4 (&s)[MT][2], const KvQueries<D, MT>& Q, const KvFrag<D, FMT>& f) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) s[m][0] = s[m][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -164,7 +187,22 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
                 s[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, Q.q[m][2 * kk + 1], s[m][t], 0, 0, 0);
             }
         }
-    const float lv = __builtin_amdgcn_logf(f.vs), rv = __builtin_amdgcn_rcpf(f.vs);
+}
+__device__ __forceinline__ void mask_unit(float (&x)[8], int token0, int first_key, int last_key, int g) {
+    const bool none = last_key < first_key;
+    const int lo = (none ? token0 + 2 * kKvGroup : first_key) - (token0 + 4 * g);  // keys from here on, up to `more` behind, are seen
+    const uint32_t more = none ? 0 : last_key - first_key;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (uint32_t)(16 * (j >> 2) + (j & 3) - lo) > more ? -__builtin_inff() : x[j];
+}
+
+template <int D, int FMT, int MT>
+__device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D, MT>& Q, const KvFrag<D, FMT>& f, const KvAttnArgs& a,
+                                          bool mask, int token0, int len, const int* first_key, const int* last_key, int g) {
+    f32x4 s[MT][2];
+    unit_scores<D, FMT, MT>(s, Q, f);
+    const float vs = v_scale_of(f.vs), lv = __builtin_amdgcn_logf(vs), rv = __builtin_amdgcn_rcpf(vs) * kSumUnit;
+    st.spread.take(vs);
     h16x8 p[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -172,13 +210,7 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
         float x[8], mx = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(s[m][j >> 2][j & 3], c, lv);
-        if (mask) {
-            const bool none = last_key[m] < first_key[m];
-            const int lo = (none ? token0 + 2 * kKvGroup : first_key[m]) - (token0 + 4 * g);  // keys from here on, up to `more` behind, are seen
-            const uint32_t more = none ? 0 : last_key[m] - first_key[m];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = (uint32_t)(16 * (j >> 2) + (j & 3) - lo) > more ? -__builtin_inff() : x[j];
-        }
+        if (mask) mask_unit(x, token0, first_key[m], last_key[m], g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) mx = fmaxf(mx, x[j]);
         mx = quad_max(mx);
@@ -229,17 +261,39 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
     }
 }
 
+// A unit's weights, summed without V's scale
+template <int D, int FMT, int MT>
+__device__ __forceinline__ void sum_unit(KvState<D, MT>& st, const KvQueries<D, MT>& Q, const KvFrag<D, FMT>& f, const KvAttnArgs& a, int token0,
+                                         const int* first_key, const int* last_key, int g) {
+    f32x4 s[MT][2];
+    unit_scores<D, FMT, MT>(s, Q, f);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const float c = a.scale_log2 * Q.unscale[m] * f.ks;
+        const float off = kSumBits - (st.top[m] == -__builtin_inff() ? 0.0f : st.top[m]) + (f.vs == f.vs ? 0.0f : f.vs);
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(s[m][j >> 2][j & 3], c, off);
+        mask_unit(x, token0, first_key[m], last_key[m], g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) st.sum[m] += __builtin_amdgcn_exp2f(x[j]);
+    }
+}
+
 __device__ __forceinline__ float weight_of(float top, float all) { return top == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - all); }
+
+// The same in two steps, for sums of weights: what a sum is multiplied with can be less than binary32 holds.
+__device__ __forceinline__ float half_weight_of(float top, float all) { return top == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(0.5f * (top - all)); }
 
 // four dims of a finished row
 __device__ __forceinline__ void write_row4(const KvAttnArgs& a, int D, size_t row, int head, int d, f32x4 o, float top, float sum) {
-    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float f = sum == 0.0f ? 0.0f : kSumUnit / sum;
     uint2 w;
     if (a.bf16) w = make_uint2(pack16<true>(o[0] * f, o[1] * f), pack16<true>(o[2] * f, o[3] * f));
     else w = make_uint2(pack16<false>(o[0] * f, o[1] * f), pack16<false>(o[2] * f, o[3] * f));
     *reinterpret_cast<uint2*>(a.out + (row * a.q_heads + head) * D + d) = w;
     if (a.lse && d == 0)
-        a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+        a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + (__builtin_amdgcn_logf(sum) - kSumBits)) * 0.6931471805599453f;
 }
 
 template <int D, int FMT, int MT>
@@ -305,6 +359,18 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
             step(it, f0, p0, f1, p1);
             step(it + 1, f1, p1, f0, p0);
         }
+        if (st.spread.wide()) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) st.sum[m] = 0.0f;
+            for (int it = 0; it < n; ++it) {
+                const int j = j0 + wave + NW * it;
+                if ((it & 63) == 0) fetch_pages(j);
+                const int page = w.lo + j * kKvGroup >= end ? -1 : page_of(it);
+                if (page < 0) continue;
+                load_unit<D, FMT, false>(f0, a.c, head, page, ((unit0 + j) & ((1 << log_upb) - 1)) * kKvGroup, r, g);
+                sum_unit<D, FMT, MT>(st, Q, f0, a, w.lo + j * kKvGroup, first_key, last_key, g);
+            }
+        }
     }
     // ---- the four waves meet
     const bool whole = n_chunks == 1;
@@ -342,7 +408,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
             for (int k = 0; k < NW; ++k) top = fmaxf(top, ml[k][16 * m + row][0]);
 #pragma unroll
             for (int k = 0; k < NW; ++k) {
-                l += ml[k][16 * m + row][1] * weight_of(ml[k][16 * m + row][0], top);
+                const float w = half_weight_of(ml[k][16 * m + row][0], top);
+                l += ml[k][16 * m + row][1] * w * w;
                 o += *reinterpret_cast<const f32x4*>(&slab[k][row][d]);
             }
             if (whole) {
@@ -372,9 +439,9 @@ __device__ __forceinline__ void join_row(const KvAttnArgs& a, const KvParts& par
             const size_t at = first + (size_t)c * step;
             const float t = parts.ml[2 * at], s = parts.ml[2 * at + 1];
             const f32x4 x = *reinterpret_cast<const f32x4*>(parts.o + at * D + 4 * lane);
-            const float m = fmaxf(top, t), f0 = weight_of(top, m), f1 = weight_of(t, m);
-            o = o * f0 + x * f1;
-            l = l * f0 + s * f1;
+            const float m = fmaxf(top, t), h0 = half_weight_of(top, m), h1 = half_weight_of(t, m);
+            o = o * (h0 * h0) + x * (h1 * h1);
+            l = l * h0 * h0 + s * h1 * h1;
             top = m;
         }
         so[side][lane] = o;
@@ -384,9 +451,9 @@ __device__ __forceinline__ void join_row(const KvAttnArgs& a, const KvParts& par
     if (side != 0) return;
 #pragma unroll
     for (int i = 1; i < kSide; ++i) {
-        const float m = fmaxf(top, sm[i]), f0 = weight_of(top, m), f1 = weight_of(sm[i], m);
-        o = o * f0 + so[i][lane] * f1;
-        l = l * f0 + sl[i] * f1;
+        const float m = fmaxf(top, sm[i]), h0 = half_weight_of(top, m), h1 = half_weight_of(sm[i], m);
+        o = o * (h0 * h0) + so[i][lane] * (h1 * h1);
+        l = l * h0 * h0 + sl[i] * h1 * h1;
         top = m;
     }
     write_row4(a, D, row, head, 4 * lane, o, top, l);
