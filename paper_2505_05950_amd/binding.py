@@ -1,5 +1,8 @@
 """ctypes binding of include/floe.h.  Argument marshalling only: torch owns device memory and streams,
-the functions below pass raw pointers and sizes to the C ABI under the same names."""
+the functions below pass raw pointers and sizes to the C ABI under the same names.
+
+A call runs on the current stream, or on `stream`: what it allocates then belongs to that stream, and the caller orders the stream
+behind those that make its inputs, and before those that use its results or take its inputs' memory back."""
 from __future__ import annotations
 
 import ctypes as C
@@ -195,6 +198,15 @@ def _stream(stream):
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
+# What a call makes for the caller or for itself comes from the pool of the stream that it runs on: a block of another stream's pool may
+# still be in use there, and would be given out again there while this call writes it.
+def _empty(shape, dtype, device, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _check(rc: int, where: str):
     if rc != 0:
         raise FloeError(rc, where)
@@ -224,9 +236,8 @@ def floe_quantize_expert(w_up_cm: torch.Tensor, bits: int, group: int, stream=No
     """w_up_cm fp16 [f][d] on the GPU -> (codes int32-viewed-uint32 [f][d*bits/32], scale fp16, zero fp16)."""
     f, d = w_up_cm.shape
     dev = w_up_cm.device
-    codes = torch.empty((f, max(1, d * bits // 32)), dtype=torch.int32, device=dev)
-    scale = torch.empty((f, max(1, d // group)), dtype=torch.float16, device=dev)
-    zero = torch.empty_like(scale)
+    codes = _empty((f, max(1, d * bits // 32)), torch.int32, dev, stream)
+    scale, zero = (_empty((f, max(1, d // group)), torch.float16, dev, stream) for _ in range(2))
     s = _shape(d, f, bits, group)
     _check(load().floe_quantize_expert(C.byref(s), _ptr(w_up_cm), _ptr(codes), _ptr(scale), _ptr(zero), _stream(stream)),
            "floe_quantize_expert")
@@ -236,17 +247,25 @@ def floe_quantize_expert(w_up_cm: torch.Tensor, bits: int, group: int, stream=No
 def floe_up_gemv(codes, scale, zero, x, d, bits, group, stream=None) -> torch.Tensor:
     f = codes.shape[0]
     T = x.shape[0]
-    v = torch.empty((T, f), dtype=torch.float32, device=x.device)
+    v = _empty((T, f), torch.float32, x.device, stream)
     s = _shape(d, f, bits, group)
     _check(load().floe_up_gemv(C.byref(s), _ptr(codes), _ptr(scale), _ptr(zero), _ptr(x), T, _ptr(v), _stream(stream)),
            "floe_up_gemv")
     return v
 
 
+def _list(shape, device, stream):
+    """Channel lists, -1 where the call writes none; filled on the stream that the call runs on."""
+    if stream is None:
+        return torch.full(shape, -1, dtype=torch.int32, device=device)
+    with torch.cuda.stream(stream):
+        return torch.full(shape, -1, dtype=torch.int32, device=device)
+
+
 def floe_select_channels(v: torch.Tensor, tau: torch.Tensor, stream=None):
     T, f = v.shape
-    idx = torch.full((T, f), -1, dtype=torch.int32, device=v.device)
-    count = torch.empty((T,), dtype=torch.int32, device=v.device)
+    idx = _list((T, f), v.device, stream)
+    count = _empty((T,), torch.int32, v.device, stream)
     _check(load().floe_select_channels(_ptr(v), f, T, _ptr(tau), _ptr(idx), _ptr(count), _stream(stream)),
            "floe_select_channels")
     return idx, count
@@ -257,8 +276,8 @@ def floe_expert_workspace_bytes(d, f, bits, group, T) -> int:
     return int(load().floe_expert_workspace_bytes(C.byref(s), int(T)))
 
 
-def _workspace(nbytes: int, device) -> torch.Tensor:
-    return torch.empty((max(nbytes, 256) + 256,), dtype=torch.uint8, device=device)
+def _workspace(nbytes: int, device, stream=None) -> torch.Tensor:
+    return _empty((max(nbytes, 256) + 256,), torch.uint8, device, stream)
 
 
 def _aligned_ptr(ws: torch.Tensor):
@@ -270,7 +289,7 @@ def _aligned_ptr(ws: torch.Tensor):
 def floe_gate_down_sparse(e: Expert, x, v, idx, count, out_scale, y_acc, workspace=None, stream=None):
     T = x.shape[0]
     if workspace is None:
-        workspace = _workspace(floe_expert_workspace_bytes(e.d, e.f, e.bits, e.group, T), x.device)
+        workspace = _workspace(floe_expert_workspace_bytes(e.d, e.f, e.bits, e.group, T), x.device, stream)
     wp, wn = _aligned_ptr(workspace)
     es = e.c_struct()
     _check(load().floe_gate_down_sparse(C.byref(es), _ptr(x), T, _ptr(v), _ptr(idx), _ptr(count), _ptr(out_scale),
@@ -286,13 +305,13 @@ def floe_expert_ffn_sparse(e: Expert, x, tau, out_scale, y_acc, idx=None, count=
     if want_list:
         if idx is None:  # a list of our own: the call that writes it also sets what lies behind its end
             call = load().floe_expert_ffn_sparse_padded
-            idx = torch.empty(T, e.f, dtype=torch.int32, device=x.device)
+            idx = _empty((T, e.f), torch.int32, x.device, stream)
         if count is None:
-            count = torch.empty(T, dtype=torch.int32, device=x.device)
+            count = _empty((T,), torch.int32, x.device, stream)
     else:
         idx = count = None
     if workspace is None:
-        workspace = _workspace(floe_expert_workspace_bytes(e.d, e.f, e.bits, e.group, T), x.device)
+        workspace = _workspace(floe_expert_workspace_bytes(e.d, e.f, e.bits, e.group, T), x.device, stream)
     wp, wn = _aligned_ptr(workspace)
     es = e.c_struct()
     _check(call(C.byref(es), _ptr(x), T, _ptr(tau), _ptr(out_scale), _ptr(y_acc), _ptr(idx), _ptr(count), wp, wn,
@@ -306,11 +325,11 @@ SPARSIFY_UP, SPARSIFY_GATE, SPARSIFY_DOWN = 0, 1, 2
 def floe_expert_ffn_sparsified(e: Expert, which: int, x, tau, out_scale, y_acc, workspace=None, stream=None):
     """Eq. 1 with the sparsity function on a_up / a_gate / a_down (Sec. 3.2.1); returns (y_acc, idx, count)."""
     T = x.shape[0]
-    idx = torch.full((T, e.f), -1, dtype=torch.int32, device=x.device)
-    count = torch.empty((T,), dtype=torch.int32, device=x.device)
+    idx = _list((T, e.f), x.device, stream)
+    count = _empty((T,), torch.int32, x.device, stream)
     if workspace is None:
         s = _shape(e.d, e.f, e.bits, e.group)
-        workspace = _workspace(int(load().floe_expert_sparsified_workspace_bytes(C.byref(s), T)), x.device)
+        workspace = _workspace(int(load().floe_expert_sparsified_workspace_bytes(C.byref(s), T)), x.device, stream)
     wp, wn = _aligned_ptr(workspace)
     es = e.c_struct()
     _check(load().floe_expert_ffn_sparsified(C.byref(es), int(which), _ptr(x), T, _ptr(tau), _ptr(out_scale), _ptr(y_acc),
@@ -337,7 +356,7 @@ class Layer:
                          self.tau_stride, None, int(gd_on_host))
         self.gd_on_host = bool(gd_on_host)
         nbytes = floe_layer_table_bytes(self)
-        self.table = torch.empty((nbytes + 256,), dtype=torch.uint8, device=tau.device)
+        self.table = _empty((nbytes + 256,), torch.uint8, tau.device, stream)
         tp, tn = _aligned_ptr(self.table)
         floe_layer_build_table(self, tp, tn, stream)
         self._c.dev_table = tp
@@ -353,9 +372,9 @@ class Layer:
         """A workspace of its own (e.g. for a prefetch that runs beside a decode call)."""
         return _workspace(floe_layer_workspace_bytes(self, T), self.tau.device)
 
-    def workspace(self, T: int) -> torch.Tensor:
+    def workspace(self, T: int, stream=None) -> torch.Tensor:
         if T not in self._ws:
-            self._ws[T] = _workspace(floe_layer_workspace_bytes(self, T), self.tau.device)
+            self._ws[T] = _workspace(floe_layer_workspace_bytes(self, T), self.tau.device, stream)
         return self._ws[T]
 
 
@@ -376,9 +395,9 @@ def floe_moe_layer_decode(L: Layer, x: torch.Tensor, y: torch.Tensor = None, sta
     """x fp16 [T][d] -> y fp16 [T][d]; stats (optional) int32 [T][slots][4] viewed as floe_slot_stat."""
     T = x.shape[0]
     if y is None:
-        y = torch.empty(T, L.d, dtype=torch.float16, device=x.device)
+        y = _empty((T, L.d), torch.float16, x.device, stream)
     if workspace is None:
-        workspace = L.workspace(T)
+        workspace = L.workspace(T, stream)
     wp, wn = _aligned_ptr(workspace)
     _check(load().floe_moe_layer_decode(C.byref(L._c), _ptr(x), T, _ptr(y), _ptr(stats), wp, wn, _stream(stream)),
            "floe_moe_layer_decode")
@@ -400,9 +419,9 @@ def floe_moe_layer_decode_offloaded(L: Layer, x, staging, capacity_rows, side_st
     """Offloaded layer: experts' gd are pinned host tensors; staging dev [T*slots][capacity_rows][2][d]."""
     T = x.shape[0]
     if y is None:
-        y = torch.empty(T, L.d, dtype=torch.float16, device=x.device)
+        y = _empty((T, L.d), torch.float16, x.device, stream)
     if workspace is None:
-        workspace = L.workspace(T)
+        workspace = L.workspace(T, stream)
     wp, wn = _aligned_ptr(workspace)
     cur = stream if stream is not None else torch.cuda.current_stream()
     # torch creates the hipEvent_t lazily on the first record(); the library records both again
@@ -467,9 +486,9 @@ def floe_moe_layer_decode_prefetched(L: Layer, P: Prefetch, M: MissPath, x, y=No
     """Layer decode on staging rows that floe_moe_layer_prefetch has (partly) filled; only the misses are copied now."""
     T = x.shape[0]
     if y is None:
-        y = torch.empty(T, L.d, dtype=torch.float16, device=x.device)
+        y = _empty((T, L.d), torch.float16, x.device, stream)
     if workspace is None:
-        workspace = L.workspace(T)
+        workspace = L.workspace(T, stream)
     wp, wn = _aligned_ptr(workspace)
     _check(load().floe_moe_layer_decode_prefetched(C.byref(L._c), C.byref(P._c), C.byref(M._c), _ptr(x), T, _ptr(y),
                                                    _ptr(stats), _ptr(prefetch_stats), wp, wn, _stream(stream)),
@@ -498,9 +517,9 @@ def floe_moe_layer_decode_cached(L: Layer, cache: ChannelCache, M: MissPath, x, 
                                  workspace=None, stream=None):
     T = x.shape[0]
     if y is None:
-        y = torch.empty(T, L.d, dtype=torch.float16, device=x.device)
+        y = _empty((T, L.d), torch.float16, x.device, stream)
     if workspace is None:
-        workspace = L.workspace(T)
+        workspace = L.workspace(T, stream)
     wp, wn = _aligned_ptr(workspace)
     _check(load().floe_moe_layer_decode_cached(C.byref(L._c), C.byref(cache._c), C.byref(M._c), _ptr(x), T, _ptr(y),
                                                _ptr(stats), _ptr(cache_stats), wp, wn, _stream(stream)),
@@ -557,12 +576,13 @@ class KVCache:
         self._at = C.addressof(self._c)
         self._ws = {}
 
-    def workspace(self, nbytes: int, stream: int):
+    def workspace(self, nbytes: int, stream: int, pool=None):
         """(address, bytes) of scratch for the attention calls on a stream: an array per stream, since the calls on one are ordered.
-        An array that was too small stays (a captured graph may hold its address); each is twice the one before or more."""
+        An array that was too small stays (a captured graph may hold its address); each is twice the one before or more.  pool: the
+        stream as an object, where it is not the current one."""
         ws = self._ws.get(stream)
         if ws is None or ws[2] < nbytes:
-            array = _workspace(max(nbytes, 2 * ws[2]) if ws else nbytes, self.k.device)
+            array = _workspace(max(nbytes, 2 * ws[2]) if ws else nbytes, self.k.device, pool)
             ws = self._ws[stream] = (array, *_aligned_ptr(array), ws)
         return ws[1], ws[2]
 
@@ -582,7 +602,7 @@ class Rope:
 
 
 def floe_rope_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
-    table = torch.empty((int(n_positions), int(rot_dim) // 2, 2), dtype=torch.float32, device=device)
+    table = _empty((int(n_positions), int(rot_dim) // 2, 2), torch.float32, device, stream)
     _check(load().floe_rope_table(_ptr(table), int(n_positions), int(rot_dim), float(base), _stream(stream)), "floe_rope_table")
     return table
 
@@ -643,9 +663,11 @@ def _kv_rows(t, cache: KVCache, heads, n_rows, name: str):
     return stride[0] if n_rows > 1 else heads * D
 
 
-def _kv_out(t, cache, shape, dtype, like, name):
+def _kv_out(t, cache, shape, dtype, like, name, stream):
     """An output tensor: the caller's, if it fits, or a new one beside `like` (which saves 1 us where it has the same form)."""
     if t is None:
+        if stream is not None:
+            return _empty(shape, dtype, like.device, stream)
         if like.dtype is dtype and like.shape == shape and like.is_contiguous():
             return torch.empty_like(like)
         return like.new_empty(shape, dtype=dtype)
@@ -665,7 +687,7 @@ def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows:
         shape = q.shape
         heads = shape[1] if len(shape) == 3 else 0
         qs, q_at = _kv_rows(q, cache, heads, n_rows, "q"), q.data_ptr()
-        q_out = _kv_out(q_out, cache, shape, cache.dtype, q, "q_out")
+        q_out = _kv_out(q_out, cache, shape, cache.dtype, q, "q_out", stream)
         q_out_at = q_out.data_ptr()
     if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n_rows,) or not positions.is_contiguous()
                                   or positions.get_device() != cache._device):
@@ -682,8 +704,8 @@ def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows:
 def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max_rows: int, k_out=None, v_out=None, stream=None):
     """Rows cu_rows[s] .. cu_rows[s + 1) are tokens first[s], first[s] + 1, ... of sequence s: (k, v) 16-bit [n_rows][kv_heads][head_dim]."""
     shape = (n_rows, cache.kv_heads, cache.head_dim)
-    k_out = _kv_out(k_out, cache, shape, cache.dtype, cache.k, "k_out")
-    v_out = _kv_out(v_out, cache, shape, cache.dtype, k_out, "v_out")
+    k_out = _kv_out(k_out, cache, shape, cache.dtype, cache.k, "k_out", stream)
+    v_out = _kv_out(v_out, cache, shape, cache.dtype, k_out, "v_out", stream)
     rc = _kv_calls()[1](cache._at, _kv_seqs(cache, cu_rows, first, block_table, n_rows, max_rows), k_out.data_ptr(), v_out.data_ptr(), _stream(stream))
     if rc:
         _check(rc, "floe_kv_gather")
@@ -698,24 +720,20 @@ def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows:
     shape = q.shape
     n_rows, heads = shape[0], shape[1] if len(shape) == 3 else 0
     qs = _kv_rows(q, cache, heads, n_rows, "q")
-    out = _kv_out(out, cache, shape, cache.dtype, q, "out")
+    out = _kv_out(out, cache, shape, cache.dtype, q, "out", stream)
     if want_lse or lse is not None:
-        lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, q, "lse")
+        lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, q, "lse", stream)
     call, need = _kv_calls()[2:]
     s = _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows)
     a = _ATTENTION_FIELDS.pack(heads, causal, window, max_len, cache.head_dim ** -0.5 if scale is None else scale)
     if workspace is not None and workspace.get_device() != cache._device:
         raise ValueError(f"workspace: on {workspace.device}, the cache is on {cache.k.device}")
     st = _stream(stream)
-    at, size = cache.workspace(256, st) if workspace is None else _aligned_ptr(workspace)
+    at, size = cache.workspace(256, st, stream) if workspace is None else _aligned_ptr(workspace)
     args = cache._at, s, a, q.data_ptr(), qs, out.data_ptr(), None if lse is None else lse.data_ptr()
     rc = call(*args, at, size, st)
     if rc == -4 and workspace is None:  # refused before anything is enqueued: the cache's workspace has to grow
-        if stream is None:
-            at, size = cache.workspace(need(cache._at, s, a), st)
-        else:
-            with torch.cuda.stream(stream):
-                at, size = cache.workspace(need(cache._at, s, a), st)
+        at, size = cache.workspace(need(cache._at, s, a), st, stream)
         rc = call(*args, at, size, st)
     if rc:
         _check(rc, "floe_kv_attention")
