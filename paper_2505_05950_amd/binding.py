@@ -601,8 +601,18 @@ class Rope:
                                  self.interleaved)
 
 
+def _launches_on(device: int, stream, what: str):
+    """The library launches on the current device, and a stream is one device's: both have to be the one that the memory is on."""
+    if device < 0:
+        raise ValueError(f"{what} is not on a GPU")
+    if device != _current_device() or (stream is not None and stream.device_index != device):
+        on = f"cuda:{_current_device()}" + ("" if stream is None else f", the stream of cuda:{stream.device_index}")
+        raise ValueError(f"{what} is on cuda:{device}, the current device is {on}: call it under torch.cuda.device({device})")
+
+
 def floe_rope_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
     table = _empty((int(n_positions), int(rot_dim) // 2, 2), torch.float32, device, stream)
+    _launches_on(table.get_device(), stream, "floe_rope_table: the table")
     _check(load().floe_rope_table(_ptr(table), int(n_positions), int(rot_dim), float(base), _stream(stream)), "floe_rope_table")
     return table
 
@@ -628,7 +638,7 @@ def _kv_calls():
     return _kv_functions
 
 
-def _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows) -> bytes:
+def _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows, stream=None) -> bytes:
     device, n, i32 = cache._device, cu_rows.shape[0] - 1, torch.int32
     shape = block_table.shape
     if not (cu_rows.dtype is i32 and length.dtype is i32 and block_table.dtype is i32 and cu_rows.is_contiguous() and length.is_contiguous()
@@ -638,6 +648,7 @@ def _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows) -> bytes:
         raise ValueError(f"{n} sequences in cu_rows, {tuple(length.shape)} lengths, block_table {tuple(shape)}")
     if cu_rows.get_device() != device or length.get_device() != device or block_table.get_device() != device or device < 0:
         raise ValueError("cu_rows, lengths and block_table are on the cache's GPU")
+    _launches_on(device, stream, "the cache")
     return _SEQS_FIELDS.pack(n, n_rows, max_rows, shape[1], cu_rows.data_ptr(), length.data_ptr(), block_table.data_ptr())
 
 
@@ -694,7 +705,7 @@ def floe_kv_append(cache: KVCache, k, v, cu_rows, length, block_table, max_rows:
         raise ValueError(f"positions: expected contiguous int32 [{n_rows}] on {cache.k.device}")
     if rope is not None and rope.table.get_device() != cache._device:
         raise ValueError(f"rope: its table is on {rope.table.device}, the cache on {cache.k.device}")
-    rc = _kv_calls()[0](cache._at, _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows), k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs,
+    rc = _kv_calls()[0](cache._at, _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows, stream), k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs,
                         heads, q_out_at, None if rope is None else rope._packed(positions), _stream(stream))
     if rc:
         _check(rc, "floe_kv_append")
@@ -706,7 +717,7 @@ def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max
     shape = (n_rows, cache.kv_heads, cache.head_dim)
     k_out = _kv_out(k_out, cache, shape, cache.dtype, cache.k, "k_out", stream)
     v_out = _kv_out(v_out, cache, shape, cache.dtype, k_out, "v_out", stream)
-    rc = _kv_calls()[1](cache._at, _kv_seqs(cache, cu_rows, first, block_table, n_rows, max_rows), k_out.data_ptr(), v_out.data_ptr(), _stream(stream))
+    rc = _kv_calls()[1](cache._at, _kv_seqs(cache, cu_rows, first, block_table, n_rows, max_rows, stream), k_out.data_ptr(), v_out.data_ptr(), _stream(stream))
     if rc:
         _check(rc, "floe_kv_gather")
     return k_out, v_out
@@ -724,7 +735,7 @@ def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows:
     if want_lse or lse is not None:
         lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, q, "lse", stream)
     call, need = _kv_calls()[2:]
-    s = _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows)
+    s = _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows, stream)
     a = _ATTENTION_FIELDS.pack(heads, causal, window, max_len, cache.head_dim ** -0.5 if scale is None else scale)
     if workspace is not None and workspace.get_device() != cache._device:
         raise ValueError(f"workspace: on {workspace.device}, the cache is on {cache.k.device}")

@@ -142,3 +142,49 @@ def test_a_workspace_that_was_outgrown_stays_for_the_graphs_that_hold_its_addres
     larger, more = c.workspace(size + 1, 7)
     assert larger != at and more >= 2 * size and c.workspace(256, 7) == (larger, more)
     assert small() is not None and small().data_ptr() <= at
+
+
+class _On:
+    """What the checks of a call's index arrays look at, of a tensor on any device."""
+    dtype = torch.int32
+
+    def __init__(self, device, *shape):
+        self.device, self.shape = device, shape
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return int(torch.Size(self.shape).numel())
+
+    def data_ptr(self):
+        return P
+
+
+class _OnStream:
+    def __init__(self, device):
+        self.device_index = device
+
+
+def test_a_cache_on_another_device_than_the_one_that_launches_is_refused(monkeypatch):
+    c = F.KVCache(2, 2, 64, 32, device="cpu")
+    c._device = 1
+    arrays = _On(1, 3), _On(1, 2), _On(1, 2, 4)
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    for stream in (None, _OnStream(0), _OnStream(1)):
+        with pytest.raises(ValueError, match="cuda:1"):
+            B._kv_seqs(c, *arrays, 3, 3, stream)
+    monkeypatch.setattr(B, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="cuda:0"):
+        B._kv_seqs(c, *arrays, 3, 3, _OnStream(0))
+    assert B._kv_seqs(c, *arrays, 3, 3) == B._kv_seqs(c, *arrays, 3, 3, _OnStream(1))
+
+
+def test_a_table_of_the_host_is_refused_before_a_kernel_writes_it(monkeypatch):
+    with pytest.raises(ValueError, match="GPU"):
+        F.floe_rope_table(4, 64, device="cpu")
+    with pytest.raises(ValueError, match="GPU"):
+        F.floe_rope_table(4, 64, device="meta")
