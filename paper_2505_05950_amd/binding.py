@@ -281,9 +281,11 @@ def _workspace(nbytes: int, device, stream=None) -> torch.Tensor:
 
 
 def _aligned_ptr(ws: torch.Tensor):
+    if not ws.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor, got strides {ws.stride()}")
     base = ws.data_ptr()
     off = (-base) % 256
-    return base + off, ws.numel() - off
+    return base + off, max(0, ws.numel() - off)
 
 
 def floe_gate_down_sparse(e: Expert, x, v, idx, count, out_scale, y_acc, workspace=None, stream=None):

@@ -188,3 +188,16 @@ def test_a_table_of_the_host_is_refused_before_a_kernel_writes_it(monkeypatch):
         F.floe_rope_table(4, 64, device="cpu")
     with pytest.raises(ValueError, match="GPU"):
         F.floe_rope_table(4, 64, device="meta")
+
+
+def test_a_workspace_is_never_larger_than_its_tensor():
+    """A view that ends before its first aligned byte holds nothing (as an unsigned size, less than nothing would be everything)."""
+    whole = torch.empty(1024, dtype=torch.uint8)
+    at = (-whole.data_ptr()) % 256  # first aligned byte
+    for lo, hi in ((at + 1, at + 1), (at + 1, at + 100), (at + 1, at + 256), (at + 1, at + 300), (at, at), (at, at + 300)):
+        ws = whole[lo:hi]
+        start, size = B._aligned_ptr(ws)
+        assert size == max(0, whole.data_ptr() + hi - start) and start % 256 == 0
+    for ws in (whole[::2], whole[:1].expand(1 << 20), whole.view(32, 32).t()):
+        with pytest.raises(ValueError):
+            B._aligned_ptr(ws)
