@@ -46,9 +46,11 @@ int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_at
     if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0) return FLOE_EINVAL;
     if (a->q_heads % c->kv_heads != 0) return FLOE_ESHAPE;
     if (a->q_heads > 1024 || a->window > kKvMaxLen) return FLOE_EUNSUPPORTED;
-    // (the widest grid that has to do: a workgroup per 128 query rows of a KV head, or per row where there are few)
+    // (the widest grid that has to do, in workgroups of 256 threads: the prompt kernel has two threads per query row of a KV head, at 256
+    // dims four; the rows kernel has up to four workgroups)
     const KvSeqs k = dev_seqs(s);
-    if (((int64_t)k.max_rows * (a->q_heads / c->kv_heads) / 128 + 4) * k.n_seqs * c->kv_heads > kMaxGrid) return FLOE_EUNSUPPORTED;
+    const int64_t rows = (int64_t)k.max_rows * (a->q_heads / c->kv_heads);
+    if ((rows / (128 / kv_prompt_split(c->head_dim)) + 4) * k.n_seqs * c->kv_heads > kMaxGrid) return FLOE_EUNSUPPORTED;
     if ((int64_t)k.max_rows * a->q_heads > 0x7fffffff) return FLOE_EUNSUPPORTED;
     return FLOE_OK;
 }
@@ -99,7 +101,6 @@ void cut_prompts(AttnPlan& w, int dim, int64_t heads, int64_t rows, int64_t tile
     for (int half = 0; half < (dim == 64 ? 1 : 2); ++half) {
         const PromptCost t = prompt_cost(dim, half);
         const int64_t tile_rows = kv_prompt_rows(dim, t.waves), row_tiles = (rows + tile_rows - 1) / tile_rows, segments = heads * row_tiles;
-        if (half && segments > kMaxGrid) break;
         const int64_t cus = num_cus(), slots = cus * t.slots;
         for (int64_t c = 1; c <= 32 && c <= tiles && (c == 1 || segments * c <= 8 * slots); ++c) {
             const int64_t groups = segments * c, rounds = (groups + slots - 1) / slots;

@@ -201,3 +201,12 @@ def test_a_workspace_is_never_larger_than_its_tensor():
     for ws in (whole[::2], whole[:1].expand(1 << 20), whole.view(32, 32).t()):
         with pytest.raises(ValueError):
             B._aligned_ptr(ws)
+
+
+def test_attention_refuses_batches_whose_workgroups_no_launch_holds(lib):
+    def need(dim, max_rows, n_seqs=128):
+        return lib.floe_kv_attention_workspace_bytes(cache(kv_heads=32, head_dim=dim), seqs(n_seqs=n_seqs, n_rows=1 << 14, max_rows=max_rows),
+                                                     attn(q_heads=1024))
+    # 32 rows per token and KV head, 4096 sequences x heads; 2^32 threads are too many: at 256 dims a row has four, else two
+    assert need(256, 8192) == 0 and need(256, 8180) > 0
+    assert need(128, 16384) == 0 and need(128, 16300) > 0 and need(192, 8192) > 0 and need(64, 8192) > 0
