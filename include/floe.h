@@ -451,7 +451,7 @@ typedef struct {
     const int32_t* positions;
     int32_t n_positions, rot_dim, interleaved;
 } floe_rope;
-/* table[p][i] = (cos, sin) of p * base^(-2 i / rot_dim), formed in binary64 and rounded once. */
+/* table[p][i] = (cos, sin) of p * base^(-2 i / rot_dim), formed in binary64 and rounded once; rot_dim <= 256, fewer than 2^32 - 256 pairs. */
 int floe_rope_table(float* table, int n_positions, int rot_dim, double base, void* stream);
 
 /*

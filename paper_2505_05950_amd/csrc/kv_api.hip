@@ -171,7 +171,7 @@ extern "C" {
 int floe_rope_table(float* table, int n_positions, int rot_dim, double base, void* stream) {
     if (!table || !aligned(table, 16) || n_positions < 0 || rot_dim <= 0 || !(base > 0.0)) return FLOE_EINVAL;
     if (rot_dim % 16 != 0) return FLOE_ESHAPE;
-    if (rot_dim > 256 || n_positions > (1 << 28)) return FLOE_EUNSUPPORTED;
+    if (rot_dim > 256 || (int64_t)n_positions * (rot_dim / 2) > kMaxGrid * 256) return FLOE_EUNSUPPORTED;  // (a thread per pair)
     if (n_positions == 0) return FLOE_OK;
     FLOE_HIP(launch_rope_table(table, n_positions, rot_dim, base, (hipStream_t)stream));
     return FLOE_OK;

@@ -210,3 +210,9 @@ def test_attention_refuses_batches_whose_workgroups_no_launch_holds(lib):
     # 32 rows per token and KV head, 4096 sequences x heads; 2^32 threads are too many: at 256 dims a row has four, else two
     assert need(256, 8192) == 0 and need(256, 8180) > 0
     assert need(128, 16384) == 0 and need(128, 16300) > 0 and need(192, 8192) > 0 and need(64, 8192) > 0
+
+
+def test_rope_table_refuses_more_pairs_than_a_launch_has_threads(lib):
+    def call(n, rot):
+        return lib.floe_rope_table(P, n, rot, 1e4, None)
+    assert call(1 << 25, 256) == EUNSUPPORTED and call(1 << 28, 32) == EUNSUPPORTED and call((1 << 31) - 1, 16) == EUNSUPPORTED
