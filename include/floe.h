@@ -495,7 +495,7 @@ typedef struct {
     int32_t causal;
     int32_t window; /* 0: none */
     int32_t max_len;
-    float scale;
+    float scale;    /* finite, of either sign */
 } floe_attention;
 size_t floe_kv_attention_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a);
 int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, const void* q, int64_t q_stride, void* out,

@@ -43,7 +43,7 @@ int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_at
     int rc = check_cache(c);
     if (rc) return rc;
     if ((rc = check_seqs(s))) return rc;
-    if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0) return FLOE_EINVAL;
+    if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0 || !__builtin_isfinite(a->scale)) return FLOE_EINVAL;
     if (a->q_heads % c->kv_heads != 0) return FLOE_ESHAPE;
     if (a->q_heads > 1024 || a->window > kKvMaxLen) return FLOE_EUNSUPPORTED;
     // (the widest grid that has to do, in workgroups of 256 threads: the prompt kernel has two threads per query row of a KV head, at 256

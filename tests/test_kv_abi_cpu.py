@@ -216,3 +216,10 @@ def test_rope_table_refuses_more_pairs_than_a_launch_has_threads(lib):
     def call(n, rot):
         return lib.floe_rope_table(P, n, rot, 1e4, None)
     assert call(1 << 25, 256) == EUNSUPPORTED and call(1 << 28, 32) == EUNSUPPORTED and call((1 << 31) - 1, 16) == EUNSUPPORTED
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf")])
+def test_attention_refuses_a_scale_that_is_not_finite(lib, scale):
+    """The prompt kernel bounds the scale from below, which takes a NaN for a small one."""
+    assert lib.floe_kv_attention_workspace_bytes(cache(), seqs(), attn(scale=scale)) == 0
+    assert lib.floe_kv_attention(cache(), seqs(n_rows=0), attn(scale=scale), None, 1024, None, None, None, 0, None) == EINVAL
