@@ -641,12 +641,12 @@ def _kv_calls():
 
 
 def _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows, stream=None) -> bytes:
-    device, n, i32 = cache._device, cu_rows.shape[0] - 1, torch.int32
+    device, n, i32 = cache._device, cu_rows.numel() - 1, torch.int32
     shape = block_table.shape
     if not (cu_rows.dtype is i32 and length.dtype is i32 and block_table.dtype is i32 and cu_rows.is_contiguous() and length.is_contiguous()
             and block_table.is_contiguous()):
         raise ValueError("cu_rows, lengths and block_table are contiguous int32 tensors")
-    if length.shape[0] != n or len(shape) != 2 or shape[0] != n:
+    if length.numel() != n or len(shape) != 2 or shape[0] != n:
         raise ValueError(f"{n} sequences in cu_rows, {tuple(length.shape)} lengths, block_table {tuple(shape)}")
     if cu_rows.get_device() != device or length.get_device() != device or block_table.get_device() != device or device < 0:
         raise ValueError("cu_rows, lengths and block_table are on the cache's GPU")

@@ -223,3 +223,14 @@ def test_attention_refuses_a_scale_that_is_not_finite(lib, scale):
     """The prompt kernel bounds the scale from below, which takes a NaN for a small one."""
     assert lib.floe_kv_attention_workspace_bytes(cache(), seqs(), attn(scale=scale)) == 0
     assert lib.floe_kv_attention(cache(), seqs(n_rows=0), attn(scale=scale), None, 1024, None, None, None, 0, None) == EINVAL
+
+
+def test_index_arrays_hold_an_entry_per_sequence_and_no_more(monkeypatch):
+    """Contiguous arrays are read one entry behind the other: what a second axis holds would be taken for the next sequence's."""
+    c = F.KVCache(2, 2, 64, 32, device="cpu")
+    c._device = 0
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    for cu, length, table in (((3,), (2, 2), (2, 4)), ((3, 2), (2,), (2, 4)), ((3,), (2,), (2, 4, 1)), ((3,), (), (2, 4)), ((0,), (0,), (0, 4))):
+        with pytest.raises(ValueError):
+            B._kv_seqs(c, _On(0, *cu), _On(0, *length), _On(0, *table), 3, 3)
+    assert B._kv_seqs(c, _On(0, 3), _On(0, 2, 1), _On(0, 2, 4), 3, 3) == B._kv_seqs(c, _On(0, 3, 1), _On(0, 2), _On(0, 2, 4), 3, 3)
