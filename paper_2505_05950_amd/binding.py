@@ -728,8 +728,9 @@ def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max
 def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows: int, max_len: int, scale: float = None,
                       causal: bool = True, window: int = 0, want_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
     """Attention of q [rows][q_heads][head_dim] over the cache; length[s] counts the rows' own tokens.  Returns out, or (out, lse) with
-    want_lse.  scale: 1 / sqrt(head_dim) by default.  workspace: the cache's own (one per stream) unless handed over; a captured call
-    keeps the one of the stream it was captured on, so graphs that run side by side are captured on different streams or bring theirs."""
+    want_lse.  scale: 1 / sqrt(head_dim) by default.  max_len: at least every length; far above them, small batches take longer (floe.h).
+    workspace: the cache's own (one per stream) unless handed over; a captured call keeps the one of the stream it was captured on, so
+    graphs that run side by side, or beside eager calls on that stream, are captured on different streams or bring theirs."""
     shape = q.shape
     n_rows, heads = shape[0], shape[1] if len(shape) == 3 else 0
     qs = _kv_rows(q, cache, heads, n_rows, "q")

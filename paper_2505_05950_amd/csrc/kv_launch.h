@@ -61,7 +61,8 @@ constexpr int64_t kKvMostParts = 65535;  // partial results of a call
 // Query rows per KV head up to which a sequence is the rows kernel's.  us, rows / prompt kernel, 32 / 8 heads of 128: 36 rows (9 tokens) of 1
 // sequence of 8000 16.1 / 18.6, 8 of 8000 50 / 69, 64 of 1000 52 / 51, 1 of 1000 11.2 / 12.0; 68 rows 23.0 / 20.2, 79 / 74, 73 / 51, 12.1 / 13.4;
 // 128 rows 21.4 / 23.5, 94 / 81, 100 / 57, 13.1 / 16.1.  16 / 4 heads of 256, 4 of 3000: 68 rows 29.8 / 31.1, 128 rows 40 / 34.  8 / 8 heads of 64,
-// 4 of 3000: 40 rows 16.5 / 18.2, 64 rows 18.3 / 19.5.
+// 4 of 3000: 40 rows 16.5 / 18.2, 64 rows 18.3 / 19.5.  The line is a batch's: one sequence by itself is up to 3 us behind what the rows kernel
+// would take at 68 to 128 rows, where its tiles leave most of the card to none.
 constexpr int kKvRowsLimit = 64;
 // Tiles of sixteen rows that a workgroup of the rows kernel takes at once: as many as its registers hold beside two units of the cache
 constexpr int kv_rows_most_tiles(int dim) { return dim == 64 ? 4 : dim <= 192 ? 2 : 1; }

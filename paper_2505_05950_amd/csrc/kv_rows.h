@@ -99,8 +99,8 @@ __device__ __forceinline__ void load_unit(KvFrag<D, FMT>& f, const KvCache& c, i
     f.vs = gloadf(c.v_scale + slot);
 }
 
-// A row of bf16 queries is multiplied with the power of two that gives its largest exponent 14 (2^14 <= largest < 2^15): what fp16
-// cannot hold then is below 2^-38 of the largest.  Zeros, infinities and NaN stay as they are.
+// A row of bf16 queries is multiplied with the power of two that gives its largest exponent 14 (2^14 <= largest < 2^15): an
+// element below 2^-31 of the largest loses bits of its eight then, below 2^-38 all of them.  Zeros, infinities and NaN stay as they are.
 struct PowerOfTwo {
     float up, down;
 };
