@@ -194,7 +194,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     // One pass over a tile makes 2 D / 16 + 4 kOut products per wave: S^T of its two units, then O^T of either.  Their operands come from LDS in
     // that order, kAhead of them on the way.
     constexpr int kStep = D / 16, kAhead = D == 192 ? 2 : 4;  // (D 192: four 297 us, two 285)
-    // (With eight waves a wave has 256 registers, and at 192 and 256 dims 18 to 21 of them spill: 80 to 88 bytes of scratch per lane.)
+    // (With eight waves a wave has 256 registers, and at 192 and 256 dims 19 to 21 of them spill: 80 to 88 bytes of scratch per lane.)
     h16x8 ring[kAhead];
     auto operand = [&](int buf, int i) {
         if (i < 2 * kStep) {  // K: unit i / kStep, dims 16 (i % kStep) ..

@@ -293,7 +293,7 @@ __device__ __forceinline__ void write_row4(const KvAttnArgs& a, int D, size_t ro
     else w = make_uint2(pack16<false>(o[0] * f, o[1] * f), pack16<false>(o[2] * f, o[3] * f));
     *reinterpret_cast<uint2*>(a.out + (row * a.q_heads + head) * D + d) = w;
     if (a.lse && d == 0)
-        a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + (__builtin_amdgcn_logf(sum) - kSumBits)) * 0.6931471805599453f;
+        a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum * (1.0f / kSumUnit))) * 0.6931471805599453f;
 }
 
 template <int D, int FMT, int MT>
