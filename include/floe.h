@@ -83,7 +83,14 @@ typedef enum {
     FLOE_KERNEL_KV_GATHER = 10,
     FLOE_KERNEL_KV_ATTENTION = 11,
     FLOE_KERNEL_KV_JOIN = 12,  /* partial results of one sequence's tokens, where the attention was split over them */
-    FLOE_KERNEL_KV_PROMPT = 13 /* attention of the sequences with many rows in the call */
+    FLOE_KERNEL_KV_PROMPT = 13, /* attention of the sequences with many rows in the call */
+    FLOE_KERNEL_KV_REORDER = 14,
+    FLOE_KERNEL_KV_TRIM = 15,
+    FLOE_KERNEL_KV_RESERVE = 16,
+    FLOE_KERNEL_KV_COMPACT = 17, /* its three launches together */
+    FLOE_KERNEL_KV_COPY = 18,    /* likewise, of a call with more caches than a launch takes */
+    FLOE_KERNEL_BEAM_ROWS = 19,  /* one pass over the logits */
+    FLOE_KERNEL_BEAM_GROUPS = 20 /* the groups' best of their rows' best */
 } floe_kernel_id;
 int floe_profile_kernel(int kernel_id, void* start_event, void* stop_event);
 
@@ -418,7 +425,7 @@ int floe_stage_channels(const floe_half* host_gd, int d, int f, const int32_t* i
  * a sequence behind its first max_rows are left out.  Tables of different sequences may name the same page for reading; an append must be
  * the only one that writes to a page.
  */
-typedef enum { FLOE_FP16 = 0, FLOE_BF16 = 1 } floe_dtype;
+typedef enum { FLOE_FP16 = 0, FLOE_BF16 = 1, FLOE_FP32 = 2 /* logits only */ } floe_dtype;
 typedef enum { FLOE_KV_INT8 = 0, FLOE_KV_E4M3 = 1 } floe_kv_format;
 
 typedef struct {
@@ -503,6 +510,108 @@ typedef struct {
 size_t floe_kv_attention_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a);
 int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, const void* q, int64_t q_stride, void* out,
                       float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * The same with first tokens that stay visible beside the window: with window > 0 a row also sees every key j < sinks (causal: none
+ * behind its position).  Pages that lie wholly between the first tokens and the windows are not read: their table entries may be absent
+ * (floe_kv_trim makes them so).  0 <= sinks <= 2^30; without a window, and with sinks 0, the result is that of floe_kv_attention.
+ */
+size_t floe_kv_attention_sinks_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, int sinks);
+int floe_kv_attention_sinks(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, int sinks, const void* q, int64_t q_stride,
+                            void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * The pages of such caches.  A model's layers share one set of tables: page p of every layer's cache belongs to the same tokens.
+ *
+ * A pool counts, for each page, the table entries that name it (of all tables that are in use); a page is free where that count is not
+ * positive.  The caller fills refs with zeros once, then only these calls change it (a page that nobody may be given: a count of its own).
+ * Everything stays on the device: no call looks at a result on the host, so a whole step can be captured.  The same state and call give
+ * the same tables.
+ *   refs  dev int32 [n_pages], 16-byte aligned
+ *   tables dev int32 [n_seqs][max_blocks]: an entry outside [0, n_pages) is an absent page
+ * Supported: block in {32, 64, 128}; n_pages <= 2^24; n_seqs <= 65535; max_blocks <= 2^23; n_seqs * max_blocks < 2^31.  Lengths are taken
+ * between 0 and 2^30.  Calls on one pool are ordered by the caller (one stream, or events).
+ */
+typedef struct {
+    int32_t n_pages;
+    int32_t block; /* tokens of a page */
+    int32_t* refs;
+} floe_kv_pool;
+
+/*
+ * Sequences take over the pages of their parents (beams that go on, samples of one prompt, sequences that leave out or change places):
+ *   table_out[i] = table[parent[i]], len_out[i] = len[parent[i]];   parent[i] outside [0, n_seqs): no pages, length 0
+ * and `table` is no longer in use: a page's count loses what `table` named and gains what table_out names.  Several children share all
+ * pages of their parent, also the one that the next token goes to: floe_kv_reserve gives whoever writes a page of its own.
+ * Outputs may not overlap `table`, `len` or `parent`.  One launch.
+ */
+int floe_kv_reorder(const floe_kv_pool* p, const int32_t* table, const int32_t* len, int n_seqs, int max_blocks, const int32_t* parent,
+                    int32_t* table_out, int32_t* len_out, int n_out, void* stream);
+
+/*
+ * Pages for the rows that an append is about to write: cu_rows and len are that call's.  Every block of rows len[s] .. len[s] + n - 1 gets
+ *   a page, if its entry is absent
+ *   a page of its own, if others name the one that it has (count > 1).  Where all that name it are sequences of this call which write
+ *   to it, the first of them keeps it.  If the block already holds tokens of the sequence (the block of len[s], len[s] not a multiple of
+ *   block), pairs[s] = (old page, new page): what has to be copied, by floe_kv_copy_pages, before the append.  Otherwise pairs[s] = (-1, -1).
+ * Pages are handed out from the lowest free one on, in the order of (sequence, block).
+ * missing dev int32 [1]: blocks that got no page since none was free or since they lie behind max_blocks (those up to 2^20).  Their entries
+ * stay as they were, so that the call can be made again when pages are free; nothing may be appended before that.
+ * pairs dev int32 [n_seqs][2].  workspace: dev, 256-byte aligned, contents are scratch.  One launch.
+ */
+size_t floe_kv_reserve_workspace_bytes(const floe_kv_pool* p);
+int floe_kv_reserve(const floe_kv_pool* p, int32_t* table, const int32_t* len, const int32_t* cu_rows, int n_seqs, int max_blocks, int32_t* pairs,
+                    int32_t* missing, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gives back what no later query sees.  A block keeps its page if it holds a token t < len[s] with
+ *   window == 0,  or t > len[s] - window (seen by the query at position len[s]),  or t < sinks
+ * Other entries become -1 and their pages lose a count: blocks that left the window, blocks behind the end (reserved, or of drafts that were
+ * rejected), all blocks of a sequence of length 0.  One launch.
+ */
+int floe_kv_trim(const floe_kv_pool* p, int32_t* table, const int32_t* len, int n_seqs, int max_blocks, int sinks, int window, void* stream);
+
+/*
+ * Packs the pool: with U used pages in all, the highest used page moves to the lowest free one, and so on, up to n_pairs moves; if these
+ * are enough, pages 0 .. U - 1 are the used ones.  refs and table follow; pairs[i] = (from, to), (-1, -1) behind the last move:
+ * floe_kv_copy_pages has to run on them before the pages are read or written.  page_map dev int32 [n_pages]: the new place of every page
+ * (itself where it stays), for tables beside `table`.  pairs dev int32 [n_pairs][2].  workspace: dev, 256-byte aligned.
+ */
+size_t floe_kv_compact_workspace_bytes(const floe_kv_pool* p, int n_pairs);
+int floe_kv_compact(const floe_kv_pool* p, int32_t* table, int n_seqs, int max_blocks, int32_t* pairs, int n_pairs, int32_t* page_map, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/*
+ * Copies pages (codes and scales of all heads) inside each of n_caches caches of one form, the layers of a model: page pairs[i][0] to
+ * page pairs[i][1].  A pair with a number outside [0, n_pages) is left out.  No page may be the target of two pairs, or of one and the
+ * source of another: what it holds afterwards is not defined then.  caches: host.  A launch for every 64 caches.
+ */
+int floe_kv_copy_pages(const floe_kv_cache* caches, int n_caches, const int32_t* pairs, int n_pairs, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Beam search: of each group of `beams` rows of logits the `take` best continuations.
+ *   x = logits in binary32 (NaN counts as -infinity, +infinity as the largest finite value, -0 as 0);  m = max x, s = sum exp(x - m) of a row
+ *   c(row, token) = score[row] + ((x - m) - log s), in binary64
+ * Candidates are the tokens with x > -infinity of rows whose score is neither -infinity nor NaN.  They are ordered by c, largest first;
+ * equal ones by row, then by x (largest first), then by token.  A row with done[row] != 0 offers `eos` alone, with c = score[row], and its
+ * logits are not read.  Terms of s have the precision of binary32: log s is off by 5e-6 at most, the same for equal rows wherever they lie.
+ *   score_out  dev float [groups][take]: c, rounded once
+ *   parent     dev int32 [groups][take]: the row (0 .. groups * beams - 1), which is what floe_kv_reorder takes
+ *   token      dev int32 [groups][take]
+ *   done_out   dev uint8 [groups][take], or NULL: 1 where the token is eos or the parent was done
+ * Places behind the last candidate hold score -infinity, parent -1, token -1, done 0.
+ * logits dev [groups * beams] rows of `vocab` values of `dtype`, row_stride elements from row to row (any that keeps rows apart; rows need
+ * no more than their type's alignment).  score dev float [groups][beams]; done dev uint8 [groups][beams], or NULL.  eos: in [0, vocab), or
+ * -1: no token ends a row (done has to be NULL then).  Outputs may overlap no input.
+ * Supported: take <= 64, beams <= 256, vocab < 2^28, groups * beams <= 2^20.  workspace: dev, 256-byte aligned, scratch.
+ */
+typedef struct {
+    int32_t groups, beams, vocab, take;
+    int32_t dtype; /* floe_dtype of the logits */
+    int32_t eos;
+} floe_beam;
+size_t floe_beam_workspace_bytes(const floe_beam* b);
+int floe_beam_select(const floe_beam* b, const void* logits, int64_t row_stride, const float* score, const uint8_t* done, float* score_out,
+                     int32_t* parent, int32_t* token, uint8_t* done_out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

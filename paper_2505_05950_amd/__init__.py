@@ -16,4 +16,5 @@ from .binding import (  # noqa: F401
     ChannelCache, floe_channel_cache_load, floe_moe_layer_decode_cached,
     floe_expert_ffn_sparsified, SPARSIFY_UP, SPARSIFY_GATE, SPARSIFY_DOWN,
     KVCache, Rope, KV_INT8, KV_E4M3, floe_rope_table, floe_kv_append, floe_kv_gather, floe_kv_attention,
+    KVPool, floe_kv_reorder, floe_kv_reserve, floe_kv_trim, floe_kv_compact, floe_kv_copy_pages, floe_beam_select,
 )

@@ -85,6 +85,14 @@ class _Rope(C.Structure):
                 ("interleaved", C.c_int32)]
 
 
+class _KvPool(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("block", C.c_int32), ("refs", C.c_void_p)]
+
+
+class _Beam(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("beams", C.c_int32), ("vocab", C.c_int32), ("take", C.c_int32), ("dtype", C.c_int32), ("eos", C.c_int32)]
+
+
 class _Attention(C.Structure):
     _fields_ = [("q_heads", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32), ("max_len", C.c_int32), ("scale", C.c_float)]
 
@@ -143,6 +151,22 @@ def load():
     lib.floe_kv_attention_workspace_bytes.restype = sz
     lib.floe_kv_attention_workspace_bytes.argtypes = [kv, seqs, attn]
     lib.floe_kv_attention.argtypes = [kv, seqs, attn, vp, i64, vp, vp, vp, sz, vp]
+    lib.floe_kv_attention_sinks_workspace_bytes.restype = sz
+    lib.floe_kv_attention_sinks_workspace_bytes.argtypes = [kv, seqs, attn, i32]
+    lib.floe_kv_attention_sinks.argtypes = [kv, seqs, attn, i32, vp, i64, vp, vp, vp, sz, vp]
+    pool, beam = C.POINTER(_KvPool), C.POINTER(_Beam)
+    lib.floe_kv_reorder.argtypes = [pool, vp, vp, i32, i32, vp, vp, vp, i32, vp]
+    lib.floe_kv_trim.argtypes = [pool, vp, vp, i32, i32, i32, i32, vp]
+    lib.floe_kv_reserve_workspace_bytes.restype = sz
+    lib.floe_kv_reserve_workspace_bytes.argtypes = [pool]
+    lib.floe_kv_reserve.argtypes = [pool, vp, vp, vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.floe_kv_compact_workspace_bytes.restype = sz
+    lib.floe_kv_compact_workspace_bytes.argtypes = [pool, i32]
+    lib.floe_kv_compact.argtypes = [pool, vp, i32, i32, vp, i32, vp, vp, sz, vp]
+    lib.floe_kv_copy_pages.argtypes = [vp, i32, vp, i32, vp]
+    lib.floe_beam_workspace_bytes.restype = sz
+    lib.floe_beam_workspace_bytes.argtypes = [beam]
+    lib.floe_beam_select.argtypes = [beam, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -152,7 +176,8 @@ def floe_status_string(status: int) -> str:
 
 
 KERNEL_IDS = {"none": 0, "quantize": 1, "router": 2, "up_gemv": 3, "select": 4, "gate_down": 5, "combine": 6, "stage": 7,
-              "fused_ffn": 8, "kv_append": 9, "kv_gather": 10, "kv_attention": 11, "kv_join": 12, "kv_prompt": 13}
+              "fused_ffn": 8, "kv_append": 9, "kv_gather": 10, "kv_attention": 11, "kv_join": 12, "kv_prompt": 13, "kv_reorder": 14, "kv_trim": 15, "kv_reserve": 16,
+              "kv_compact": 17, "kv_copy": 18, "beam_rows": 19, "beam_groups": 20}
 
 
 def floe_profile_kernel(kernel: str, start_event=None, stop_event=None):
@@ -630,12 +655,12 @@ def _kv_calls():
     global _kv_functions
     if _kv_functions is None:
         lib, vp, i64, i32, packed, sz = load(), C.c_void_p, C.c_int64, C.c_int, C.c_char_p, C.c_size_t
-        append, gather, attention, need = (lib[n] for n in ("floe_kv_append", "floe_kv_gather", "floe_kv_attention",
-                                                            "floe_kv_attention_workspace_bytes"))
+        append, gather, attention, need = (lib[n] for n in ("floe_kv_append", "floe_kv_gather", "floe_kv_attention_sinks",
+                                                            "floe_kv_attention_sinks_workspace_bytes"))
         append.argtypes = [vp, packed, vp, i64, vp, i64, vp, i64, i32, vp, packed, vp]
         gather.argtypes = [vp, packed, vp, vp, vp]
-        attention.argtypes = [vp, packed, packed, vp, i64, vp, vp, vp, sz, vp]
-        need.argtypes, need.restype = [vp, packed, packed], sz
+        attention.argtypes = [vp, packed, packed, i32, vp, i64, vp, vp, vp, sz, vp]
+        need.argtypes, need.restype = [vp, packed, packed, i32], sz
         _kv_functions = append, gather, attention, need
     return _kv_functions
 
@@ -726,9 +751,10 @@ def floe_kv_gather(cache: KVCache, first, cu_rows, block_table, n_rows: int, max
 
 
 def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows: int, max_len: int, scale: float = None,
-                      causal: bool = True, window: int = 0, want_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
+                      causal: bool = True, window: int = 0, want_lse: bool = False, out=None, lse=None, workspace=None, stream=None,
+                      sinks: int = 0):
     """Attention of q [rows][q_heads][head_dim] over the cache; length[s] counts the rows' own tokens.  Returns out, or (out, lse) with
-    want_lse.  scale: 1 / sqrt(head_dim) by default.  max_len: at least every length; far above them, small batches take longer (floe.h).
+    want_lse.  scale: 1 / sqrt(head_dim) by default.  sinks: first tokens that rows see beside their window.  max_len: at least every length; far above them, small batches take longer (floe.h).
     workspace: the cache's own (one per stream) unless handed over; a captured call keeps the one of the stream it was captured on, so
     graphs that run side by side, or beside eager calls on that stream, are captured on different streams or bring theirs."""
     shape = q.shape
@@ -744,11 +770,162 @@ def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows:
         raise ValueError(f"workspace: on {workspace.device}, the cache is on {cache.k.device}")
     st = _stream(stream)
     at, size = cache.workspace(256, st, stream) if workspace is None else _aligned_ptr(workspace)
-    args = cache._at, s, a, q.data_ptr(), qs, out.data_ptr(), None if lse is None else lse.data_ptr()
+    args = cache._at, s, a, sinks, q.data_ptr(), qs, out.data_ptr(), None if lse is None else lse.data_ptr()
     rc = call(*args, at, size, st)
     if rc == -4 and workspace is None:  # refused before anything is enqueued: the cache's workspace has to grow
-        at, size = cache.workspace(need(cache._at, s, a), st, stream)
+        at, size = cache.workspace(need(cache._at, s, a, sinks), st, stream)
         rc = call(*args, at, size, st)
     if rc:
         _check(rc, "floe_kv_attention")
     return (out, lse) if lse is not None else out
+
+
+# ---- the pages of such caches: handed out, shared, given back, packed, copied (include/floe.h)
+def _i32(t, shape, device, name):
+    """Address of a contiguous int32 tensor of this shape (None: any size) on the pool's GPU."""
+    if t.dtype is not torch.int32 or not t.is_contiguous() or len(t.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        want = "".join(f"[{'n' if n is None else n}]" for n in shape)
+        raise ValueError(f"{name}: expected contiguous int32 {want}, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
+    return t.data_ptr()
+
+
+class KVPool:
+    """How many table entries name each of a cache's pages: refs int32 [n_pages], zeros at the start (refs=: an array that exists).  One
+    pool serves the caches of all layers, which share their tables."""
+
+    def __init__(self, n_pages: int, block: int = 64, refs=None, device="cuda"):
+        self.n_pages, self.block = int(n_pages), int(block)
+        if self.n_pages < 1:
+            raise ValueError(f"KVPool: at least one page, not {n_pages}")
+        if refs is None:
+            refs = torch.zeros((self.n_pages,), dtype=torch.int32, device=device)
+        if refs.dtype is not torch.int32 or refs.shape != (self.n_pages,) or not refs.is_contiguous():
+            raise ValueError(f"KVPool: refs is a contiguous int32 tensor [{self.n_pages}], got {refs.dtype} {tuple(refs.shape)}")
+        self.refs, self._device = refs, refs.get_device()
+        self._c = _KvPool(self.n_pages, self.block, refs.data_ptr())
+
+    def _table(self, table, name="table", stream=None):
+        _launches_on(self._device, stream, "the pool")
+        return _i32(table, (None, None), self._device, name)
+
+
+# Address and size of a call's scratch.  Where the caller brings none, the call takes its own from the pool of its stream and gives it back
+# when it has been enqueued: no two calls, and no two captured graphs, share an array that outlives them.
+def _scratch(workspace, device: int):
+    if workspace.get_device() != device:
+        raise ValueError(f"workspace: on {workspace.device}, expected cuda:{device}")
+    return _aligned_ptr(workspace)
+
+
+def _out_i32(t, shape, device, name, stream):
+    if t is None:
+        return _empty(shape, torch.int32, torch.device("cuda", device), stream)
+    _i32(t, shape, device, name)
+    return t
+
+
+def floe_kv_reorder(pool: KVPool, table, length, parent, table_out=None, length_out=None, stream=None):
+    """Sequence i takes over the pages and the length of sequence parent[i] (outside the table: none); `table` is no longer in use afterwards.
+    Returns (table_out, length_out)."""
+    at = pool._table(table, stream=stream)
+    (n, blocks), dev = table.shape, pool._device
+    length_at, parent_at = _i32(length, (n,), dev, "length"), _i32(parent, (None,), dev, "parent")
+    m = parent.shape[0]
+    table_out = _out_i32(table_out, (m, blocks), dev, "table_out", stream)
+    length_out = _out_i32(length_out, (m,), dev, "length_out", stream)
+    _check(load().floe_kv_reorder(C.byref(pool._c), at, length_at, n, blocks, parent_at, table_out.data_ptr(), length_out.data_ptr(), m, _stream(stream)),
+           "floe_kv_reorder")
+    return table_out, length_out
+
+
+def floe_kv_reserve(pool: KVPool, table, length, cu_rows, pairs=None, missing=None, workspace=None, stream=None):
+    """Gives every block that an append of cu_rows behind `length` tokens writes to a page that only its sequence names.  Returns (pairs
+    int32 [sequences][2], what floe_kv_copy_pages has to copy before the append; missing int32 [1], blocks that got no page)."""
+    at = pool._table(table, stream=stream)
+    (n, blocks), dev = table.shape, pool._device
+    length_at, cu_at = _i32(length, (n,), dev, "length"), _i32(cu_rows, (n + 1,), dev, "cu_rows")
+    pairs, missing = _out_i32(pairs, (n, 2), dev, "pairs", stream), _out_i32(missing, (1,), dev, "missing", stream)
+    lib = load()
+    if workspace is None:
+        workspace = _workspace(lib.floe_kv_reserve_workspace_bytes(C.byref(pool._c)), table.device, stream)
+    wp, wn = _scratch(workspace, dev)
+    _check(lib.floe_kv_reserve(C.byref(pool._c), at, length_at, cu_at, n, blocks, pairs.data_ptr(), missing.data_ptr(), wp, wn, _stream(stream)),
+           "floe_kv_reserve")
+    return pairs, missing
+
+
+def floe_kv_trim(pool: KVPool, table, length, window: int = 0, sinks: int = 0, stream=None):
+    """Gives back the blocks of `table` that no query behind `length` tokens sees: all behind the end, and with a window those before it
+    that hold none of the first `sinks` tokens."""
+    at = pool._table(table, stream=stream)
+    n, blocks = table.shape
+    _check(load().floe_kv_trim(C.byref(pool._c), at, _i32(length, (n,), pool._device, "length"), n, blocks, int(sinks), int(window), _stream(stream)),
+           "floe_kv_trim")
+
+
+def floe_kv_compact(pool: KVPool, table, max_moves: int = None, pairs=None, page_map=None, workspace=None, stream=None):
+    """Moves the highest used pages to the lowest free ones (max_moves at most: as many as there are pages by default); the pool and `table`
+    follow at once.  Returns (pairs int32 [max_moves][2], what floe_kv_copy_pages has to copy; page_map int32 [n_pages], where each page went)."""
+    at = pool._table(table, stream=stream)
+    (n, blocks), dev = table.shape, pool._device
+    moves = pool.n_pages if max_moves is None else int(max_moves)
+    pairs, page_map = _out_i32(pairs, (moves, 2), dev, "pairs", stream), _out_i32(page_map, (pool.n_pages,), dev, "page_map", stream)
+    lib = load()
+    if workspace is None:
+        workspace = _workspace(lib.floe_kv_compact_workspace_bytes(C.byref(pool._c), moves), table.device, stream)
+    wp, wn = _scratch(workspace, dev)
+    _check(lib.floe_kv_compact(C.byref(pool._c), at, n, blocks, pairs.data_ptr(), moves, page_map.data_ptr(), wp, wn, _stream(stream)), "floe_kv_compact")
+    return pairs, page_map
+
+
+def floe_kv_copy_pages(caches, pairs, stream=None):
+    """Copies page pairs[i][0] to page pairs[i][1] (-1: none) in each of the caches, the layers of a model."""
+    caches = [caches] if isinstance(caches, KVCache) else list(caches)
+    if not caches:
+        return
+    dev = caches[0]._device
+    if any(c._device != dev for c in caches):
+        raise ValueError("floe_kv_copy_pages: the caches are on one device")
+    _launches_on(dev, stream, "the cache")
+    at = _i32(pairs, (None, 2), dev, "pairs")
+    packed = b"".join([bytes(c._c) for c in caches])
+    _check(load().floe_kv_copy_pages(packed, len(caches), at, pairs.shape[0], _stream(stream)), "floe_kv_copy_pages")
+
+
+# ---- beam search
+_BEAM_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+def floe_beam_select(logits, score, take: int = None, done=None, eos: int = -1, score_out=None, parent=None, token=None, done_out=None, workspace=None,
+                     stream=None):
+    """The `take` best continuations (as many as beams by default) of each group: logits [groups * beams][vocab] fp16, bf16 or fp32 (rows may lie
+    anywhere), score fp32 [groups][beams], done uint8 [groups][beams] (rows that offer `eos` alone).  Returns (score, parent, token, done), all
+    [groups][take]; parent is the row that a continuation comes from, -1 behind the last one (include/floe.h)."""
+    if logits.dtype not in _BEAM_DTYPES or logits.dim() != 2 or score.dim() != 2 or logits.shape[0] != score.numel():
+        raise ValueError(f"floe_beam_select: logits fp16, bf16 or fp32 [groups * beams][vocab], got {logits.dtype} {tuple(logits.shape)}, score {tuple(score.shape)}")
+    groups, beams = score.shape
+    rows, vocab = logits.shape
+    if (vocab > 1 and rows and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < vocab):
+        raise ValueError(f"floe_beam_select: the logits of a row lie one behind the other, and rows apart (strides {logits.stride()})")
+    dev = logits.get_device()
+    _launches_on(dev, stream, "floe_beam_select: logits")
+    for t, kind, name in ((score, torch.float32, "score"), (done, torch.uint8, "done")):
+        if t is not None and (t.dtype is not kind or t.shape != (groups, beams) or not t.is_contiguous() or t.get_device() != dev):
+            raise ValueError(f"{name}: expected contiguous {kind} {(groups, beams)} on {logits.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    shape = (groups, beams if take is None else int(take))
+    outs = []
+    for t, kind, name in ((score_out, torch.float32, "score_out"), (parent, torch.int32, "parent"), (token, torch.int32, "token"), (done_out, torch.uint8, "done_out")):
+        if t is None:
+            t = _empty(shape, kind, logits.device, stream)
+        elif t.dtype is not kind or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError(f"{name}: expected contiguous {kind} {shape} on {logits.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        outs.append(t)
+    b, lib = _Beam(groups, beams, vocab, shape[1], _BEAM_DTYPES[logits.dtype], int(eos)), load()
+    if workspace is None:
+        workspace = _workspace(lib.floe_beam_workspace_bytes(C.byref(b)), logits.device, stream)
+    wp, wn = _scratch(workspace, dev)
+    _check(lib.floe_beam_select(C.byref(b), logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, score.data_ptr(), None if done is None else done.data_ptr(),
+                                *(t.data_ptr() for t in outs), wp, wn, _stream(stream)), "floe_beam_select")
+    return tuple(outs)

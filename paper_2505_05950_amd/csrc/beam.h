@@ -1,0 +1,35 @@
+// Beam search's selection (include/floe.h): what its two kernels share, and their launcher.  Arguments are checked in beam_api.hip.
+#pragma once
+
+#include "kv_cache.h"
+#include "launch.h"
+
+namespace floe {
+
+constexpr int kBeamTake = 64;       // candidates of a group, at most: a lane each
+constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / kWave;
+constexpr int kBeamRows = 256;      // rows of a group, at most
+
+struct BeamArgs {
+    const void* logits;
+    int64_t stride;
+    const float* score;
+    const uint8_t* done;
+    int groups, beams, vocab, take, eos;
+    int slices, slice;  // of a row, and the tokens of one
+    float* score_out;
+    int32_t *parent, *token;
+    uint8_t* done_out;
+    // [rows][slices]: largest logit and the sum of exp(x - it); [rows][slices][take]: the best tokens, in no order, 0 where there are fewer
+    float* sums;
+    uint64_t* best;
+};
+
+struct BeamCut {
+    int slices, slice;
+};
+BeamCut beam_cut(int rows, int vocab, int dtype);  // dtype: floe_dtype
+hipError_t launch_beam_rows(const BeamArgs& a, int dtype, hipStream_t st);
+hipError_t launch_beam_groups(const BeamArgs& a, hipStream_t st);
+
+}  // namespace floe

@@ -49,4 +49,17 @@ constexpr size_t kAlign = 256;
 inline size_t align_up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+constexpr int64_t kMaxGrid = (1 << 24) - 1;  // workgroups of 256 threads along one axis
+
+inline int check_kv_cache(const floe_kv_cache* c) {
+    if (!c || c->n_pages <= 0 || c->kv_heads <= 0 || !c->k || !c->v || !c->k_scale || !c->v_scale) return FLOE_EINVAL;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return FLOE_EINVAL;
+    if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 192 && c->head_dim != 256) return FLOE_EUNSUPPORTED;
+    if (c->block != 32 && c->block != 64 && c->block != 128) return FLOE_EUNSUPPORTED;
+    if (c->kv_heads > 256) return FLOE_EUNSUPPORTED;
+    if (c->format != FLOE_KV_INT8 && c->format != FLOE_KV_E4M3) return FLOE_EUNSUPPORTED;
+    if (c->dtype != FLOE_FP16 && c->dtype != FLOE_BF16) return FLOE_EUNSUPPORTED;
+    return FLOE_OK;
+}
+
 }  // namespace floe

@@ -6,18 +6,6 @@ using namespace floe;
 
 namespace {
 
-constexpr int64_t kMaxGrid = (1 << 24) - 1;  // workgroups of 256 threads along one axis
-
-int check_cache(const floe_kv_cache* c) {
-    if (!c || c->n_pages <= 0 || c->kv_heads <= 0 || !c->k || !c->v || !c->k_scale || !c->v_scale) return FLOE_EINVAL;
-    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return FLOE_EINVAL;
-    if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 192 && c->head_dim != 256) return FLOE_EUNSUPPORTED;
-    if (c->block != 32 && c->block != 64 && c->block != 128) return FLOE_EUNSUPPORTED;
-    if (c->kv_heads > 256) return FLOE_EUNSUPPORTED;
-    if (c->format != FLOE_KV_INT8 && c->format != FLOE_KV_E4M3) return FLOE_EUNSUPPORTED;
-    if (c->dtype != FLOE_FP16 && c->dtype != FLOE_BF16) return FLOE_EUNSUPPORTED;
-    return FLOE_OK;
-}
 int check_seqs(const floe_kv_seqs* s) {
     if (!s || s->n_seqs < 0 || s->n_rows < 0 || s->max_rows < 0 || s->max_blocks < 0) return FLOE_EINVAL;
     if (s->n_seqs > 65535 || s->n_rows > (1 << 24) || s->max_blocks > (1 << 24)) return FLOE_EUNSUPPORTED;
@@ -39,13 +27,13 @@ int64_t block_tasks(const floe_kv_cache* c, const KvSeqs& s) {
     return (int64_t)s.n_seqs * kv_blocks_per_seq(s.max_rows, c->block) * c->kv_heads * 2;
 }
 
-int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
-    int rc = check_cache(c);
+int check_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, int sinks) {
+    int rc = check_kv_cache(c);
     if (rc) return rc;
     if ((rc = check_seqs(s))) return rc;
-    if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0 || !__builtin_isfinite(a->scale)) return FLOE_EINVAL;
+    if (!a || a->q_heads <= 0 || a->window < 0 || a->max_len < 0 || sinks < 0 || !__builtin_isfinite(a->scale)) return FLOE_EINVAL;
     if (a->q_heads % c->kv_heads != 0) return FLOE_ESHAPE;
-    if (a->q_heads > 1024 || a->window > kKvMaxLen) return FLOE_EUNSUPPORTED;
+    if (a->q_heads > 1024 || a->window > kKvMaxLen || sinks > kKvMaxLen) return FLOE_EUNSUPPORTED;
     // (the widest grid that has to do, in workgroups of 256 threads: the prompt kernel has two threads per query row of a KV head, at 256
     // dims four; the rows kernel has up to four workgroups)
     const KvSeqs k = dev_seqs(s);
@@ -117,7 +105,12 @@ void cut_prompts(AttnPlan& w, int dim, int64_t heads, int64_t rows, int64_t tile
     }
     w.prompt_chunks = (int)((tiles + w.prompt_chunk - 1) / w.prompt_chunk);
 }
-AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
+// The most tokens that `rows` rows of a sequence see: their windows, the first tokens, and what the steps of the walk take beside both
+int64_t keys_of(const floe_attention* a, int sinks, int64_t rows) {
+    const int64_t seen = a->window + rows + (sinks ? sinks + 63 : 0);
+    return a->window > 0 && seen < a->max_len ? seen : a->max_len;
+}
+AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, int sinks) {
     AttnPlan w{};
     w.total = kAlign;  // (so that a workspace is a workspace whichever kernels run)
     const KvSeqs k = dev_seqs(s);
@@ -134,10 +127,8 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
         w.most_rows = w.rows ? most : 0;
         w.row_limit = most;
     }
-    const int64_t max_keys = a->max_len;
     if (w.prompt) {
-        const int64_t seen = a->window + (int64_t)k.max_rows;  // (a tile of rows sees less where they are many)
-        const int64_t keys = a->window > 0 && seen < max_keys ? seen : max_keys;
+        const int64_t keys = keys_of(a, sinks, k.max_rows);  // (a tile of rows sees less where they are many)
         cut_prompts(w, c->head_dim, (int64_t)k.n_seqs * c->kv_heads, (int64_t)k.max_rows * group, (keys + 63) / 64 + 1);
         if ((int64_t)a->q_heads * k.max_rows > kMaxGrid) w.prompt_chunks = 1;  // (more rows than a join has workgroups)
         if (w.prompt_chunks > 1) {
@@ -151,7 +142,7 @@ AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_att
     w.mt = kv_rows_tiles_for(c->head_dim, rows);
     w.tiles = (rows + 16 * w.mt - 1) / (16 * w.mt);
     const int64_t segments = (int64_t)k.n_seqs * c->kv_heads * w.tiles;
-    const int64_t keys = a->window > 0 && a->window + (int64_t)w.row_limit < max_keys ? a->window + (int64_t)w.row_limit : max_keys;
+    const int64_t keys = keys_of(a, sinks, w.row_limit);
     cut_segments(w, segments, (keys + kKvGroup - 1) / kKvGroup + 1);
     if (w.chunks > 1) {
         w.part_rows = rows < 16 * w.mt ? rows : 16 * w.mt;
@@ -179,7 +170,7 @@ int floe_rope_table(float* table, int n_positions, int rot_dim, double base, voi
 
 int floe_kv_append(const floe_kv_cache* c, const floe_kv_seqs* s, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                    const void* q, int64_t q_stride, int q_heads, void* q_out, const floe_rope* rope, void* stream) {
-    int rc = check_cache(c);
+    int rc = check_kv_cache(c);
     if (rc) return rc;
     if ((rc = check_seqs(s))) return rc;
     const int64_t row = (int64_t)c->kv_heads * c->head_dim, limit = (int64_t)1 << 40;
@@ -217,7 +208,7 @@ int floe_kv_append(const floe_kv_cache* c, const floe_kv_seqs* s, const void* k,
 }
 
 int floe_kv_gather(const floe_kv_cache* c, const floe_kv_seqs* s, void* k_out, void* v_out, void* stream) {
-    int rc = check_cache(c);
+    int rc = check_kv_cache(c);
     if (rc) return rc;
     if ((rc = check_seqs(s))) return rc;
     if (nothing(s)) return FLOE_OK;
@@ -232,13 +223,21 @@ int floe_kv_gather(const floe_kv_cache* c, const floe_kv_seqs* s, void* k_out, v
     return FLOE_OK;
 }
 
+size_t floe_kv_attention_sinks_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, int sinks) {
+    return check_attention(c, s, a, sinks) == FLOE_OK && !nothing(s) ? attn_plan(c, s, a, a->window > 0 ? sinks : 0).total : 0;
+}
 size_t floe_kv_attention_workspace_bytes(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a) {
-    return check_attention(c, s, a) == FLOE_OK && !nothing(s) ? attn_plan(c, s, a).total : 0;
+    return floe_kv_attention_sinks_workspace_bytes(c, s, a, 0);
 }
 
 int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, const void* q, int64_t q_stride, void* out,
                       float* lse, void* workspace, size_t workspace_bytes, void* stream) {
-    int rc = check_attention(c, s, a);
+    return floe_kv_attention_sinks(c, s, a, 0, q, q_stride, out, lse, workspace, workspace_bytes, stream);
+}
+
+int floe_kv_attention_sinks(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, int sinks, const void* q, int64_t q_stride,
+                            void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_attention(c, s, a, sinks);
     if (rc) return rc;
     if (q_stride < (int64_t)a->q_heads * c->head_dim || q_stride % 8) return FLOE_EINVAL;
     if (q_stride > (int64_t)1 << 40) return FLOE_EUNSUPPORTED;
@@ -246,7 +245,8 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     if ((rc = check_arrays(s))) return rc;
     if (!q || !out || !workspace || !aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, kAlign))
         return FLOE_EINVAL;
-    const AttnPlan w = attn_plan(c, s, a);
+    if (a->window == 0) sinks = 0;  // (every row sees its first tokens)
+    const AttnPlan w = attn_plan(c, s, a, sinks);
     if (workspace_bytes < w.total) return FLOE_EWORKSPACE;
     char* base = static_cast<char*>(workspace);
     KvAttnArgs k{};
@@ -261,6 +261,7 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     k.scale_log2 = a->scale * 1.4426950408889634f;
     k.causal = a->causal != 0;
     k.window = a->window;
+    k.sinks = sinks;
     k.bf16 = c->dtype == FLOE_BF16;
     k.most_rows = w.most_rows;
     k.parts = KvParts{reinterpret_cast<float*>(base + w.rows_off), reinterpret_cast<float*>(base + w.ml_off)};
@@ -276,12 +277,14 @@ int floe_kv_attention(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_
     k.part_rows = w.part_rows;
     hipStream_t st = (hipStream_t)stream;
     const bool int8 = c->format == FLOE_KV_INT8;
+    const auto prompt = sinks ? int8 ? launch_kv_prompt_sinks_int8 : launch_kv_prompt_sinks_e4m3 : int8 ? launch_kv_prompt_int8 : launch_kv_prompt_e4m3;
+    const auto rows = sinks ? int8 ? launch_kv_rows_sinks_int8 : launch_kv_rows_sinks_e4m3 : int8 ? launch_kv_rows_int8 : launch_kv_rows_e4m3;
     if (w.prompt) {
-        FLOE_LAUNCH(FLOE_KERNEL_KV_PROMPT, st, int8 ? launch_kv_prompt_int8(k, st) : launch_kv_prompt_e4m3(k, st));
+        FLOE_LAUNCH(FLOE_KERNEL_KV_PROMPT, st, prompt(k, st));
         if (w.prompt_chunks > 1) FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_prompt_join(k, st));
     }
     if (w.rows) {
-        FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st, int8 ? launch_kv_rows_int8(k, w.mt, st) : launch_kv_rows_e4m3(k, w.mt, st));
+        FLOE_LAUNCH(FLOE_KERNEL_KV_ATTENTION, st, rows(k, w.mt, st));
         if (w.chunks > 1) FLOE_LAUNCH(FLOE_KERNEL_KV_JOIN, st, launch_kv_join(k, w.mt, w.row_limit, st));
     }
     return FLOE_OK;

@@ -42,6 +42,7 @@ struct KvAttnArgs {
     int q_heads, group;
     float scale_log2;  // softmax scale * log2(e)
     int causal, window;
+    int sinks;  // with a window: the first tokens that every row sees beside it
     bool bf16;
     int most_rows;  // sequences of up to so many rows are the rows kernel's, the others the prompt kernel's
     // rows kernel (kv_rows.h)
@@ -73,11 +74,15 @@ inline int kv_rows_tiles_for(int dim, int rows) {
 constexpr int kv_rows_waves_per_simd(int dim, int mt) { return dim * mt <= 128 ? 3 : dim * mt <= 256 && dim < 256 ? 2 : 1; }
 hipError_t launch_kv_rows_int8(const KvAttnArgs& a, int mt, hipStream_t st);  // mt tiles of sixteen rows per workgroup
 hipError_t launch_kv_rows_e4m3(const KvAttnArgs& a, int mt, hipStream_t st);
+hipError_t launch_kv_rows_sinks_int8(const KvAttnArgs& a, int mt, hipStream_t st);  // where a.sinks > 0
+hipError_t launch_kv_rows_sinks_e4m3(const KvAttnArgs& a, int mt, hipStream_t st);
 // prompt kernel (kv_prompt.h): how many waves share 32 query rows, rows of a workgroup
 constexpr int kv_prompt_split(int dim) { return dim == 256 ? 2 : 1; }
 constexpr int kv_prompt_rows(int dim, int waves) { return 32 * waves / kv_prompt_split(dim); }
 hipError_t launch_kv_prompt_int8(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_prompt_e4m3(const KvAttnArgs& a, hipStream_t st);
+hipError_t launch_kv_prompt_sinks_int8(const KvAttnArgs& a, hipStream_t st);
+hipError_t launch_kv_prompt_sinks_e4m3(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_prompt_join(const KvAttnArgs& a, hipStream_t st);
 hipError_t launch_kv_join(const KvAttnArgs& a, int mt, int rows, hipStream_t st);  // rows: at least those of any sequence it joins
 

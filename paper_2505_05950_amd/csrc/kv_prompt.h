@@ -22,22 +22,26 @@ struct PromptStage {  // a thread's share of a tile on its way: 16-byte pieces o
     uint4 k[kPieces], v[kPieces];
 };
 
-// The tokens that a tile of rows sees: `n` tiles of 64 from `start` on, cut into chunks as a.prompt_chunk says.
+// The tokens that a tile of rows sees: `n` tiles of 64, cut into chunks as a.prompt_chunk says; the first `sunk` lie at the sequence's
+// start, the others `skip` tokens further on (kv_gap).
 struct PromptRange {
-    int start, n, chunks;
+    int sunk, skip, n, chunks;
 };
+template <bool SINKS>
 __device__ __forceinline__ PromptRange prompt_range(const KvAttnArgs& a, const KvSpan& span, int row0, int rows) {
     const int first = span.pos0 + row0 / a.group, last = span.pos0 + min((row0 + rows - 1) / a.group, span.rows - 1);
     const int end = a.causal ? last + 1 : span.len;  // behind the last token that any row sees
     PromptRange r;
-    r.start = a.window > 0 ? max(0, first - a.window + 1) & ~(kPromptTokens - 1) : 0;
-    r.n = max(0, (end - r.start + kPromptTokens - 1) / kPromptTokens);
+    const KvGap gap = kv_gap<SINKS>(a, a.window > 0 ? max(0, first - a.window + 1) : 0, kPromptTokens);
+    r.sunk = gap.sunk;
+    r.skip = gap.skip;
+    r.n = max(0, (end - r.skip + kPromptTokens - 1) / kPromptTokens);
     r.chunks = min(max(1, (r.n + a.prompt_chunk - 1) / a.prompt_chunk), a.prompt_chunks);
     return r;
 }
 
 // blockIdx.x: KV head, sequence, tile of rows; blockIdx.y: chunk of the tokens (one, unless the card would not be filled)
-template <int D, int FMT, int NW>
+template <int D, int FMT, int NW, bool SINKS>
 __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_prompt_kernel(KvAttnArgs a) {
     // kSplit waves share 32 rows: each forms all of S^T and the weights, and a part of the dims of O^T (whose registers bound the waves)
     constexpr int kThreads = 64 * NW, kPieces = PromptStage<D, NW>::kPieces, kChunks = D / 8;
@@ -55,11 +59,14 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     const KvSpan span = kv_span(a.s, seq);
     const int all_rows = span.rows * a.group, row0 = tile * 32 * kRowWaves;
     if (row0 >= all_rows || span.rows <= a.most_rows) return;
-    const PromptRange range = prompt_range(a, span, row0, 32 * kRowWaves);
+    const PromptRange range = prompt_range<SINKS>(a, span, row0, 32 * kRowWaves);
     const int chunk = blockIdx.y;
     if (chunk >= range.chunks) return;
     // (quotients are formed in vector registers: what all lanes hold alike goes back to scalar ones)
-    const int start = __builtin_amdgcn_readfirstlane(range.start + chunk * a.prompt_chunk * kPromptTokens);
+    // the walk's it-th tile begins at token `start` + 64 it; before the gap `skip` tokens earlier
+    const int skip = SINKS ? __builtin_amdgcn_readfirstlane(range.skip) : 0, sunk = SINKS ? __builtin_amdgcn_readfirstlane(range.sunk - chunk * a.prompt_chunk) : 0;
+    const int start = __builtin_amdgcn_readfirstlane(range.skip + chunk * a.prompt_chunk * kPromptTokens);
+    auto first_token = [&](int it) { return start + it * kPromptTokens - (SINKS && it < sunk ? skip : 0); };
     const int n_tiles = __builtin_amdgcn_readfirstlane(chunk + 1 < range.chunks ? a.prompt_chunk : range.n - chunk * a.prompt_chunk);
     // ---- queries of this wave
     const int rr = row0 + 32 * row_wave + c32, token = min(rr / a.group, span.rows - 1), pos = span.pos0 + token;
@@ -93,7 +100,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     }
     const float row_scale = fabsf(a.scale_log2) * unscale;
     // ---- tokens that the workgroup and this wave's rows see
-    const int first_key = a.window > 0 ? max(0, pos - a.window + 1) : 0, last_key = a.causal ? pos : span.len - 1;
+    const int first_key = kv_first_key<SINKS>(a, pos), last_key = a.causal ? pos : span.len - 1;
     const int w_first = span.pos0 + min((row0 + 32 * row_wave) / a.group, span.rows - 1);
     const int w_last = span.pos0 + min((row0 + 32 * row_wave + 31) / a.group, span.rows - 1);
     // tokens that every row of the wave sees
@@ -112,7 +119,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     int pages = -1;
     auto page_of = [&](int unit) {  // page of the walk's unit-th unit of 32 tokens (0, 1, 2 ... in order), -1 where there is none
         if ((unit & 63) == 0) {
-            const int t = start + (unit + lane) * kKvGroup;
+            const int t = SINKS ? first_token((unit + lane) >> 1) + ((unit + lane) & 1) * kKvGroup : start + (unit + lane) * kKvGroup;
             pages = t < span.len ? kv_page(a.s, a.c, seq, (t / kKvGroup) >> log_upb) : -1;
         }
         return __builtin_amdgcn_readlane(pages, unit & 63);
@@ -120,10 +127,11 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     PromptStage<D, NW> next;
     auto request = [&](int it, const int* page) {  // codes of a tile
         const uint8_t *kp[2], *vp[2];
+        const int t0 = SINKS ? first_token(it) : 0;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const size_t slot = (size_t)max(page[u], 0) * a.c.heads + head;
-            const size_t at = (slot * a.c.block + ((unit0 + 2 * it + u) & ((1 << log_upb) - 1)) * kKvGroup) * D;
+            const size_t at = (slot * a.c.block + (SINKS ? (t0 + kKvGroup * u) & (a.c.block - 1) : ((unit0 + 2 * it + u) & ((1 << log_upb) - 1)) * kKvGroup)) * D;
             kp[u] = scalar_ptr(a.c.k + at);
             vp[u] = scalar_ptr(a.c.v + at);
         }
@@ -149,10 +157,11 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     // nobody's) become zeros: bytes to keep of the two runs of four tokens in a piece, for either unit of the tile.
     uint32_t keep[2][2] = {{~0u, ~0u}, {~0u, ~0u}};
     auto set_keep = [&](int it, const int* page) {
+        const int t0 = first_token(it);
         const int g = tid & 3;  // (pieces of V: g is the fastest index, and a workgroup is a multiple of four threads)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int left = page[u] < 0 ? 0 : span.len - (start + it * kPromptTokens) - kKvGroup * u;
+            const int left = page[u] < 0 ? 0 : span.len - t0 - kKvGroup * u;
             if (left >= kKvGroup) {
                 keep[u][0] = keep[u][1] = ~0u;
             } else {
@@ -230,6 +239,15 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
                 const bool none = (u ? page1 : page0) < 0 || last_key < first_key;
                 const int lo = (none ? t0 + 2 * kPromptTokens : first_key) - (t0 + 32 * u + 4 * h);  // keys from here on, up to `more` behind, are seen
                 const uint32_t more = none ? 0 : last_key - first_key;
+                if (SINKS && t0 < a.sinks) {  // (the same in every lane)
+                    const int seen = none || first_key == 0 ? 0 : a.sinks - (t0 + 32 * u + 4 * h);  // keys before this one are seen too
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int at = 8 * (j >> 2) + (j & 3);
+                        const float x = s[u][j] + poison;
+                        s[u][j] = (uint32_t)(at - lo) > more && at >= seen ? -__builtin_inff() : x;
+                    }
+                } else
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const float x = s[u][j] + poison;
@@ -287,10 +305,10 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
         set_keep(1, page_next);
     }
     for (int it = 0; it < n_tiles; ++it) {
-        const int buf = it & 1, t0 = start + it * kPromptTokens;
+        const int buf = it & 1, t0 = first_token(it);
         page_then[0] = page_of(2 * it + 4), page_then[1] = page_of(2 * it + 5);
         __syncthreads();  // this tile is in LDS, and nobody reads the one before it any more
-        const bool masked = t0 < w_clear_lo || t0 + kPromptTokens - 1 > w_clear_hi || page0 < 0 || page1 < 0 || !(ks[0] * vs[0] + ks[1] * vs[1] > 0.0f);
+        const bool masked = (t0 < w_clear_lo && (!SINKS || t0 + kPromptTokens > a.sinks)) || t0 + kPromptTokens - 1 > w_clear_hi || page0 < 0 || page1 < 0 || !(ks[0] * vs[0] + ks[1] * vs[1] > 0.0f);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) ring[i] = operand(buf, i);
 #pragma unroll
@@ -331,7 +349,8 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
             const int page = page_of(unit);
             if (page < 0) continue;
             const size_t slot = (size_t)page * a.c.heads + head;
-            const uint8_t* k = a.c.k + (slot * a.c.block + ((unit0 + unit) & ((1 << log_upb) - 1)) * kKvGroup + c32) * D + 8 * h;
+            const int t0 = SINKS ? first_token(unit >> 1) + (unit & 1) * kKvGroup : start + unit * kKvGroup;
+            const uint8_t* k = a.c.k + (slot * a.c.block + (SINKS ? t0 & (a.c.block - 1) : ((unit0 + unit) & ((1 << log_upb) - 1)) * kKvGroup) + c32) * D + 8 * h;
             f32x16 x;
 #pragma unroll
             for (int j = 0; j < 16; ++j) x[j] = 0.0f;
@@ -344,12 +363,13 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
             const bool poisoned = !(k_scale == k_scale) || !(v_scale == v_scale);
             const float by = fmaxf(row_scale * k_scale, 0x1p-126f), from = poisoned ? __builtin_nanf("") : off;
             const bool none = last_key < first_key;
-            const int lo = (none ? start + 2 * (unit + 2) * kKvGroup : first_key) - (start + unit * kKvGroup + 4 * h);
+            const int lo = (none ? t0 + 2 * kPromptTokens : first_key) - (t0 + 4 * h), seen = !SINKS || none || first_key == 0 ? 0 : a.sinks - (t0 + 4 * h);
             const uint32_t more = none ? 0 : last_key - first_key;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], by, from));
-                sum += (uint32_t)(8 * (j >> 2) + (j & 3) - lo) > more ? 0.0f : e;
+                const int at = 8 * (j >> 2) + (j & 3);
+                sum += (uint32_t)(at - lo) > more && (!SINKS || at >= seen) ? 0.0f : e;
             }
         }
     }
@@ -380,7 +400,7 @@ __global__ __launch_bounds__(256) void kv_prompt_join_kernel(KvAttnArgs a) {
     const KvSpan span = kv_span(a.s, seq);
     if (token >= span.rows || span.rows <= a.most_rows) return;
     const int head = head_q / a.group, rr = token * a.group + head_q - head * a.group, tile = rr / a.prompt_rows;
-    const PromptRange range = prompt_range(a, span, tile * a.prompt_rows, a.prompt_rows);
+    const PromptRange range = prompt_range<true>(a, span, tile * a.prompt_rows, a.prompt_rows);
     if (range.chunks == 1) return;  // finished where it was formed
     const size_t segment = ((size_t)seq * a.c.heads + head) * a.prompt_tiles + tile;
     join_row<D>(a, a.prompt_parts, segment * a.prompt_chunks * a.prompt_rows + rr - tile * a.prompt_rows, a.prompt_rows, range.chunks, span.row0 + token, head_q);

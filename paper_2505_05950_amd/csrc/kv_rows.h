@@ -47,20 +47,45 @@ struct KvSpread {
     __device__ __forceinline__ bool wide() const { return most - least > 80 << 23; }
 };
 
-// Units of one sequence: `tiles` tiles of rows per KV head, `units` units of 32 tokens from token `lo` on for each.
+// Kernels exist with and without first tokens that stay visible beside a window (SINKS): looking for them in every call costs registers,
+// which at 64 dims took a wave from the prompt kernel and at 192 and 256 spilled a third more.
+// Units of one sequence: `tiles` tiles of rows per KV head, for each `units` units of 32 tokens: the first `sunk` of them lie at the
+// sequence's start, the others `skip` tokens further on than they would without the gap.
+template <bool SINKS>
 struct KvUnits {
     KvSpan span;
-    int tiles, units, lo;
+    int tiles, units, sunk, skip;
+    __device__ __forceinline__ int token(int unit) const { return unit * kKvGroup + (SINKS && unit < sunk ? 0 : skip); }
 };
-template <int MT>
-__device__ __forceinline__ KvUnits kv_units(const KvAttnArgs& a, int seq) {
-    KvUnits u;
+// First tokens of a window that begins at `lo`: from where on `step` tokens at a time are walked, and how many steps lie before the gap.
+// Where the window begins inside the first tokens, or right behind their last step, there is no gap.
+struct KvGap {
+    int sunk, skip;
+};
+template <bool SINKS>
+__device__ __forceinline__ KvGap kv_gap(const KvAttnArgs& a, int lo, int step) {
+    const int start = lo & ~(step - 1);
+    if (!SINKS || a.sinks == 0) return KvGap{0, start};
+    const int sunk = (a.sinks + step - 1) / step;
+    return start <= sunk * step ? KvGap{0, 0} : KvGap{sunk, start - sunk * step};
+}
+// The first token of a row's window; 0 where that lies among the first tokens, or right behind them
+template <bool SINKS>
+__device__ __forceinline__ int kv_first_key(const KvAttnArgs& a, int pos) {
+    const int first = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+    return SINKS && first <= a.sinks ? 0 : first;
+}
+template <int MT, bool SINKS>
+__device__ __forceinline__ KvUnits<SINKS> kv_units(const KvAttnArgs& a, int seq) {
+    KvUnits<SINKS> u;
     u.span = kv_span(a.s, seq);
     if (u.span.rows > a.most_rows) u.span.rows = 0;  // the prompt kernel's
     u.tiles = (u.span.rows * a.group + 16 * MT - 1) / (16 * MT);
-    u.lo = a.window > 0 ? max(0, u.span.pos0 - a.window + 1) & ~(kKvGroup - 1) : 0;
+    const KvGap gap = kv_gap<SINKS>(a, a.window > 0 ? max(0, u.span.pos0 - a.window + 1) : 0, kKvGroup);
+    u.sunk = gap.sunk;
+    u.skip = gap.skip;
     const int end = a.causal ? max(0, u.span.pos0 + u.span.rows) : u.span.len;  // behind the last token that any row sees
-    u.units = max(0, end - u.lo + kKvGroup - 1) / kKvGroup;
+    u.units = max(0, end - u.skip + kKvGroup - 1) / kKvGroup;
     return u;
 }
 // Chunks of a segment: a.chunk units each; the last of the a.chunks that the launch has takes whatever is left.
@@ -188,15 +213,25 @@ __device__ __forceinline__ void unit_scores(f32x4 (&s)[MT][2], const KvQueries<D
             }
         }
 }
-__device__ __forceinline__ void mask_unit(float (&x)[8], int token0, int first_key, int last_key, int g) {
+template <bool SINKS>
+__device__ __forceinline__ void mask_unit(float (&x)[8], int token0, int sinks, int first_key, int last_key, int g) {
     const bool none = last_key < first_key;
     const int lo = (none ? token0 + 2 * kKvGroup : first_key) - (token0 + 4 * g);  // keys from here on, up to `more` behind, are seen
     const uint32_t more = none ? 0 : last_key - first_key;
+    if (SINKS && token0 < sinks) {  // (the same in every lane)
+        const int sunk = none || first_key == 0 ? 0 : sinks - (token0 + 4 * g);  // keys before this one are seen too
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int o = 16 * (j >> 2) + (j & 3);
+            x[j] = (uint32_t)(o - lo) > more && o >= sunk ? -__builtin_inff() : x[j];
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = (uint32_t)(16 * (j >> 2) + (j & 3) - lo) > more ? -__builtin_inff() : x[j];
 }
 
-template <int D, int FMT, int MT>
+template <bool SINKS, int D, int FMT, int MT>
 __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D, MT>& Q, const KvFrag<D, FMT>& f, const KvAttnArgs& a,
                                           bool mask, int token0, int len, const int* first_key, const int* last_key, int g) {
     f32x4 s[MT][2];
@@ -210,7 +245,7 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
         float x[8], mx = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(s[m][j >> 2][j & 3], c, lv);
-        if (mask) mask_unit(x, token0, first_key[m], last_key[m], g);
+        if (mask) mask_unit<SINKS>(x, token0, a.sinks, first_key[m], last_key[m], g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) mx = fmaxf(mx, x[j]);
         mx = quad_max(mx);
@@ -262,7 +297,7 @@ __device__ __forceinline__ void take_unit(KvState<D, MT>& st, const KvQueries<D,
 }
 
 // A unit's weights, summed without V's scale
-template <int D, int FMT, int MT>
+template <bool SINKS, int D, int FMT, int MT>
 __device__ __forceinline__ void sum_unit(KvState<D, MT>& st, const KvQueries<D, MT>& Q, const KvFrag<D, FMT>& f, const KvAttnArgs& a, int token0,
                                          const int* first_key, const int* last_key, int g) {
     f32x4 s[MT][2];
@@ -274,7 +309,7 @@ __device__ __forceinline__ void sum_unit(KvState<D, MT>& st, const KvQueries<D, 
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(s[m][j >> 2][j & 3], c, off);
-        mask_unit(x, token0, first_key[m], last_key[m], g);
+        mask_unit<SINKS>(x, token0, a.sinks, first_key[m], last_key[m], g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) st.sum[m] += __builtin_amdgcn_exp2f(x[j]);
     }
@@ -296,7 +331,7 @@ __device__ __forceinline__ void write_row4(const KvAttnArgs& a, int D, size_t ro
         a.lse[row * a.q_heads + head] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum * (1.0f / kSumUnit))) * 0.6931471805599453f;
 }
 
-template <int D, int FMT, int MT>
+template <int D, int FMT, int MT, bool SINKS>
 __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) void kv_rows_kernel(KvAttnArgs a) {
     constexpr int NW = kRowsWaves, kStride = D + 4;
     __shared__ float slab[NW][16][kStride];
@@ -306,7 +341,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
     const int segments = a.c.heads * a.tiles, seq = __builtin_amdgcn_readfirstlane(blockIdx.x / segments);
     const int seg = blockIdx.x - seq * segments, chunk = blockIdx.y;
     const int head = __builtin_amdgcn_readfirstlane(seg / a.tiles), tile = seg - head * a.tiles, row0 = tile * 16 * MT;
-    const KvUnits w = kv_units<MT>(a, seq);
+    const KvUnits<SINKS> w = kv_units<MT, SINKS>(a, seq);
     const int n_chunks = __builtin_amdgcn_readfirstlane(kv_chunks(a, w.units));
     if (tile >= w.tiles || chunk >= n_chunks) return;
     const int j0 = chunk * a.chunk, j1 = chunk + 1 < n_chunks ? j0 + a.chunk : w.units;
@@ -319,7 +354,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) st.o[m][d] = f32x4{0, 0, 0, 0};
         const int token = min((row0 + 16 * m + r) / a.group, w.span.rows - 1), pos = w.span.pos0 + token;
-        first_key[m] = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+        first_key[m] = kv_first_key<SINKS>(a, pos);
         last_key[m] = a.causal ? pos : w.span.len - 1;
     }
     // units between these need no mask
@@ -328,11 +363,11 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
     const int clear_lo = __builtin_amdgcn_readfirstlane(a.window > 0 ? pos1 - a.window + 1 : 0);
     const int clear_hi = __builtin_amdgcn_readfirstlane(a.causal ? pos0 + 1 : w.span.len);  // first token that some row does not see
     const int end = __builtin_amdgcn_readfirstlane(a.causal ? pos1 + 1 : w.span.len);       // behind the last token that any row sees
-    const int unit0 = w.lo / kKvGroup, log_upb = a.c.block == 32 ? 0 : a.c.block == 64 ? 1 : 2;  // units per block: 1, 2 or 4
+    const int log_upb = a.c.block == 32 ? 0 : a.c.block == 64 ? 1 : 2;  // units per block: 1, 2 or 4
     int pages = -1;
     auto fetch_pages = [&](int j) {  // pages of this wave's next 64 units
         const int mine = j + NW * lane;
-        pages = mine < j1 ? kv_page(a.s, a.c, seq, (unit0 + mine) >> log_upb) : -1;
+        pages = mine < j1 ? kv_page(a.s, a.c, seq, w.token(mine) / kKvGroup >> log_upb) : -1;
     };
     auto page_of = [&](int it) { return __builtin_amdgcn_readlane(pages, it & 63); };
     const int n = (j1 - j0 - wave + NW - 1) / NW;  // units of this wave (may be none)
@@ -342,8 +377,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
     auto request = [&](int next, KvFrag<D, FMT>& f, int& page) {
         const int it = min(next, n - 1), j = j0 + wave + NW * it;
         if ((it & 63) == 0 && it == next) fetch_pages(j);
-        page = w.lo + j * kKvGroup >= end ? -1 : page_of(it);
-        load_unit<D, FMT>(f, a.c, head, page, ((unit0 + j) & ((1 << log_upb) - 1)) * kKvGroup, r, g);
+        const int token0 = w.token(j);
+        page = token0 >= end ? -1 : page_of(it);
+        load_unit<D, FMT>(f, a.c, head, page, token0 & (a.c.block - 1), r, g);
     };
     if (n > 0) {
         request(0, f0, p0);
@@ -352,8 +388,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
         auto step = [&](int it, const KvFrag<D, FMT>& f, int page, KvFrag<D, FMT>& fill, int& fill_page) {
             request(it + 1, fill, fill_page);
             if (it >= n || page < 0) return;
-            const int token0 = w.lo + (j0 + wave + NW * it) * kKvGroup;
-            take_unit<D, FMT, MT>(st, Q, f, a, token0 < clear_lo || token0 + kKvGroup > clear_hi, token0, w.span.len, first_key, last_key, g);
+            const int token0 = w.token(j0 + wave + NW * it);
+            take_unit<SINKS, D, FMT, MT>(st, Q, f, a, (token0 < clear_lo && (!SINKS || token0 + kKvGroup > a.sinks)) || token0 + kKvGroup > clear_hi, token0, w.span.len, first_key, last_key, g);
         };
         for (int it = 0; it < n; it += 2) {
             step(it, f0, p0, f1, p1);
@@ -365,10 +401,10 @@ __global__ __launch_bounds__(64 * kRowsWaves, kv_rows_waves_per_simd(D, MT)) voi
             for (int it = 0; it < n; ++it) {
                 const int j = j0 + wave + NW * it;
                 if ((it & 63) == 0) fetch_pages(j);
-                const int page = w.lo + j * kKvGroup >= end ? -1 : page_of(it);
+                const int token0 = w.token(j), page = token0 >= end ? -1 : page_of(it);
                 if (page < 0) continue;
-                load_unit<D, FMT, false>(f0, a.c, head, page, ((unit0 + j) & ((1 << log_upb) - 1)) * kKvGroup, r, g);
-                sum_unit<D, FMT, MT>(st, Q, f0, a, w.lo + j * kKvGroup, first_key, last_key, g);
+                load_unit<D, FMT, false>(f0, a.c, head, page, token0 & (a.c.block - 1), r, g);
+                sum_unit<SINKS, D, FMT, MT>(st, Q, f0, a, token0, first_key, last_key, g);
             }
         }
     }
@@ -462,7 +498,7 @@ __device__ __forceinline__ void join_row(const KvAttnArgs& a, const KvParts& par
 template <int D, int MT>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a) {
     const int seq = blockIdx.y, head_q = blockIdx.x % a.q_heads, token = blockIdx.x / a.q_heads;
-    const KvUnits w = kv_units<MT>(a, seq);
+    const KvUnits<true> w = kv_units<MT, true>(a, seq);
     if (token >= w.span.rows) return;
     const int n_chunks = kv_chunks(a, w.units);
     if (n_chunks == 1) return;  // finished where it was formed

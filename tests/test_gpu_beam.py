@@ -1,0 +1,212 @@
+"""Beam search's selection against the definition in 64 bits.
+
+Tolerance of c.  A term of the sum, exp(d) with d = x - m <= 0, is formed in binary32: d and d log2(e) are rounded (2^-24 |d| each), the power
+of two is good to 2^-23 of itself; relative to the sum that is at most 2^-23 (1 + mean |d|), and the mean of |d| under the softmax is at
+most log(vocabulary) + 1 < 14: 1.8e-6.  Sums of 8 terms in a chain, four of them in a tree, rounded once more: 11 * 2^-24 = 7e-7.  In
+all below 3e-6 absolute; 5e-6 is allowed.  score_out: that, and half a step of binary32.
+Order: rows are compared by c, so candidates of different rows may change places where their c lie closer than twice that; those of one row
+may not."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_05950_amd as F
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TOL = 5e-6
+DTYPES = {"fp16": torch.float16, "bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def rows64(logits):
+    x = logits.float().cpu().numpy().astype(np.float64)
+    x[np.isnan(x)] = -np.inf
+    return np.minimum(x, np.float64(np.finfo(np.float32).max))
+
+
+def candidates(x, score, done, eos, take):
+    """Of each row of a group: [(c, token)] in the row's order, at most `take`."""
+    out = []
+    for r in range(x.shape[0]):
+        if not score[r] > -np.inf:
+            out.append([])
+        elif done is not None and done[r]:
+            out.append([(float(score[r]), eos)])
+        else:
+            order = np.lexsort((np.arange(x.shape[1]), -x[r]))[:take]
+            m = x[r].max()
+            if m == -np.inf:
+                out.append([])
+                continue
+            log_s = np.log(np.exp(x[r] - m).sum())
+            out.append([(float(score[r]) + ((x[r][t] - m) - log_s), int(t)) for t in order if x[r][t] > -np.inf])
+    return out
+
+
+def check(logits, score, take=None, done=None, eos=-1, exact=False):
+    G, W = score.shape
+    take = W if take is None else take
+    got = F.floe_beam_select(logits, score, take=take, done=done, eos=eos)
+    torch.cuda.synchronize()
+    got_c, parent, token, ended = (t.cpu().numpy() for t in got)
+    x, s = rows64(logits), score.double().cpu().numpy()
+    d = None if done is None else done.cpu().numpy()
+    for g in range(G):
+        rows = candidates(x[g * W:(g + 1) * W], s[g], None if d is None else d[g], eos, take)
+        merged = sorted(((-c, r, i) for r, row in enumerate(rows) for i, (c, _) in enumerate(row)))[:take]
+        n = len(merged)
+        seen = [0] * W
+        for i in range(n):
+            c = -merged[i][0]
+            assert abs(got_c[g, i] - c) <= 2 * TOL + 2.0 ** -24 * abs(c), (g, i, got_c[g, i], c)
+            r = parent[g, i] - g * W
+            assert 0 <= r < W, (g, i, parent[g])
+            # the row's candidates come in the row's order, and this one has the c that it should
+            mine, t = rows[r][seen[r]]
+            seen[r] += 1
+            assert token[g, i] == t and abs(mine - c) <= 2 * TOL, (g, i, token[g, i], t, mine, c)
+            assert abs(got_c[g, i] - mine) <= TOL + 2.0 ** -24 * abs(mine)
+            if exact:
+                assert r == merged[i][1], (g, i, r, merged[i])
+            over = t == eos or (d is not None and d[g][r] > 0)
+            assert ended[g, i] == over
+        assert (got_c[g, n:] == -np.inf).all() and (parent[g, n:] == -1).all() and (token[g, n:] == -1).all() and (ended[g, n:] == 0).all()
+    return got
+
+
+def case(seed, G, W, V, dtype, pad=0, size=2.5):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = (torch.randn((G * W, V + pad), generator=g, device=DEV) * size).to(DTYPES[dtype])
+    return x[:, :V], torch.randn((G, W), generator=g, device=DEV) * 2 - 9
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("G,W,V,take,pad", [(1, 1, 1, 1, 0), (2, 3, 2, 6, 1), (1, 4, 63, 4, 0), (3, 2, 65, 64, 0), (2, 5, 511, 10, 3), (1, 2, 1024, 2, 0), (2, 1, 2049, 1, 7),
+                                            (1, 4, 8191, 4, 0), (1, 3, 8193, 64, 1), (1, 2, 50257, 4, 47), (5, 64, 700, 64, 0), (2, 256, 300, 33, 0), (1, 13, 33333, 26, 1)])
+def test_sizes(dtype, G, W, V, take, pad):
+    logits, score = case(V + take, G, W, V, dtype, pad)
+    check(logits, score, take)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+def test_more_rows_than_the_card_takes_at_a_time(dtype):
+    logits, score = case(1, 300, 5, 9001, dtype)
+    check(logits, score, 10)
+
+
+@pytest.mark.parametrize("take", [1, 8, 64])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", ["same", "ascending", "descending", "steps", "one high", "two values"])
+def test_values_that_are_hard_on_a_threshold(form, dtype, take):
+    """Ties, and values that keep passing what was the best so far."""
+    V, W = 20011, 3
+    i = torch.arange(V, device=DEV, dtype=torch.float64)
+    x = {"same": i * 0 + 1.5, "ascending": i / V * 4, "descending": -i / V * 4, "steps": (i // 500) * 0.25, "one high": (i == 17777) * 30.0, "two values": (i % 2) * 1.0}[form]
+    logits = x.to(DTYPES[dtype]).repeat(W, 1)
+    score = torch.tensor([[-1.0, -1.0, -1.0]], device=DEV)
+    # the rows are the same, and so are their scores: the lower row comes first wherever tokens tie
+    check(logits, score, take, exact=True)
+    check(logits, torch.tensor([[-1.0, -1.25, -0.5]], device=DEV), take)
+
+
+def test_equal_rows_tie_whatever_their_alignment():
+    g = torch.Generator(device=DEV).manual_seed(3)
+    V = 12345
+    row = (torch.randn((V,), generator=g, device=DEV) * 3).half()
+    for stride in (V, V + 1, V + 4):
+        wide = torch.zeros((4, stride), dtype=torch.float16, device=DEV)
+        wide[:, :V] = row
+        check(wide[:, :V], torch.full((1, 4), -3.25, device=DEV), 8, exact=True)
+    flat = torch.zeros((4 * V + 9,), dtype=torch.float16, device=DEV)
+    for shift in (1, 2, 3):  # rows that begin at any multiple of two bytes
+        view = flat[shift:shift + 4 * V].view(4, V)
+        view.copy_(row.expand(4, V))
+        check(view, torch.full((1, 4), -3.25, device=DEV), 8, exact=True)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_values_that_are_not_finite(dtype):
+    logits, score = case(5, 2, 6, 5001, dtype)
+    x = logits.clone()
+    x[0] = -float("inf")                    # a row that offers nothing
+    x[1, 1:] = -float("inf")                # one that offers one token
+    x[2, ::3] = float("nan")
+    x[3, 777] = float("inf")
+    x[4] = float("nan")
+    x[6, [5, 4000]] = float("inf")          # two of them
+    x[7] = torch.finfo(x.dtype).min         # the lowest value of the type is a value
+    x[8, ::2] = -float("inf")
+    check(x, score, 12)
+    check(x, score, 64)
+    only = torch.full_like(x, -float("inf"))
+    check(only, score, 6)
+
+
+def test_zeros_of_either_sign_are_equal():
+    x = torch.zeros((2, 3000), device=DEV)
+    x[:, ::2] = -0.0
+    check(x, torch.zeros((1, 2), device=DEV), 5, exact=True)
+
+
+def test_scores_that_count_and_scores_that_do_not():
+    logits, score = case(6, 3, 4, 2000, "fp16")
+    inf = float("inf")
+    score = torch.tensor([[0.0, -inf, -inf, -inf], [-inf] * 4, [float("nan"), -5.0, -1e30, -2.0]], device=DEV)  # a first step, a dead group
+    check(logits, score, 8)
+    assert F.floe_beam_select(logits, score)[1][1].tolist() == [-1] * 4
+
+
+def test_rows_that_are_done_offer_their_end_alone():
+    logits, score = case(7, 4, 5, 3001, "bf16")
+    done = torch.zeros((4, 5), dtype=torch.uint8, device=DEV)
+    done[0, 2] = done[1] = 1
+    done[2, 0] = 255
+    score[3, 3], done[3, 3] = -float("inf"), 1
+    score[0, 2] = 3.0
+    logits = logits.clone()
+    logits[2] = float("nan")  # is not read
+    logits[9, 7] = 40.0       # a row that ends now
+    for take in (3, 5, 10):
+        got = check(logits, score, take, done, eos=7)
+        assert got[1][0, 0] == 2 and got[2][0, 0] == 7 and got[3][0, 0] == 1 and got[0][0, 0] == 3.0
+        assert got[1][1, :3].tolist() == (torch.sort(score[1], descending=True, stable=True).indices[:3] + 5).tolist()
+    check(logits, score, 5, None, eos=7)
+    check(logits, score, 5, None, eos=-1)
+
+
+def test_outputs_and_workspace_of_the_caller():
+    logits, score = case(8, 2, 4, 9999, "fp32")
+    want = F.floe_beam_select(logits, score, take=6)
+    outs = [torch.empty_like(t) for t in want]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    got = F.floe_beam_select(logits, score, take=6, score_out=outs[0], parent=outs[1], token=outs[2], done_out=outs[3],
+                             workspace=torch.empty((1 << 20,), dtype=torch.uint8, device=DEV), stream=stream)
+    torch.cuda.synchronize()
+    assert all(a is b and torch.equal(a, c) for a, b, c in zip(got, outs, want))
+    with pytest.raises(F.FloeError) as err:
+        F.floe_beam_select(logits, score, take=6, workspace=torch.empty((600,), dtype=torch.uint8, device=DEV))
+    assert err.value.status == -4
+
+
+def test_a_captured_selection_reads_what_is_there_at_each_replay():
+    logits, score = case(9, 3, 4, 40000, "fp16")
+    logits, done = logits.clone(), torch.zeros((3, 4), dtype=torch.uint8, device=DEV)
+    call = lambda: F.floe_beam_select(logits, score, take=4, done=done, eos=3)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for i in range(5):
+        x, s = case(20 + i, 3, 4, 40000, "fp16")
+        logits.copy_(x)
+        score.copy_(s)
+        done.copy_(torch.rand((3, 4), device=DEV) < 0.3)
+        graph.replay()
+        want = check(logits, score, 4, done, 3)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), i
