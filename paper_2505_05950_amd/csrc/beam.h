@@ -26,10 +26,10 @@ struct BeamArgs {
 };
 
 struct BeamCut {
-    int slices, slice;
+    int slices, slice, loads;  // loads: of sixteen bytes per lane and tile
 };
 BeamCut beam_cut(int rows, int vocab, int dtype);  // dtype: floe_dtype
-hipError_t launch_beam_rows(const BeamArgs& a, int dtype, hipStream_t st);
+hipError_t launch_beam_rows(const BeamArgs& a, int dtype, int loads, hipStream_t st);
 hipError_t launch_beam_groups(const BeamArgs& a, hipStream_t st);
 
 }  // namespace floe

@@ -50,7 +50,7 @@ int floe_beam_select(const floe_beam* b, const void* logits, int64_t row_stride,
     const BeamArgs a{logits, row_stride, score, done, b->groups, b->beams, b->vocab, b->take, b->eos, cut.slices, cut.slice, score_out, parent, token,
                      done_out, reinterpret_cast<float*>(base), reinterpret_cast<uint64_t*>(base + w.best)};
     hipStream_t st = (hipStream_t)stream;
-    FLOE_LAUNCH(FLOE_KERNEL_BEAM_ROWS, st, launch_beam_rows(a, b->dtype, st));
+    FLOE_LAUNCH(FLOE_KERNEL_BEAM_ROWS, st, launch_beam_rows(a, b->dtype, cut.loads, st));
     FLOE_LAUNCH(FLOE_KERNEL_BEAM_GROUPS, st, launch_beam_groups(a, st));
     return FLOE_OK;
 }

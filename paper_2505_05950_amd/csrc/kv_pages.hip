@@ -84,52 +84,178 @@ __device__ __forceinline__ void meet_in_memory() {  // what the workgroup wrote 
     __threadfence();
 }
 
+// Pages with several names among up to 1024 blocks: the first sequence of the call that writes each, and how many do (open addressing,
+// half full at most).
+constexpr int kNames = 2 * kReserveThreads;
+struct NameTable {
+    int page[kNames], first[kNames], writers[kNames];
+    __device__ __forceinline__ int place(int e) {
+        int at = ((uint32_t)e * 2654435761u) >> 21;
+        static_assert(kNames == 1 << 11, "the hash has eleven bits");
+        for (;;) {
+            const int was = atomicCAS(&page[at], -1, e);
+            if (was == -1 || was == e) return at;
+            at = (at + 1) & (kNames - 1);
+        }
+    }
+};
+
+// A step's call (up to 1024 sequences that touch up to 1024 blocks in all) keeps a block per thread in registers from the first look at the
+// tables to the last; what its phases exchange lies in LDS.  Others go over their blocks once per phase, with scratch in memory.
 __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(KvPool p, KvTable t, const int32_t* len, const int32_t* cu, int32_t* pairs,
                                                                      int32_t* missing, KvReserveScratch w) {
-    __shared__ int waves[kReserveWaves], ends[kReserveThreads], blocks[kReserveThreads];
-    const int tid = threadIdx.x;
-    // Every block that the call's rows touch, in order: f(sequence, block, slot) by threads that take 1024 neighbouring ones at a time
-    // (f is called by all threads together; slot < 0: none).  Returns how many blocks lie behind the table.
-    auto each_block = [&](auto&& f) {
-        int outside = 0;
-        for (int s0 = 0; s0 < t.n_seqs; s0 += kReserveThreads) {
-            const int s = s0 + tid;
-            int n = 0, first = 0;
-            if (s < t.n_seqs) {
-                const int L = length_of(len, s), rows = min(max(cu[s + 1] - cu[s], 0), kKvMaxLen);
-                if (rows > 0) {
-                    first = L / p.block;
-                    const int behind = (int)(((uint32_t)L + rows - 1) / p.block) + 1;
-                    n = max(0, min(behind, t.max_blocks) - first);
-                    outside = min(outside + (behind - first - n), 1 << 20);  // (1024 threads' stay within 31 bits)
+    __shared__ int waves[kReserveWaves], ends[kReserveThreads], blocks[kReserveThreads], begun[kReserveThreads];
+    __shared__ NameTable names;
+    __shared__ KvRequest wanted[kReserveThreads];
+    __shared__ int replaced[kReserveThreads];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // ---- free pages, from the lowest on: a wave looks at 1024 neighbouring ones in a round of 16384
+    constexpr int kRound = 16 * kReserveThreads;
+    struct Pages {
+        int4 names[4];
+    };
+    auto page_of = [&](int round, int u) { return round * kRound + wave * 1024 + u * 256 + lane * 4; };
+    auto look = [&](int round) {
+        Pages g;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int page = page_of(round, u);
+            g.names[u] = make_int4(1, 1, 1, 1);
+            if (page + 3 < p.n_pages) {
+                g.names[u] = *reinterpret_cast<const int4*>(p.refs + page);
+            } else {
+                if (page < p.n_pages) g.names[u].x = p.refs[page];
+                if (page + 1 < p.n_pages) g.names[u].y = p.refs[page + 1];
+                if (page + 2 < p.n_pages) g.names[u].z = p.refs[page + 2];
+            }
+        }
+        return g;
+    };
+    Pages pages = look(0);
+    // serve(rank, page): gives the request of that rank the page; returns how many requests were served
+    auto hand_out = [&](int requests, auto&& serve) {
+        int served = 0;
+        const int rounds = (p.n_pages + kRound - 1) / kRound;
+        for (int round = 0; round < rounds && served < requests; ++round) {
+            const Pages now = pages;
+            if (round + 1 < rounds) pages = look(round + 1);
+            int n[4], before[4], mine = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                n[u] = (now.names[u].x <= 0) + (now.names[u].y <= 0) + (now.names[u].z <= 0) + (now.names[u].w <= 0);
+                const int up_to = wave_inclusive_scan(n[u]);
+                before[u] = mine + up_to - n[u];
+                mine += __builtin_amdgcn_readlane(up_to, 63);
+            }
+            __syncthreads();  // (`waves` may still be read)
+            if (lane == 0) waves[wave] = mine;
+            __syncthreads();
+            int rank0 = served;
+#pragma unroll
+            for (int k = 0; k < kReserveWaves; ++k) {
+                const int x = waves[k];
+                rank0 += k < wave ? x : 0;
+                served += x;
+            }
+            if (mine == 0 || rank0 >= requests) continue;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int here[4] = {now.names[u].x, now.names[u].y, now.names[u].z, now.names[u].w};
+                int rank = rank0 + before[u];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (here[j] > 0) continue;
+                    if (rank < requests) serve(rank, page_of(round, u) + j);
+                    ++rank;
                 }
             }
-            int total;
-            const int before = workgroup_scan(n, waves, total);
+        }
+        return min(served, requests);
+    };
+    auto entry = [&](int s, int b) { return t.at + (size_t)s * t.max_blocks + b; };
+    // a sequence's first block, how many of its blocks lie inside the table, and how many behind it
+    auto blocks_of = [&](int s, int& first, int& outside) {
+        first = outside = 0;
+        if (s >= t.n_seqs) return 0;
+        const int L = length_of(len, s), rows = min(max(cu[s + 1] - cu[s], 0), kKvMaxLen);
+        if (rows == 0) return 0;
+        first = L / p.block;
+        const int behind = (int)(((uint32_t)L + rows - 1) / p.block) + 1, n = max(0, min(behind, t.max_blocks) - first);
+        outside = behind - first - n;
+        return n;
+    };
+    // the sequence among a batch of 1024 (whose blocks end at ends[]) that a block belongs to
+    auto owner = [&](int slot) {
+        int lo = 0, hi = kReserveThreads - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (ends[mid] > slot) hi = mid;
+            else lo = mid + 1;
+        }
+        return lo;
+    };
+    for (int s = tid; s < t.n_seqs; s += kReserveThreads) pairs[2 * s] = pairs[2 * s + 1] = -1;
+    if (t.n_seqs <= kReserveThreads) {
+        for (int i = tid; i < kNames; i += kReserveThreads) names.page[i] = -1, names.first[i] = 0x7fffffff, names.writers[i] = 0;
+        int first, outside, total;
+        const int n = blocks_of(tid, first, outside), before = workgroup_scan(n, waves, total);
+        ends[tid] = before + n;
+        blocks[tid] = first - before;
+        begun[tid] = tid < t.n_seqs && length_of(len, tid) % p.block != 0 ? first : -1;  // the block that holds tokens already
+        __syncthreads();
+        if (total <= kReserveThreads) {
+            const bool there = tid < total;
+            const int s = there ? owner(tid) : 0, b = blocks[s] + tid;
+            const int e = there ? *entry(s, b) : -1;
+            const int count = is_page(p, e) ? p.refs[e] : 0;
+            const bool shared = is_page(p, e) && count > 1;
+            bool need = there && !is_page(p, e);
+            int place = 0;
+            if (shared) {
+                place = names.place(e);
+                atomicMin(&names.first[place], s);
+                atomicAdd(&names.writers[place], 1);
+            }
+            if (__syncthreads_or(shared) && shared) need = !(names.first[place] == s && count <= names.writers[place]);
+            int requests;
+            const int rank = workgroup_scan(need, waves, requests);
+            if (need) wanted[rank] = KvRequest{s, b}, replaced[rank] = shared ? e : -1;
+            int all_outside;
+            workgroup_scan(min(outside, 1 << 20), waves, all_outside);  // (1024 threads' stay within 31 bits)
+            const int served = hand_out(requests, [&](int rank, int page) {
+                const KvRequest r = wanted[rank];
+                const int old = replaced[rank];
+                *entry(r.seq, r.block) = page;
+                p.refs[page] = 1;
+                if (old < 0) return;
+                add_ref(p, old, -1);
+                if (begun[r.seq] == r.block) pairs[2 * r.seq] = old, pairs[2 * r.seq + 1] = page;
+            });
+            if (tid == 0) *missing = requests - served + all_outside;
+            return;
+        }
+    }
+    // Every block that the call's rows touch, in order: f(sequence, block, whether there is one) by threads that take 1024 neighbouring ones at
+    // a time (f is called by all threads together).  Returns how many blocks of this thread's sequences lie behind the table.
+    auto each_block = [&](auto&& f) {
+        int all_outside = 0;
+        for (int s0 = 0; s0 < t.n_seqs; s0 += kReserveThreads) {
+            int first, outside, total;
+            const int n = blocks_of(s0 + tid, first, outside), before = workgroup_scan(n, waves, total);
+            all_outside = min(all_outside + outside, 1 << 20);
             __syncthreads();  // (the arrays may still be read)
             ends[tid] = before + n;
             blocks[tid] = first - before;
             __syncthreads();
             for (int slot0 = 0; slot0 < total; slot0 += kReserveThreads) {
-                const int slot = slot0 + tid;
-                int lo = 0;
-                if (slot < total) {
-                    int hi = kReserveThreads - 1;
-                    while (lo < hi) {  // the first sequence whose blocks end behind the slot
-                        const int mid = (lo + hi) >> 1;
-                        if (ends[mid] > slot) hi = mid;
-                        else lo = mid + 1;
-                    }
-                }
-                f(s0 + lo, blocks[lo] + slot, slot < total);
+                const int slot = slot0 + tid, s = slot < total ? owner(slot) : 0;
+                f(s0 + s, blocks[s] + slot, slot < total);
             }
         }
-        return outside;
+        return all_outside;
     };
-    auto entry = [&](int s, int b) { return t.at + (size_t)s * t.max_blocks + b; };
     // pages with more than one name
     bool any = false;
-    for (int s = tid; s < t.n_seqs; s += kReserveThreads) pairs[2 * s] = pairs[2 * s + 1] = -1;
     const int mine_outside = each_block([&](int s, int b, bool there) {
         if (!there) return;
         const int e = *entry(s, b);
@@ -160,8 +286,8 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(KvPool p, K
             const int e = *entry(s, b);
             need = 1;
             if (is_page(p, e)) {
-                const int names = p.refs[e];
-                need = names > 1 && !(load_agent(w.first + e) == s && names <= load_agent(w.writers + e));
+                const int count = p.refs[e];
+                need = count > 1 && !(load_agent(w.first + e) == s && count <= load_agent(w.writers + e));
             }
         }
         int all;
@@ -170,40 +296,17 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(KvPool p, K
         requests += all;
     });
     meet_in_memory();
-    // free pages, from the lowest on
-    int served = 0;
-    for (int p0 = 0; p0 < p.n_pages && served < requests; p0 += 4 * kReserveThreads) {
-        const int page = p0 + 4 * tid;
-        int4 names = make_int4(1, 1, 1, 1);
-        if (page + 3 < p.n_pages) {
-            names = *reinterpret_cast<const int4*>(p.refs + page);
-        } else {
-            if (page < p.n_pages) names.x = p.refs[page];
-            if (page + 1 < p.n_pages) names.y = p.refs[page + 1];
-            if (page + 2 < p.n_pages) names.z = p.refs[page + 2];
-        }
-        const int here[4] = {names.x <= 0, names.y <= 0, names.z <= 0, names.w <= 0};
-        int all;
-        int rank = served + workgroup_scan(here[0] + here[1] + here[2] + here[3], waves, all);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (!here[j]) continue;
-            if (rank < requests) {
-                const KvRequest r = w.list[rank];
-                int32_t* at = entry(r.seq, r.block);
-                const int old = *at, L = length_of(len, r.seq);
-                if (is_page(p, old)) {
-                    add_ref(p, old, -1);
-                    if (r.block == L / p.block && L % p.block != 0) pairs[2 * r.seq] = old, pairs[2 * r.seq + 1] = page + j;
-                }
-                *at = page + j;
-                p.refs[page + j] = 1;
-            }
-            ++rank;
-        }
-        served += all;
-    }
-    if (tid == 0) *missing = max(0, requests - served) + outside;
+    const int served = hand_out(requests, [&](int rank, int page) {
+        const KvRequest r = w.list[rank];
+        int32_t* at = entry(r.seq, r.block);
+        const int old = *at, L = length_of(len, r.seq);
+        *at = page;
+        p.refs[page] = 1;
+        if (!is_page(p, old)) return;
+        add_ref(p, old, -1);
+        if (r.block == L / p.block && L % p.block != 0) pairs[2 * r.seq] = old, pairs[2 * r.seq + 1] = page;
+    });
+    if (tid == 0) *missing = requests - served + outside;
 }
 
 // ---- compact
