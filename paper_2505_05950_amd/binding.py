@@ -781,14 +781,46 @@ def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows:
 
 
 # ---- the pages of such caches: handed out, shared, given back, packed, copied (include/floe.h)
-def _i32(t, shape, device, name):
-    """Address of a contiguous int32 tensor of this shape (None: any size) on the pool's GPU."""
-    if t.dtype is not torch.int32 or not t.is_contiguous() or len(t.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        want = "".join(f"[{'n' if n is None else n}]" for n in shape)
-        raise ValueError(f"{name}: expected contiguous int32 {want}, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+_page_functions = None
+
+
+def _page_calls():
+    """The pages' functions with plain integers for addresses (these calls are bound by the host too)."""
+    global _page_functions
+    if _page_functions is None:
+        lib, vp, i32, sz = load(), C.c_void_p, C.c_int, C.c_size_t
+        reorder, reserve, trim, compact, copy = (lib["floe_kv_" + n] for n in ("reorder", "reserve", "trim", "compact", "copy_pages"))
+        reorder.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, i32, vp]
+        reserve.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp, sz, vp]
+        trim.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp]
+        compact.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, sz, vp]
+        copy.argtypes = [vp, i32, vp, i32, vp]
+        _page_functions = reorder, reserve, trim, compact, copy
+    return _page_functions
+
+
+def _i32(t, shape, device: int, name: str) -> int:
+    """Address of a contiguous int32 tensor of this shape on the pool's GPU."""
+    if t.dtype is torch.int32 and t.shape == shape and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
     if t.get_device() != device:
         raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: expected contiguous int32 {tuple(shape)}, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
+
+
+def _new(like, shape, dtype, stream):
+    return like.new_empty(shape, dtype=dtype) if stream is None else _empty(shape, dtype, like.device, stream)
+
+
+# Scratch of a call: the caller's, or its own from the pool of its stream, given back when the call has been enqueued.  No two calls, and no two
+# captured graphs, share an array that outlives them.  Returns the tensor, an address and the bytes behind it.
+def _scratch(given, like, nbytes: int, stream):
+    if given is None:
+        given = _new(like, (nbytes + 256,), torch.uint8, stream)
+        return (given, given.data_ptr(), nbytes) if given.data_ptr() % 256 == 0 else (given, *_aligned_ptr(given))
+    if given.get_device() != like.get_device():
+        raise ValueError(f"workspace: on {given.device}, expected {like.device}")
+    return (given, *_aligned_ptr(given))
 
 
 class KVPool:
@@ -805,78 +837,75 @@ class KVPool:
             raise ValueError(f"KVPool: refs is a contiguous int32 tensor [{self.n_pages}], got {refs.dtype} {tuple(refs.shape)}")
         self.refs, self._device = refs, refs.get_device()
         self._c = _KvPool(self.n_pages, self.block, refs.data_ptr())
+        self._at = C.addressof(self._c)
+        self._reserve_bytes = None
 
-    def _table(self, table, name="table", stream=None):
+    def _table(self, table, stream):
+        """Address and sizes of a table, on the device that launches."""
+        shape = table.shape
+        if len(shape) != 2:
+            raise ValueError(f"table: expected int32 [sequences][blocks], got {tuple(shape)}")
         _launches_on(self._device, stream, "the pool")
-        return _i32(table, (None, None), self._device, name)
+        return _i32(table, shape, self._device, "table"), shape[0], shape[1]
 
 
-# Address and size of a call's scratch.  Where the caller brings none, the call takes its own from the pool of its stream and gives it back
-# when it has been enqueued: no two calls, and no two captured graphs, share an array that outlives them.
-def _scratch(workspace, device: int):
-    if workspace.get_device() != device:
-        raise ValueError(f"workspace: on {workspace.device}, expected cuda:{device}")
-    return _aligned_ptr(workspace)
-
-
-def _out_i32(t, shape, device, name, stream):
+def _given_or_new(t, shape, pool, like, name, stream):
     if t is None:
-        return _empty(shape, torch.int32, torch.device("cuda", device), stream)
-    _i32(t, shape, device, name)
+        return _new(like, shape, torch.int32, stream)
+    _i32(t, shape, pool._device, name)
     return t
 
 
 def floe_kv_reorder(pool: KVPool, table, length, parent, table_out=None, length_out=None, stream=None):
     """Sequence i takes over the pages and the length of sequence parent[i] (outside the table: none); `table` is no longer in use afterwards.
     Returns (table_out, length_out)."""
-    at = pool._table(table, stream=stream)
-    (n, blocks), dev = table.shape, pool._device
-    length_at, parent_at = _i32(length, (n,), dev, "length"), _i32(parent, (None,), dev, "parent")
-    m = parent.shape[0]
-    table_out = _out_i32(table_out, (m, blocks), dev, "table_out", stream)
-    length_out = _out_i32(length_out, (m,), dev, "length_out", stream)
-    _check(load().floe_kv_reorder(C.byref(pool._c), at, length_at, n, blocks, parent_at, table_out.data_ptr(), length_out.data_ptr(), m, _stream(stream)),
-           "floe_kv_reorder")
+    at, n, blocks = pool._table(table, stream)
+    m = parent.numel()
+    length_at, parent_at = _i32(length, (n,), pool._device, "length"), _i32(parent, (m,), pool._device, "parent")
+    table_out = _given_or_new(table_out, (m, blocks), pool, table, "table_out", stream)
+    length_out = _given_or_new(length_out, (m,), pool, table, "length_out", stream)
+    rc = _page_calls()[0](pool._at, at, length_at, n, blocks, parent_at, table_out.data_ptr(), length_out.data_ptr(), m, _stream(stream))
+    if rc:
+        _check(rc, "floe_kv_reorder")
     return table_out, length_out
 
 
 def floe_kv_reserve(pool: KVPool, table, length, cu_rows, pairs=None, missing=None, workspace=None, stream=None):
     """Gives every block that an append of cu_rows behind `length` tokens writes to a page that only its sequence names.  Returns (pairs
     int32 [sequences][2], what floe_kv_copy_pages has to copy before the append; missing int32 [1], blocks that got no page)."""
-    at = pool._table(table, stream=stream)
-    (n, blocks), dev = table.shape, pool._device
-    length_at, cu_at = _i32(length, (n,), dev, "length"), _i32(cu_rows, (n + 1,), dev, "cu_rows")
-    pairs, missing = _out_i32(pairs, (n, 2), dev, "pairs", stream), _out_i32(missing, (1,), dev, "missing", stream)
-    lib = load()
-    if workspace is None:
-        workspace = _workspace(lib.floe_kv_reserve_workspace_bytes(C.byref(pool._c)), table.device, stream)
-    wp, wn = _scratch(workspace, dev)
-    _check(lib.floe_kv_reserve(C.byref(pool._c), at, length_at, cu_at, n, blocks, pairs.data_ptr(), missing.data_ptr(), wp, wn, _stream(stream)),
-           "floe_kv_reserve")
+    at, n, blocks = pool._table(table, stream)
+    length_at, cu_at = _i32(length, (n,), pool._device, "length"), _i32(cu_rows, (n + 1,), pool._device, "cu_rows")
+    pairs = _given_or_new(pairs, (n, 2), pool, table, "pairs", stream)
+    missing = _given_or_new(missing, (1,), pool, table, "missing", stream)
+    if pool._reserve_bytes is None:
+        pool._reserve_bytes = load().floe_kv_reserve_workspace_bytes(C.byref(pool._c))
+    workspace, wp, wn = _scratch(workspace, table, pool._reserve_bytes, stream)
+    rc = _page_calls()[1](pool._at, at, length_at, cu_at, n, blocks, pairs.data_ptr(), missing.data_ptr(), wp, wn, _stream(stream))
+    if rc:
+        _check(rc, "floe_kv_reserve")
     return pairs, missing
 
 
 def floe_kv_trim(pool: KVPool, table, length, window: int = 0, sinks: int = 0, stream=None):
     """Gives back the blocks of `table` that no query behind `length` tokens sees: all behind the end, and with a window those before it
     that hold none of the first `sinks` tokens."""
-    at = pool._table(table, stream=stream)
-    n, blocks = table.shape
-    _check(load().floe_kv_trim(C.byref(pool._c), at, _i32(length, (n,), pool._device, "length"), n, blocks, int(sinks), int(window), _stream(stream)),
-           "floe_kv_trim")
+    at, n, blocks = pool._table(table, stream)
+    rc = _page_calls()[2](pool._at, at, _i32(length, (n,), pool._device, "length"), n, blocks, sinks, window, _stream(stream))
+    if rc:
+        _check(rc, "floe_kv_trim")
 
 
 def floe_kv_compact(pool: KVPool, table, max_moves: int = None, pairs=None, page_map=None, workspace=None, stream=None):
     """Moves the highest used pages to the lowest free ones (max_moves at most: as many as there are pages by default); the pool and `table`
     follow at once.  Returns (pairs int32 [max_moves][2], what floe_kv_copy_pages has to copy; page_map int32 [n_pages], where each page went)."""
-    at = pool._table(table, stream=stream)
-    (n, blocks), dev = table.shape, pool._device
+    at, n, blocks = pool._table(table, stream)
     moves = pool.n_pages if max_moves is None else int(max_moves)
-    pairs, page_map = _out_i32(pairs, (moves, 2), dev, "pairs", stream), _out_i32(page_map, (pool.n_pages,), dev, "page_map", stream)
-    lib = load()
-    if workspace is None:
-        workspace = _workspace(lib.floe_kv_compact_workspace_bytes(C.byref(pool._c), moves), table.device, stream)
-    wp, wn = _scratch(workspace, dev)
-    _check(lib.floe_kv_compact(C.byref(pool._c), at, n, blocks, pairs.data_ptr(), moves, page_map.data_ptr(), wp, wn, _stream(stream)), "floe_kv_compact")
+    pairs = _given_or_new(pairs, (moves, 2), pool, table, "pairs", stream)
+    page_map = _given_or_new(page_map, (pool.n_pages,), pool, table, "page_map", stream)
+    workspace, wp, wn = _scratch(workspace, table, load().floe_kv_compact_workspace_bytes(C.byref(pool._c), moves), stream)
+    rc = _page_calls()[3](pool._at, at, n, blocks, pairs.data_ptr(), moves, page_map.data_ptr(), wp, wn, _stream(stream))
+    if rc:
+        _check(rc, "floe_kv_compact")
     return pairs, page_map
 
 
@@ -889,13 +918,37 @@ def floe_kv_copy_pages(caches, pairs, stream=None):
     if any(c._device != dev for c in caches):
         raise ValueError("floe_kv_copy_pages: the caches are on one device")
     _launches_on(dev, stream, "the cache")
-    at = _i32(pairs, (None, 2), dev, "pairs")
-    packed = b"".join([bytes(c._c) for c in caches])
-    _check(load().floe_kv_copy_pages(packed, len(caches), at, pairs.shape[0], _stream(stream)), "floe_kv_copy_pages")
+    n = pairs.shape[0] if pairs.dim() else 0
+    at = _i32(pairs, (n, 2), dev, "pairs")
+    rc = _page_calls()[4](b"".join([bytes(c._c) for c in caches]), len(caches), at, n, _stream(stream))
+    if rc:
+        _check(rc, "floe_kv_copy_pages")
 
 
 # ---- beam search
 _BEAM_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+_BEAM_FIELDS = struct.Struct("6i")
+assert _BEAM_FIELDS.size == C.sizeof(_Beam)
+_beam_functions = None
+
+
+def _beam_calls():
+    global _beam_functions
+    if _beam_functions is None:
+        lib, vp, packed = load(), C.c_void_p, C.c_char_p
+        select, need = lib["floe_beam_select"], lib["floe_beam_workspace_bytes"]
+        select.argtypes = [packed, vp, C.c_int64, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        need.argtypes, need.restype = [packed], C.c_size_t
+        _beam_functions = select, need
+    return _beam_functions
+
+
+def _beam_out(t, shape, dtype, like, name, stream):
+    if t is None:
+        return _new(like, shape, dtype, stream)
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {like.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
 
 
 def floe_beam_select(logits, score, take: int = None, done=None, eos: int = -1, score_out=None, parent=None, token=None, done_out=None, workspace=None,
@@ -903,29 +956,26 @@ def floe_beam_select(logits, score, take: int = None, done=None, eos: int = -1, 
     """The `take` best continuations (as many as beams by default) of each group: logits [groups * beams][vocab] fp16, bf16 or fp32 (rows may lie
     anywhere), score fp32 [groups][beams], done uint8 [groups][beams] (rows that offer `eos` alone).  Returns (score, parent, token, done), all
     [groups][take]; parent is the row that a continuation comes from, -1 behind the last one (include/floe.h)."""
-    if logits.dtype not in _BEAM_DTYPES or logits.dim() != 2 or score.dim() != 2 or logits.shape[0] != score.numel():
-        raise ValueError(f"floe_beam_select: logits fp16, bf16 or fp32 [groups * beams][vocab], got {logits.dtype} {tuple(logits.shape)}, score {tuple(score.shape)}")
-    groups, beams = score.shape
-    rows, vocab = logits.shape
-    if (vocab > 1 and rows and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < vocab):
-        raise ValueError(f"floe_beam_select: the logits of a row lie one behind the other, and rows apart (strides {logits.stride()})")
-    dev = logits.get_device()
-    _launches_on(dev, stream, "floe_beam_select: logits")
-    for t, kind, name in ((score, torch.float32, "score"), (done, torch.uint8, "done")):
-        if t is not None and (t.dtype is not kind or t.shape != (groups, beams) or not t.is_contiguous() or t.get_device() != dev):
-            raise ValueError(f"{name}: expected contiguous {kind} {(groups, beams)} on {logits.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    shape = (groups, beams if take is None else int(take))
-    outs = []
-    for t, kind, name in ((score_out, torch.float32, "score_out"), (parent, torch.int32, "parent"), (token, torch.int32, "token"), (done_out, torch.uint8, "done_out")):
-        if t is None:
-            t = _empty(shape, kind, logits.device, stream)
-        elif t.dtype is not kind or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
-            raise ValueError(f"{name}: expected contiguous {kind} {shape} on {logits.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        outs.append(t)
-    b, lib = _Beam(groups, beams, vocab, shape[1], _BEAM_DTYPES[logits.dtype], int(eos)), load()
-    if workspace is None:
-        workspace = _workspace(lib.floe_beam_workspace_bytes(C.byref(b)), logits.device, stream)
-    wp, wn = _scratch(workspace, dev)
-    _check(lib.floe_beam_select(C.byref(b), logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, score.data_ptr(), None if done is None else done.data_ptr(),
-                                *(t.data_ptr() for t in outs), wp, wn, _stream(stream)), "floe_beam_select")
-    return tuple(outs)
+    kind, shape, sizes = _BEAM_DTYPES.get(logits.dtype), logits.shape, score.shape
+    if kind is None or len(shape) != 2 or len(sizes) != 2 or shape[0] != sizes[0] * sizes[1]:
+        raise ValueError(f"floe_beam_select: logits fp16, bf16 or fp32 [groups * beams][vocab], got {logits.dtype} {tuple(shape)}, score {tuple(sizes)}")
+    (rows, vocab), (groups, beams), strides = shape, sizes, logits.stride()
+    if (vocab > 1 and rows and strides[1] != 1) or (rows > 1 and strides[0] < vocab):
+        raise ValueError(f"floe_beam_select: the logits of a row lie one behind the other, and rows apart (strides {strides})")
+    _launches_on(logits.get_device(), stream, "floe_beam_select: logits")
+    for t, dtype, name in ((score, torch.float32, "score"), (done, torch.uint8, "done")):
+        if t is not None:
+            _beam_out(t, sizes, dtype, logits, name, stream)
+    take = beams if take is None else take
+    out = groups, take
+    score_out = _beam_out(score_out, out, torch.float32, logits, "score_out", stream)
+    parent = _beam_out(parent, out, torch.int32, logits, "parent", stream)
+    token = _beam_out(token, out, torch.int32, logits, "token", stream)
+    done_out = _beam_out(done_out, out, torch.uint8, logits, "done_out", stream)
+    b, (call, need) = _BEAM_FIELDS.pack(groups, beams, vocab, take, kind, eos), _beam_calls()
+    workspace, wp, wn = _scratch(workspace, logits, need(b), stream)
+    rc = call(b, logits.data_ptr(), strides[0] if rows > 1 else vocab, score.data_ptr(), None if done is None else done.data_ptr(), score_out.data_ptr(),
+              parent.data_ptr(), token.data_ptr(), done_out.data_ptr(), wp, wn, _stream(stream))
+    if rc:
+        _check(rc, "floe_beam_select")
+    return score_out, parent, token, done_out

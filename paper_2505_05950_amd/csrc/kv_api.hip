@@ -107,7 +107,7 @@ void cut_prompts(AttnPlan& w, int dim, int64_t heads, int64_t rows, int64_t tile
 }
 // The most tokens that `rows` rows of a sequence see: their windows, the first tokens, and what the steps of the walk take beside both
 int64_t keys_of(const floe_attention* a, int sinks, int64_t rows) {
-    const int64_t seen = a->window + rows + (sinks ? sinks + 63 : 0);
+    const int64_t seen = a->window + rows + (sinks ? sinks + 127 : 0);
     return a->window > 0 && seen < a->max_len ? seen : a->max_len;
 }
 AttnPlan attn_plan(const floe_kv_cache* c, const floe_kv_seqs* s, const floe_attention* a, int sinks) {

@@ -22,8 +22,9 @@ struct PromptStage {  // a thread's share of a tile on its way: 16-byte pieces o
     uint4 k[kPieces], v[kPieces];
 };
 
-// The tokens that a tile of rows sees: `n` tiles of 64, cut into chunks as a.prompt_chunk says; the first `sunk` lie at the sequence's
-// start, the others `skip` tokens further on (kv_gap).
+// The tokens that a tile of rows sees: `n` tiles of 64, cut into chunks as a.prompt_chunk says.  Where some row's window begins behind the
+// first tokens that every row sees, the first `sunk` tiles are those tokens' and the others begin `skip` tokens further on (or sooner: the
+// tile in which the first tokens end may come twice, once for them and once for what lies behind): each tile has one interval per row then.
 struct PromptRange {
     int sunk, skip, n, chunks;
 };
@@ -32,10 +33,16 @@ __device__ __forceinline__ PromptRange prompt_range(const KvAttnArgs& a, const K
     const int first = span.pos0 + row0 / a.group, last = span.pos0 + min((row0 + rows - 1) / a.group, span.rows - 1);
     const int end = a.causal ? last + 1 : span.len;  // behind the last token that any row sees
     PromptRange r;
-    const KvGap gap = kv_gap<SINKS>(a, a.window > 0 ? max(0, first - a.window + 1) : 0, kPromptTokens);
-    r.sunk = gap.sunk;
-    r.skip = gap.skip;
-    r.n = max(0, (end - r.skip + kPromptTokens - 1) / kPromptTokens);
+    int start = a.window > 0 ? max(0, first - a.window + 1) : 0;
+    r.sunk = 0;
+    if (SINKS && a.sinks > 0) {
+        const bool apart = last - a.window + 1 > a.sinks;
+        r.sunk = apart ? (min(a.sinks, end) + kPromptTokens - 1) / kPromptTokens : 0;
+        start = apart ? max(start, a.sinks) : 0;
+    }
+    start &= ~(kPromptTokens - 1);
+    r.skip = start - r.sunk * kPromptTokens;
+    r.n = r.sunk + max(0, (end - start + kPromptTokens - 1) / kPromptTokens);
     r.chunks = min(max(1, (r.n + a.prompt_chunk - 1) / a.prompt_chunk), a.prompt_chunks);
     return r;
 }
@@ -64,6 +71,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     if (chunk >= range.chunks) return;
     // (quotients are formed in vector registers: what all lanes hold alike goes back to scalar ones)
     // the walk's it-th tile begins at token `start` + 64 it; before the gap `skip` tokens earlier
+    const bool apart = SINKS && __builtin_amdgcn_readfirstlane(range.sunk) > 0;
     const int skip = SINKS ? __builtin_amdgcn_readfirstlane(range.skip) : 0, sunk = SINKS ? __builtin_amdgcn_readfirstlane(range.sunk - chunk * a.prompt_chunk) : 0;
     const int start = __builtin_amdgcn_readfirstlane(range.skip + chunk * a.prompt_chunk * kPromptTokens);
     auto first_token = [&](int it) { return start + it * kPromptTokens - (SINKS && it < sunk ? skip : 0); };
@@ -100,11 +108,13 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     }
     const float row_scale = fabsf(a.scale_log2) * unscale;
     // ---- tokens that the workgroup and this wave's rows see
-    const int first_key = kv_first_key<SINKS>(a, pos), last_key = a.causal ? pos : span.len - 1;
+    // (in a tile of the first tokens: 0 .. sinks - 1, or up to the row's own)
+    const int window_key = a.window > 0 ? max(0, pos - a.window + 1) : 0, last_key = a.causal ? pos : span.len - 1;
+    const int first_key = !SINKS ? window_key : apart ? max(window_key, a.sinks) : 0;
     const int w_first = span.pos0 + min((row0 + 32 * row_wave) / a.group, span.rows - 1);
     const int w_last = span.pos0 + min((row0 + 32 * row_wave + 31) / a.group, span.rows - 1);
     // tokens that every row of the wave sees
-    const int w_clear_lo = __builtin_amdgcn_readfirstlane(a.window > 0 ? w_last - a.window + 1 : 0);
+    const int w_clear_lo = __builtin_amdgcn_readfirstlane(!SINKS ? (a.window > 0 ? w_last - a.window + 1 : 0) : apart ? max(w_last - a.window + 1, a.sinks) : 0);
     const int w_clear_hi = __builtin_amdgcn_readfirstlane(a.causal ? w_first : span.len - 1);
 
     f32x16 o[kOut];
@@ -230,24 +240,16 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
         }
     };
     // mask and running maximum of the tile
-    auto maximum = [&](int t0, bool masked) {
+    auto maximum = [&](int t0, bool masked, bool of_first) {
         if (masked) {
+            const int from = SINKS && of_first ? 0 : first_key, to = SINKS && of_first ? min(last_key, a.sinks - 1) : last_key;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const bool poisoned = !(ks[u] == ks[u]) || !(vs[u] == vs[u]);  // a NaN scale: NaN for whoever sees a token, nothing for others
                 const float poison = poisoned ? __builtin_nanf("") : 0.0f;
-                const bool none = (u ? page1 : page0) < 0 || last_key < first_key;
-                const int lo = (none ? t0 + 2 * kPromptTokens : first_key) - (t0 + 32 * u + 4 * h);  // keys from here on, up to `more` behind, are seen
-                const uint32_t more = none ? 0 : last_key - first_key;
-                if (SINKS && t0 < a.sinks) {  // (the same in every lane)
-                    const int seen = none || first_key == 0 ? 0 : a.sinks - (t0 + 32 * u + 4 * h);  // keys before this one are seen too
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const int at = 8 * (j >> 2) + (j & 3);
-                        const float x = s[u][j] + poison;
-                        s[u][j] = (uint32_t)(at - lo) > more && at >= seen ? -__builtin_inff() : x;
-                    }
-                } else
+                const bool none = (u ? page1 : page0) < 0 || to < from;
+                const int lo = (none ? t0 + 2 * kPromptTokens : from) - (t0 + 32 * u + 4 * h);  // keys from here on, up to `more` behind, are seen
+                const uint32_t more = none ? 0 : to - from;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const float x = s[u][j] + poison;
@@ -308,7 +310,8 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
         const int buf = it & 1, t0 = first_token(it);
         page_then[0] = page_of(2 * it + 4), page_then[1] = page_of(2 * it + 5);
         __syncthreads();  // this tile is in LDS, and nobody reads the one before it any more
-        const bool masked = (t0 < w_clear_lo && (!SINKS || t0 + kPromptTokens > a.sinks)) || t0 + kPromptTokens - 1 > w_clear_hi || page0 < 0 || page1 < 0 || !(ks[0] * vs[0] + ks[1] * vs[1] > 0.0f);
+        const bool of_first = SINKS && it < sunk;
+        const bool masked = (of_first ? t0 + kPromptTokens > a.sinks : t0 < w_clear_lo) || t0 + kPromptTokens - 1 > w_clear_hi || page0 < 0 || page1 < 0 || !(ks[0] * vs[0] + ks[1] * vs[1] > 0.0f);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) ring[i] = operand(buf, i);
 #pragma unroll
@@ -328,7 +331,7 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(0);
         request(min(it + 2, n_tiles - 1), page_then);
-        maximum(t0, masked);
+        maximum(t0, masked, of_first);
         weights(0);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
@@ -362,14 +365,15 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
             const float k_scale = gloadf(a.c.k_scale + slot), v_scale = gloadf(a.c.v_scale + slot);
             const bool poisoned = !(k_scale == k_scale) || !(v_scale == v_scale);
             const float by = fmaxf(row_scale * k_scale, 0x1p-126f), from = poisoned ? __builtin_nanf("") : off;
-            const bool none = last_key < first_key;
-            const int lo = (none ? t0 + 2 * kPromptTokens : first_key) - (t0 + 4 * h), seen = !SINKS || none || first_key == 0 ? 0 : a.sinks - (t0 + 4 * h);
-            const uint32_t more = none ? 0 : last_key - first_key;
+            const bool of_first = SINKS && (unit >> 1) < sunk;
+            const int from_key = of_first ? 0 : first_key, to_key = of_first ? min(last_key, a.sinks - 1) : last_key;
+            const bool none = to_key < from_key;
+            const int lo = (none ? t0 + 2 * kPromptTokens : from_key) - (t0 + 4 * h);
+            const uint32_t more = none ? 0 : to_key - from_key;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], by, from));
-                const int at = 8 * (j >> 2) + (j & 3);
-                sum += (uint32_t)(at - lo) > more && (!SINKS || at >= seen) ? 0.0f : e;
+                sum += (uint32_t)(8 * (j >> 2) + (j & 3) - lo) > more ? 0.0f : e;
             }
         }
     }

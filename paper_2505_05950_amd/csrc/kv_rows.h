@@ -47,8 +47,8 @@ struct KvSpread {
     __device__ __forceinline__ bool wide() const { return most - least > 80 << 23; }
 };
 
-// Kernels exist with and without first tokens that stay visible beside a window (SINKS): looking for them in every call costs registers,
-// which at 64 dims took a wave from the prompt kernel and at 192 and 256 spilled a third more.
+// Kernels exist with and without first tokens that stay visible beside a window (SINKS): to look for them in every call costs the rows kernel
+// up to eight registers, at 64 dims a wave of four.
 // Units of one sequence: `tiles` tiles of rows per KV head, for each `units` units of 32 tokens: the first `sunk` of them lie at the
 // sequence's start, the others `skip` tokens further on than they would without the gap.
 template <bool SINKS>
@@ -57,18 +57,6 @@ struct KvUnits {
     int tiles, units, sunk, skip;
     __device__ __forceinline__ int token(int unit) const { return unit * kKvGroup + (SINKS && unit < sunk ? 0 : skip); }
 };
-// First tokens of a window that begins at `lo`: from where on `step` tokens at a time are walked, and how many steps lie before the gap.
-// Where the window begins inside the first tokens, or right behind their last step, there is no gap.
-struct KvGap {
-    int sunk, skip;
-};
-template <bool SINKS>
-__device__ __forceinline__ KvGap kv_gap(const KvAttnArgs& a, int lo, int step) {
-    const int start = lo & ~(step - 1);
-    if (!SINKS || a.sinks == 0) return KvGap{0, start};
-    const int sunk = (a.sinks + step - 1) / step;
-    return start <= sunk * step ? KvGap{0, 0} : KvGap{sunk, start - sunk * step};
-}
 // The first token of a row's window; 0 where that lies among the first tokens, or right behind them
 template <bool SINKS>
 __device__ __forceinline__ int kv_first_key(const KvAttnArgs& a, int pos) {
@@ -81,9 +69,14 @@ __device__ __forceinline__ KvUnits<SINKS> kv_units(const KvAttnArgs& a, int seq)
     u.span = kv_span(a.s, seq);
     if (u.span.rows > a.most_rows) u.span.rows = 0;  // the prompt kernel's
     u.tiles = (u.span.rows * a.group + 16 * MT - 1) / (16 * MT);
-    const KvGap gap = kv_gap<SINKS>(a, a.window > 0 ? max(0, u.span.pos0 - a.window + 1) : 0, kKvGroup);
-    u.sunk = gap.sunk;
-    u.skip = gap.skip;
+    u.sunk = 0;
+    u.skip = a.window > 0 ? max(0, u.span.pos0 - a.window + 1) & ~(kKvGroup - 1) : 0;
+    if (SINKS && a.sinks > 0) {  // where the first window begins inside the first tokens, or right behind their last unit, there is no gap
+        const int sunk = (a.sinks + kKvGroup - 1) / kKvGroup;
+        const bool apart = u.skip > sunk * kKvGroup;
+        u.sunk = apart ? sunk : 0;
+        u.skip = apart ? u.skip - sunk * kKvGroup : 0;
+    }
     const int end = a.causal ? max(0, u.span.pos0 + u.span.rows) : u.span.len;  // behind the last token that any row sees
     u.units = max(0, end - u.skip + kKvGroup - 1) / kKvGroup;
     return u;
