@@ -31,6 +31,7 @@ struct KvReserveScratch {
 hipError_t launch_kv_reserve(const KvPool& p, const KvTable& t, const int32_t* len, const int32_t* cu_rows, int32_t* pairs, int32_t* missing,
                              const KvReserveScratch& w, hipStream_t st);
 
+constexpr int kFewPages = 8192, kFewEntries = 8192;  // pools and tables that one workgroup packs (eight pages per thread of 1024)
 constexpr int kCompactChunk = 1024;  // pages that a workgroup of the compaction looks at
 struct KvCompactScratch {
     int32_t* count;         // [chunks]: used pages

@@ -401,6 +401,92 @@ __global__ __launch_bounds__(kThreads) void kv_compact_move_kernel(KvPool p, KvT
     }
 }
 
+// The same by one workgroup, for pools of up to kFewPages: eight pages per thread in registers, places in LDS.  us, one launch / three, with
+// 1000 and 8000 entries: 100 pages 4.8 5.8 / 6.0, 2000 5.7 6.7 / 8.0, 8000 7.1 8.2 / 8.8; 32000 entries and 8000 pages 12.0 / 8.8.
+__global__ __launch_bounds__(kReserveThreads) void kv_compact_few_kernel(KvPool p, KvTable t, int32_t* pairs, int n_pairs, int32_t* page_map) {
+    __shared__ uint16_t place[kFewPages], high[kFewPages / 2], low[kFewPages / 2];
+    __shared__ int waves[kReserveWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto page_of = [&](int u, int j) { return wave * 512 + u * 256 + lane * 4 + j; };
+    int names[2][4], n[2], before[2], mine = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        int4 x = make_int4(0, 0, 0, 0);
+        const int page = page_of(u, 0);
+        if (page + 3 < p.n_pages) {
+            x = *reinterpret_cast<const int4*>(p.refs + page);
+        } else {
+            if (page < p.n_pages) x.x = p.refs[page];
+            if (page + 1 < p.n_pages) x.y = p.refs[page + 1];
+            if (page + 2 < p.n_pages) x.z = p.refs[page + 2];
+        }
+        names[u][0] = x.x, names[u][1] = x.y, names[u][2] = x.z, names[u][3] = x.w;
+        n[u] = (x.x > 0) + (x.y > 0) + (x.z > 0) + (x.w > 0);
+        const int up_to = wave_inclusive_scan(n[u]);
+        before[u] = mine + up_to - n[u];
+        mine += __builtin_amdgcn_readlane(up_to, 63);
+    }
+    if (lane == 0) waves[wave] = mine;
+    __syncthreads();
+    int rank0 = 0, used = 0;
+#pragma unroll
+    for (int k = 0; k < kReserveWaves; ++k) {
+        const int x = waves[k];
+        rank0 += k < wave ? x : 0;
+        used += x;
+    }
+    int below_mine = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) below_mine += names[u][j] > 0 && page_of(u, j) < used;
+    int below;
+    workgroup_scan(below_mine, waves, below);
+    const int moves = min(used - below, n_pairs);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        int rank = rank0 + before[u];  // used pages before the next one
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int page = page_of(u, j);
+            if (page < p.n_pages) {
+                place[page] = (uint16_t)page;
+                if (names[u][j] > 0 && page >= used && used - 1 - rank < moves) high[used - 1 - rank] = (uint16_t)page;
+                if (names[u][j] <= 0 && page < used && page - rank < moves) low[page - rank] = (uint16_t)page;
+            }
+            rank += names[u][j] > 0;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        int rank = rank0 + before[u];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int page = page_of(u, j), i = used - 1 - rank;
+            if (page < p.n_pages && names[u][j] > 0 && page >= used && i < moves) {
+                const int to = low[i];
+                place[page] = (uint16_t)to;
+                p.refs[to] = names[u][j];
+                p.refs[page] = 0;
+            }
+            rank += names[u][j] > 0;
+        }
+    }
+    for (int i = tid; i < n_pairs; i += kReserveThreads) {
+        pairs[2 * i] = i < moves ? high[i] : -1;
+        pairs[2 * i + 1] = i < moves ? low[i] : -1;
+    }
+    __syncthreads();
+    for (int i = tid; i < p.n_pages; i += kReserveThreads) page_map[i] = place[i];
+    const int entries = t.n_seqs * t.max_blocks;
+#pragma unroll 4
+    for (int i = tid; i < entries; i += kReserveThreads) {
+        const int e = t.at[i], to = is_page(p, e) ? place[e] : e;
+        if (to != e) t.at[i] = to;
+    }
+}
+
 // ---- copy
 __global__ __launch_bounds__(kThreads) void kv_copy_pages_kernel(KvCopyArgs a) {
     const int pair = blockIdx.x / a.pieces, piece = blockIdx.x - pair * a.pieces, tid = threadIdx.x;
@@ -449,6 +535,10 @@ hipError_t launch_kv_reserve(const KvPool& p, const KvTable& t, const int32_t* l
 }
 hipError_t launch_kv_compact(const KvPool& p, const KvTable& t, int32_t* pairs, int n_pairs, int32_t* page_map, const KvCompactScratch& w,
                              hipStream_t st) {
+    if (p.n_pages <= kFewPages && (int64_t)t.n_seqs * t.max_blocks <= kFewEntries) {
+        kv_compact_few_kernel<<<dim3(1), dim3(kReserveThreads), 0, st>>>(p, t, pairs, n_pairs, page_map);
+        return hipGetLastError();
+    }
     const int chunks = (p.n_pages + kCompactChunk - 1) / kCompactChunk;
     kv_compact_count_kernel<<<dim3(chunks), dim3(kThreads), 0, st>>>(p, pairs, n_pairs, w);
     kv_compact_choose_kernel<<<dim3(chunks), dim3(kThreads), 0, st>>>(p, n_pairs, w);
