@@ -812,20 +812,9 @@ def _new(like, shape, dtype, stream):
     return like.new_empty(shape, dtype=dtype) if stream is None else _empty(shape, dtype, like.device, stream)
 
 
-# Scratch of a call: the caller's, or its own from the pool of its stream, given back when the call has been enqueued.  No two calls, and no two
-# captured graphs, share an array that outlives them.  Returns the tensor, an address and the bytes behind it.
-def _scratch(given, like, nbytes: int, stream):
-    if given is None:
-        given = _new(like, (nbytes + 256,), torch.uint8, stream)
-        return (given, given.data_ptr(), nbytes) if given.data_ptr() % 256 == 0 else (given, *_aligned_ptr(given))
-    if given.get_device() != like.get_device():
-        raise ValueError(f"workspace: on {given.device}, expected {like.device}")
-    return (given, *_aligned_ptr(given))
-
-
 class KVPool:
     """How many table entries name each of a cache's pages: refs int32 [n_pages], zeros at the start (refs=: an array that exists).  One
-    pool serves the caches of all layers, which share their tables."""
+    pool serves the caches of all layers, which share their tables.  Its calls are ordered by the caller, captured ones too."""
 
     def __init__(self, n_pages: int, block: int = 64, refs=None, device="cuda"):
         self.n_pages, self.block = int(n_pages), int(block)
@@ -838,7 +827,18 @@ class KVPool:
         self.refs, self._device = refs, refs.get_device()
         self._c = _KvPool(self.n_pages, self.block, refs.data_ptr())
         self._at = C.addressof(self._c)
-        self._reserve_bytes = None
+        # scratch of the calls: those on one pool are ordered by the caller, as they change its counts
+        lib, at = load(), C.byref(self._c)
+        nbytes = max(lib.floe_kv_reserve_workspace_bytes(at), lib.floe_kv_compact_workspace_bytes(at, self.n_pages))
+        self._scratch = _workspace(nbytes, refs.device)
+        self._scratch_at = _aligned_ptr(self._scratch)
+
+    def _workspace(self, given):
+        if given is None:
+            return self._scratch_at
+        if given.get_device() != self._device:
+            raise ValueError(f"workspace: on {given.device}, the pool is on {self.refs.device}")
+        return _aligned_ptr(given)
 
     def _table(self, table, stream):
         """Address and sizes of a table, on the device that launches."""
@@ -877,9 +877,7 @@ def floe_kv_reserve(pool: KVPool, table, length, cu_rows, pairs=None, missing=No
     length_at, cu_at = _i32(length, (n,), pool._device, "length"), _i32(cu_rows, (n + 1,), pool._device, "cu_rows")
     pairs = _given_or_new(pairs, (n, 2), pool, table, "pairs", stream)
     missing = _given_or_new(missing, (1,), pool, table, "missing", stream)
-    if pool._reserve_bytes is None:
-        pool._reserve_bytes = load().floe_kv_reserve_workspace_bytes(C.byref(pool._c))
-    workspace, wp, wn = _scratch(workspace, table, pool._reserve_bytes, stream)
+    wp, wn = pool._workspace(workspace)
     rc = _page_calls()[1](pool._at, at, length_at, cu_at, n, blocks, pairs.data_ptr(), missing.data_ptr(), wp, wn, _stream(stream))
     if rc:
         _check(rc, "floe_kv_reserve")
@@ -902,7 +900,7 @@ def floe_kv_compact(pool: KVPool, table, max_moves: int = None, pairs=None, page
     moves = pool.n_pages if max_moves is None else int(max_moves)
     pairs = _given_or_new(pairs, (moves, 2), pool, table, "pairs", stream)
     page_map = _given_or_new(page_map, (pool.n_pages,), pool, table, "page_map", stream)
-    workspace, wp, wn = _scratch(workspace, table, load().floe_kv_compact_workspace_bytes(C.byref(pool._c), moves), stream)
+    wp, wn = pool._workspace(workspace)
     rc = _page_calls()[3](pool._at, at, n, blocks, pairs.data_ptr(), moves, page_map.data_ptr(), wp, wn, _stream(stream))
     if rc:
         _check(rc, "floe_kv_compact")
@@ -941,6 +939,17 @@ def _beam_calls():
         need.argtypes, need.restype = [packed], C.c_size_t
         _beam_functions = select, need
     return _beam_functions
+
+
+# Scratch of a call: the caller's, or its own from the pool of its stream, given back when the call has been enqueued.  No two calls, and no two
+# captured graphs, share an array that outlives them.  Returns the tensor, an address and the bytes behind it.
+def _scratch(given, like, nbytes: int, stream):
+    if given is None:
+        given = _new(like, (nbytes + 256,), torch.uint8, stream)
+        return (given, given.data_ptr(), nbytes) if given.data_ptr() % 256 == 0 else (given, *_aligned_ptr(given))
+    if given.get_device() != like.get_device():
+        raise ValueError(f"workspace: on {given.device}, expected {like.device}")
+    return (given, *_aligned_ptr(given))
 
 
 def _beam_out(t, shape, dtype, like, name, stream):
