@@ -393,6 +393,7 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
     __shared__ uint8_t row_kind[kBeamRows];  // 0: offers nothing, 1: tokens, 2: its end
     __shared__ __attribute__((aligned(16))) uint32_t set_top[kGroupThreads / 8];
     __shared__ double list_c[kGroupList];
+    __shared__ __attribute__((aligned(16))) uint32_t list_key[kGroupList];  // of c in binary32; 0 behind the last
     __shared__ uint64_t list_e[kGroupList];
     __shared__ int16_t list_row[kGroupList];
     __shared__ uint32_t bar_order;
@@ -479,6 +480,7 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
             if (kind == 1) entries(r, w - r * parts, first_entry(r, w - r * parts), [&](uint64_t e) { f(r, value(r, e), e); });
         }
     };
+    list_key[tid] = 0;
     if (tid == 0) listed = 0;
     double bar = threshold();
 #pragma unroll 1
@@ -486,7 +488,7 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
         each([&](int r, double c, uint64_t e) {
             if (!(c >= bar)) return;
             const int at = atomicAdd(&listed, 1);
-            if (at < kGroupList) list_c[at] = c, list_e[at] = e, list_row[at] = (int16_t)r;
+            if (at < kGroupList) list_c[at] = c, list_e[at] = e, list_row[at] = (int16_t)r, list_key[at] = order_of((float)c);
         });
         __syncthreads();
         if (listed <= kGroupThreads / 4) break;
@@ -497,6 +499,7 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
         const double higher = threshold();
         if (!(higher > bar)) break;  // ties: what was listed stays
         bar = higher;
+        list_key[tid] = 0;
         if (tid == 0) listed = 0;
         __syncthreads();
     }
@@ -510,20 +513,21 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
         if (a.done_out) a.done_out[out + rank] = token == a.eos || row_kind[row] == 2;
     };
     if (listed <= kGroupList) {
-        // eight neighbouring threads count what comes before a candidate
+        // eight neighbouring threads count what comes before a candidate, by c in binary32 and, where others have the same, in full
         for (int i = tid >> 3; i < n; i += kGroupThreads / 8) {
-            const double c = list_c[i];
+            const uint32_t key = list_key[i];
             int rank = 0, same = 0;
-#pragma unroll 4
-            for (int k = tid & 7; k < n; k += 8) {
-                const double x = list_c[k];
-                rank += x > c;
-                same += x == c;
+            for (int k = 4 * (tid & 7); k < n; k += 32) {
+                const uint4 x = *reinterpret_cast<const uint4*>(&list_key[k]);
+                rank += (x.x > key) + (x.y > key) + (x.z > key) + (x.w > key);
+                same += (x.x == key) + (x.y == key) + (x.z == key) + (x.w == key);
             }
+            const double c = list_c[i];
             const uint64_t e = list_e[i];
             const int row = list_row[i];
-            if (same > (int)((i & 7) == (tid & 7)))  // others than itself
-                for (int k = tid & 7; k < n; k += 8) rank += list_c[k] == c && before(c, list_row[k], list_e[k], c, row, e);
+            if (same > (int)(((i >> 2) & 7) == (tid & 7)))  // others than itself
+                for (int k0 = 4 * (tid & 7); k0 < n; k0 += 32)
+                    for (int k = k0; k < k0 + 4; ++k) rank += list_key[k] == key && before(list_c[k], list_row[k], list_e[k], c, row, e);
             rank = eight_sum(rank);
             if ((tid & 7) == 0 && rank < a.take) write(rank, c, row, e);
         }
