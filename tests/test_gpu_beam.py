@@ -210,3 +210,26 @@ def test_a_captured_selection_reads_what_is_there_at_each_replay():
         want = check(logits, score, 4, done, 3)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+
+
+@pytest.mark.parametrize("dtype,bits", [("fp32", 0x7f800001), ("bf16", 0x7f81), ("fp16", 0x7c01)])
+def test_signalling_nans_count_as_nothing_too(dtype, bits):
+    logits, score = case(31, 1, 3, 4100, dtype)
+    x = logits.clone()
+    raw = x.view(torch.int32 if dtype == "fp32" else torch.int16)
+    raw[0, ::5] = bits
+    raw[1] = bits
+    raw[1, 4099] = 0
+    check(x, score, 6)
+
+
+@pytest.mark.parametrize("take", [3, 16, 17, 64])
+def test_few_rows_that_have_all_of_the_best(take):
+    """One beam that counts among many, and beams whose scores lie far apart: what reaches the first threshold is far more than is taken."""
+    logits, score = case(32, 3, 100, 3000, "fp32")
+    score[0] = score[0] * 0 - 50.0
+    score[0, 71] = 0.0
+    score[1] = -torch.arange(100, device=DEV) * 3.0
+    check(logits, score, take)
+    same = logits[:1].expand(300, 3000).contiguous()  # and rows that are all the same: ties across a hundred of them
+    check(same, torch.zeros((3, 100), device=DEV), take, exact=True)

@@ -296,3 +296,40 @@ def test_two_streams_with_pools_of_their_own():
             ref.reserve(table, length, [3] * 50)
             length = [x + 3 for x in length]
         same(pool, t, ref, table)
+
+
+@pytest.mark.parametrize("n_seqs,rows", [(40, 1200), (1024, 1), (1025, 1), (1024, 33), (16, 2048), (16, 2049), (2, 16384)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_reserve_on_both_sides_of_what_a_workgroup_keeps_in_registers(n_seqs, rows, shared):
+    """Up to 1024 sequences with up to 1024 blocks in all, and more of either; blocks that are begun, shared by some or by all of their writers."""
+    P, width = 32, -(-(rows + 60) // 32) + 1
+    length = [(13 * s) % 60 for s in range(n_seqs)]
+    table, page = [[-1] * width for _ in range(n_seqs)], 0
+    for s in range(n_seqs):
+        if shared and s % 3:
+            length[s], table[s] = length[s - 1], list(table[s - 1])
+            continue
+        for b in range(-(-length[s] // P)):
+            table[s][b] = page
+            page += 1
+    ref = Pool(page + n_seqs * (rows // P + 2), P).count(table)
+    count = [rows if not shared or s % 5 else 0 for s in range(n_seqs)]
+    pool, t = device_pool(ref), i32(table)
+    pairs, missing = F.floe_kv_reserve(pool, t, i32(length), cu_of(count))
+    want = ref.reserve(table, length, count)
+    same(pool, t, ref, table)
+    assert pairs.tolist() == want[0] and missing.item() == want[1] == 0
+
+
+@pytest.mark.parametrize("n_seqs,block,most,spare,moves", [(20, 32, 500, 9000, None), (700, 32, 400, 50, None), (700, 32, 400, 50, 77), (30, 32, 300, 7800, 3)])
+def test_compact_on_both_sides_of_what_one_workgroup_takes(n_seqs, block, most, spare, moves):
+    ref, table, length, rng = state(9, n_seqs, block, most, spare, 0.02)
+    gone = [n if rng.random() < 0.5 else 0 for n in length]
+    pool, t = device_pool(ref), i32(table)
+    F.floe_kv_trim(pool, t, i32(gone))
+    ref.trim(table, gone, 0, 0)
+    moves = 400 if moves is None else moves
+    pairs, where = F.floe_kv_compact(pool, t, moves)
+    want_pairs, want_where = ref.compact(table, moves)
+    same(pool, t, ref, table)
+    assert pairs.tolist() == want_pairs and where.tolist() == want_where
