@@ -176,6 +176,11 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     float bar = -kLargest;
     int n = 0;           // entries of the wave's list
     auto load = [&](int t0, BeamTile<LOADS>& f) {
+        if (t0 + kTile <= end) {  // a whole tile: requests without conditions
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) f.raw[u] = gload16_any(logits + (size_t)(t0 + (u * kWave + lane) * E) * kSize);
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
             const int i = t0 + (u * kWave + lane) * E;
@@ -185,11 +190,12 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     float x[LOADS][E], most[LOADS];  // a tile's values, and the largest of each sixteen bytes
     auto values = [&](int t0, const BeamTile<LOADS>& f) {
 #pragma unroll
-        for (int u = 0; u < LOADS; ++u) {
-            const int i = t0 + (u * kWave + lane) * E;
-            if (i + E <= end) {
-                unpack<DTYPE>(f.raw[u], x[u]);
-            } else {
+        for (int u = 0; u < LOADS; ++u) unpack<DTYPE>(f.raw[u], x[u]);
+        if (t0 + kTile > end) {
+#pragma unroll
+            for (int u = 0; u < LOADS; ++u) {
+                const int i = t0 + (u * kWave + lane) * E;
+                if (i + E <= end) continue;
 #pragma unroll
                 for (int e = 0; e < E; ++e) x[u][e] = i + e < end ? logit<DTYPE>(logits, i + e) : -kInf;
             }

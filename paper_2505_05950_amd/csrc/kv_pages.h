@@ -42,7 +42,7 @@ struct KvCompactScratch {
 hipError_t launch_kv_compact(const KvPool& p, const KvTable& t, int32_t* pairs, int n_pairs, int32_t* page_map, const KvCompactScratch& w,
                              hipStream_t st);
 
-constexpr int kCopyLoads = 2, kCopyBytes = kCopyLoads * 16 * 256;  // of a thread, sixteen bytes each, and of a workgroup
+constexpr int kCopyLoads = 4, kCopyBytes = kCopyLoads * 16 * 256;  // of a thread, sixteen bytes each, and of a workgroup
 inline int kv_copy_pieces(int bytes) { return 2 * ((bytes + kCopyBytes - 1) / kCopyBytes); }  // of a page's K and V
 constexpr int kCopyCaches = 64;  // of a launch
 struct KvCopyArgs {

@@ -488,9 +488,9 @@ __global__ __launch_bounds__(kReserveThreads) void kv_compact_few_kernel(KvPool 
 }
 
 // ---- copy
-// Bound by bytes, mostly those written (a page that goes to several places is read from L2).  Small workgroups, and stores that leave the caches
-// to the sources: us of a whole step of 128 beams with eight layers (82 MB written), of a fork and its end (252 MB), of packing and what is around
-// it (472 MB): 16 KB a workgroup 54 97 182, with such stores 52 87 174; 8 KB 52 98 187, with them 46 88 182; 4 KB with them 50 86 208.
+// Bound by bytes, mostly those written (a page that goes to several places is read from L2).  Stores leave the caches to the sources: us of a
+// whole step of 128 beams with eight layers (82 MB written), of a fork and its end (252 MB), of packing and what is around it (472 MB), a
+// workgroup taking 16 KB 46 70 177, with plain stores 52 80 182; 4 KB 50 87 197, 8 KB 46 77 182, 32 KB 51 74 179.
 __global__ __launch_bounds__(kThreads) void kv_copy_pages_kernel(KvCopyArgs a) {
     const int pair = blockIdx.x / a.pieces, piece = blockIdx.x - pair * a.pieces, tid = threadIdx.x;
     const int from = a.pairs[2 * pair], to = a.pairs[2 * pair + 1];
@@ -501,16 +501,15 @@ __global__ __launch_bounds__(kThreads) void kv_copy_pages_kernel(KvCopyArgs a) {
     const int at0 = (is_v ? piece - half : piece) * kCopyBytes;
     const uint8_t* src = (is_v ? c.v : c.k) + (size_t)from * a.bytes;
     uint8_t* dst = (is_v ? c.v : c.k) + (size_t)to * a.bytes;
-    u32x4 x[kCopyLoads];
+    if (at0 + kCopyBytes <= a.bytes) {  // (requests behind conditions of their own cost a quarter)
+        u32x4 x[kCopyLoads];
 #pragma unroll
-    for (int i = 0; i < kCopyLoads; ++i) {
-        const int at = at0 + (i * kThreads + tid) * 16;
-        if (at < a.bytes) x[i] = *(const FLOE_GLOBAL u32x4*)(src + at);
-    }
+        for (int i = 0; i < kCopyLoads; ++i) x[i] = *(const FLOE_GLOBAL u32x4*)(src + at0 + (i * kThreads + tid) * 16);
 #pragma unroll
-    for (int i = 0; i < kCopyLoads; ++i) {
-        const int at = at0 + (i * kThreads + tid) * 16;
-        if (at < a.bytes) __builtin_nontemporal_store(x[i], (FLOE_GLOBAL u32x4*)(dst + at));
+        for (int i = 0; i < kCopyLoads; ++i) __builtin_nontemporal_store(x[i], (FLOE_GLOBAL u32x4*)(dst + at0 + (i * kThreads + tid) * 16));
+    } else {
+        for (int at = at0 + tid * 16; at < a.bytes; at += kThreads * 16)
+            __builtin_nontemporal_store(*(const FLOE_GLOBAL u32x4*)(src + at), (FLOE_GLOBAL u32x4*)(dst + at));
     }
     if (at0 == 0) {
         float* s = is_v ? c.vs : c.ks;
