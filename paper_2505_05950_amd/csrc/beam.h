@@ -10,6 +10,10 @@ constexpr int kBeamTake = 64;       // candidates of a group, at most: a lane ea
 constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / kWave;
 constexpr int kBeamRows = 256;      // rows of a group, at most
 
+struct BeamSum {
+    float top;   // the largest logit
+    double sum;  // of exp(x - top)
+};
 struct BeamArgs {
     const void* logits;
     int64_t stride;
@@ -20,8 +24,8 @@ struct BeamArgs {
     float* score_out;
     int32_t *parent, *token;
     uint8_t* done_out;
-    // [rows][slices]: largest logit and the sum of exp(x - it); [rows][slices][take]: the best tokens, in no order, 0 where there are fewer
-    float* sums;
+    // [rows][slices]; [rows][slices][take]: the best tokens, in no order, 0 where there are fewer
+    BeamSum* sums;
     uint64_t* best;
 };
 

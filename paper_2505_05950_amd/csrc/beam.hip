@@ -40,6 +40,20 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
     const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
     return __builtin_amdgcn_readfirstlane(max((uint32_t)b[0], (uint32_t)b[1]));
 }
+__device__ __forceinline__ double halves(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo); }
+template <int CTRL>
+__device__ __forceinline__ double dpp_add64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    return x + halves((uint32_t)dpp_movi<CTRL>((int)(uint32_t)u), (uint32_t)dpp_movi<CTRL>((int)(uint32_t)(u >> 32)));
+}
+__device__ __forceinline__ double wave_sum64(double x) {
+    x = dpp_add64<0x121>(dpp_add64<0x122>(dpp_add64<0x124>(dpp_add64<0x128>(x))));
+    uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const auto l16 = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false), h16 = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    u = __builtin_bit_cast(uint64_t, halves(l16[0], h16[0]) + halves(l16[1], h16[1]));
+    const auto l32 = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), h32 = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+    return halves(l32[0], h32[0]) + halves(l32[1], h32[1]);
+}
 // The largest T that at least `k` of the wave's 64 N values reach (0 if there are fewer), in bits `low` to `high`, with `t` above them
 template <int N>
 __device__ __forceinline__ uint32_t wave_kth(const uint32_t (&v)[N], int k, int low, int high = 31, uint32_t t = 0) {
@@ -161,7 +175,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     constexpr int E = kElements<DTYPE>, kTile = LOADS * kWave * E;
     constexpr float kLargest = 3.4028234663852886e38f, kInf = __builtin_inff(), kLog2e = 1.4426950408889634f;
     __shared__ uint64_t lists[kBeamWaves][kList];
-    __shared__ float wave_sums[kBeamWaves][2];
+    __shared__ BeamSum wave_sums[kBeamWaves];
     __shared__ int kept[kBeamWaves];
     __shared__ uint32_t shares[kBeamWaves];  // q of each wave, as order
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -334,20 +348,19 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
         n = a.take;
     }
     const float all = quad_max(row16_allreduce_max(top));
-    float sum32 = (float)(sum * (double)__builtin_amdgcn_exp2f((top - (all == -kInf ? 0.0f : all)) * kLog2e));
-    sum32 = quad_sum(row16_allreduce_sum(sum32));
+    sum = wave_sum64(sum * (double)__builtin_amdgcn_exp2f((top - (all == -kInf ? 0.0f : all)) * kLog2e));
     if (lane == 0) {
-        wave_sums[wave][0] = all;
-        wave_sums[wave][1] = sum32;
+        wave_sums[wave] = BeamSum{all, sum};
         kept[wave] = n;
     }
     __syncthreads();
     if (wave != 0) return;
-    float m = -kInf, s = 0.0f;
+    float m = -kInf;
+    double s = 0.0;
 #pragma unroll
-    for (int k = 0; k < kBeamWaves; ++k) m = fmaxf(m, wave_sums[k][0]);
+    for (int k = 0; k < kBeamWaves; ++k) m = fmaxf(m, wave_sums[k].top);
 #pragma unroll
-    for (int k = 0; k < kBeamWaves; ++k) s += wave_sums[k][1] * __builtin_amdgcn_exp2f((wave_sums[k][0] - (m == -kInf ? 0.0f : m)) * kLog2e);
+    for (int k = 0; k < kBeamWaves; ++k) s += wave_sums[k].sum * (double)__builtin_amdgcn_exp2f((wave_sums[k].top - (m == -kInf ? 0.0f : m)) * kLog2e);
     for (int k = 1; k < kBeamWaves; ++k) {
         if (lane < kept[k]) list[n + lane] = lists[k][lane];
         n += kept[k];
@@ -361,10 +374,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
         n = a.take;
     }
     __builtin_amdgcn_wave_barrier();
-    if (lane == 0) {
-        a.sums[2 * blockIdx.x] = m;
-        a.sums[2 * blockIdx.x + 1] = s;
-    }
+    if (lane == 0) a.sums[blockIdx.x] = BeamSum{m, s};
     if (lane < a.take) a.best[(size_t)blockIdx.x * a.take + lane] = lane < n ? list[lane] : 0;
 }
 
@@ -380,10 +390,15 @@ __device__ __forceinline__ int eight_sum(int x) {
     return x + dpp_movi<0x141>(x);
 }
 
-// log s in 64 bits, good to 2^-23: the exponent's part is exact, and the logarithm of a value between 1/2 and 1 is small
+// log s to 1e-10 (the library's logarithm is four times the code): s = 2^e f with f between sqrt(1/2) and sqrt(2), and
+// log f = 2 artanh(z) = 2 (z + z^3 / 3 + z^5 / 5 + ...) with z = (f - 1) / (f + 1), at most 0.172
 __device__ __forceinline__ double log_of(double s) {
-    const float f = (float)__builtin_amdgcn_frexp_mant(s);
-    return ((double)__builtin_amdgcn_frexp_exp(s) + (double)__builtin_amdgcn_logf(f)) * 0.6931471805599453;
+    double f = __builtin_amdgcn_frexp_mant(s);  // 1/2 .. 1
+    int e = __builtin_amdgcn_frexp_exp(s);
+    if (f < 0.70710678) f *= 2.0, --e;
+    const double z = (f - 1.0) / (f + 1.0), y = z * z;
+    const double p = 1.0 + y * (1.0 / 3 + y * (1.0 / 5 + y * (1.0 / 7 + y * (1.0 / 9 + y * (1.0 / 11)))));
+    return (double)e * 0.69314718055994531 + 2.0 * z * p;
 }
 
 // A workgroup per group.
@@ -433,22 +448,22 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
     };
     for (int w = sub; w < a.beams * parts; w += kSubs) {
         const int r = w / parts, row = group * a.beams + r;
-        const float* sums = a.sums + (size_t)row * a.slices * 2;
+        const BeamSum* sums = a.sums + (size_t)row * a.slices;
         const bool has = sixteenth < a.slices;
         // (asked for before it is known whether the row has any)
-        const f32x2 mine = *reinterpret_cast<const f32x2*>(sums + (has ? 2 * sixteenth : 0));
+        const BeamSum mine = sums[has ? sixteenth : 0];
         const uint64_t first = first_entry(r, w - r * parts);
         const float score = a.score[row];
         const bool alive = score > -kInf, ended = a.done && a.done[row];
         float m = -kInf;
         double s = 0.0;
         if (alive && !ended) {
-            if (has) m = mine.x;
-            for (int k = sixteenth + 16; k < a.slices; k += 16) m = fmaxf(m, sums[2 * k]);
+            if (has) m = mine.top;
+            for (int k = sixteenth + 16; k < a.slices; k += 16) m = fmaxf(m, sums[k].top);
             m = row16_allreduce_max(m);
             const float base = m == -kInf ? 0.0f : m;
-            if (has) s = (double)(mine.y * __builtin_amdgcn_exp2f((mine.x - base) * 1.4426950408889634f));
-            for (int k = sixteenth + 16; k < a.slices; k += 16) s += (double)(sums[2 * k + 1] * __builtin_amdgcn_exp2f((sums[2 * k] - base) * 1.4426950408889634f));
+            if (has) s = mine.sum * (double)__builtin_amdgcn_exp2f((mine.top - base) * 1.4426950408889634f);
+            for (int k = sixteenth + 16; k < a.slices; k += 16) s += sums[k].sum * (double)__builtin_amdgcn_exp2f((sums[k].top - base) * 1.4426950408889634f);
 #pragma unroll
             for (int step = 8; step; step >>= 1) s += __shfl_xor(s, step);
         }

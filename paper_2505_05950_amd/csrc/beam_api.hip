@@ -19,7 +19,7 @@ struct BeamWs {
 BeamWs beam_ws(const floe_beam* b, const BeamCut& cut) {
     const size_t lists = (size_t)b->groups * b->beams * cut.slices;
     BeamWs w;
-    w.best = align_up(lists * 8);
+    w.best = align_up(lists * sizeof(BeamSum));
     w.total = w.best + align_up(lists * b->take * 8);
     return w;
 }
@@ -48,7 +48,7 @@ int floe_beam_select(const floe_beam* b, const void* logits, int64_t row_stride,
     if (workspace_bytes < w.total) return FLOE_EWORKSPACE;
     char* base = static_cast<char*>(workspace);
     const BeamArgs a{logits, row_stride, score, done, b->groups, b->beams, b->vocab, b->take, b->eos, cut.slices, cut.slice, score_out, parent, token,
-                     done_out, reinterpret_cast<float*>(base), reinterpret_cast<uint64_t*>(base + w.best)};
+                     done_out, reinterpret_cast<BeamSum*>(base), reinterpret_cast<uint64_t*>(base + w.best)};
     hipStream_t st = (hipStream_t)stream;
     FLOE_LAUNCH(FLOE_KERNEL_BEAM_ROWS, st, launch_beam_rows(a, b->dtype, cut.loads, st));
     FLOE_LAUNCH(FLOE_KERNEL_BEAM_GROUPS, st, launch_beam_groups(a, st));

@@ -233,3 +233,12 @@ def test_few_rows_that_have_all_of_the_best(take):
     check(logits, score, take)
     same = logits[:1].expand(300, 3000).contiguous()  # and rows that are all the same: ties across a hundred of them
     check(same, torch.zeros((3, 100), device=DEV), take, exact=True)
+
+
+def test_rows_that_lie_more_than_32_bits_of_bytes_apart():
+    V, stride = 5000, (1 << 31) + 5
+    flat = torch.empty((stride + V,), dtype=torch.float16, device=DEV)
+    view = flat.as_strided((2, V), (stride, 1))
+    view.copy_(torch.randn((2, V), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV) * 2)
+    check(view, torch.tensor([[-1.0, 0.5]], device=DEV), 8)
+    check(view, torch.tensor([[-1.0], [0.5]], device=DEV), 3)

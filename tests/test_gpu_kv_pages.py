@@ -333,3 +333,20 @@ def test_compact_on_both_sides_of_what_one_workgroup_takes(n_seqs, block, most, 
     want_pairs, want_where = ref.compact(table, moves)
     same(pool, t, ref, table)
     assert pairs.tolist() == want_pairs and where.tolist() == want_where
+
+
+def test_pages_that_lie_behind_32_bits_of_bytes():
+    n, heads, dim, block = 70_000, 8, 128, 64
+    cache = F.KVCache(n, heads, dim, block)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    for t in (cache.k, cache.v):
+        t[n - 2].copy_(torch.randint(0, 256, t[0].shape, generator=g, device=DEV, dtype=torch.uint8))
+        t[3].copy_(torch.randint(0, 256, t[0].shape, generator=g, device=DEV, dtype=torch.uint8))
+        t[n - 1].zero_()
+        t[5].zero_()
+    cache.k_scale[n - 2], cache.v_scale[n - 2] = 2.0, 3.0
+    F.floe_kv_copy_pages(cache, i32([[n - 2, 5], [3, n - 1]]))
+    torch.cuda.synchronize()
+    for t in (cache.k, cache.v):
+        assert torch.equal(t[5], t[n - 2]) and torch.equal(t[n - 1], t[3]) and int(t[5].sum()) > 0
+    assert bool((cache.k_scale[5] == 2.0).all()) and bool((cache.v_scale[5] == 3.0).all())

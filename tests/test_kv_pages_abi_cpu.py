@@ -144,7 +144,7 @@ def test_selection_refuses(lib):
 def test_the_selection_s_workspace_stays_small_beside_the_logits(lib, rows, vocab, take, dtype):
     beams = 256 if rows == 1 << 20 else 1
     need = lib.floe_beam_workspace_bytes(beam(rows // beams, beams, vocab, take, dtype))
-    assert 0 < need <= 512 + rows * (8 + 8 * take) * max(1, min(-(-vocab // 1024), 2048 // rows + 1))
+    assert 0 < need <= 512 + rows * (16 + 8 * take) * max(1, min(-(-vocab // 1024), 2048 // rows + 1))
 
 
 def i32(*v):
