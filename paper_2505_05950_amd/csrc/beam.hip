@@ -7,8 +7,9 @@
 // a slice of a row, its four waves the slice's tiles in turn.  Each lane keeps a running maximum and sum; what reaches the workgroup's
 // threshold goes to its wave's list in LDS.  The threshold: if each of the waves has seen `quota` values that reach q of its own, with
 // quota * waves >= take, then `take` values reach the least of the four q, and what lies below is not among the slice's best.  q is at first
-// the quota-th largest of the 64 lanes' maxima in the wave's first tile, later the quota-th best of its list, formed again where that grows
-// over 64 entries.  A list that would not hold a tile's values is cut to its best `take`, which bounds it whatever the values are.
+// the quota-th largest of the 64 lanes' maxima in the wave's first tile, later the quota-th best of its list, formed again whenever that has
+// grown by some quotas: what passes falls as 1 / tiles then.  A list that would not hold a tile's values is cut to its best `take`, which
+// bounds it whatever the values are.
 // beam_groups_kernel: a workgroup per group joins the slices' sums, and finds the best of their lists with a threshold formed alike.
 #include "beam.h"
 
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     __shared__ uint64_t lists[kBeamWaves][kList];
     __shared__ BeamSum wave_sums[kBeamWaves];
     __shared__ int kept[kBeamWaves];
-    __shared__ uint32_t shares[kBeamWaves];  // q of each wave, as order
+    __shared__ uint64_t shares[kBeamWaves / 2];  // q of each wave, as order; of one without a tile the largest
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = blockIdx.x / a.slices, part = blockIdx.x - row * a.slices;
     if (!(a.score[row] > -kInf) || (a.done && a.done[row])) return;  // (the groups' kernel does not look at such a row either)
@@ -245,12 +246,23 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     };
     // waves of this slice that have a tile, and how many values each vouches for
     const int active = min(kBeamWaves, (end - begin + kTile - 1) / kTile), quota = (a.take + active - 1) / active;
-    auto shared_bar = [&]() {
-        uint32_t t = 0xffffffffu;
-        for (int k = 0; k < active; ++k) t = min(t, *(volatile uint32_t*)&shares[k]);
-        return value_of(t);  // (a NaN where a wave has too few values: the comparison with it leaves the bar)
+    auto share = [&](uint32_t q) {
+        if (lane == 0) reinterpret_cast<volatile uint32_t*>(shares)[wave] = q;
     };
+    auto shared_bar = [&]() {
+        const volatile uint64_t* p = shares;
+        const uint64_t a = p[0], b = p[1];
+        // (a NaN where a wave has too few values: the comparison with it leaves the bar)
+        return value_of(min(min((uint32_t)a, (uint32_t)(a >> 32)), min((uint32_t)b, (uint32_t)(b >> 32))));
+    };
+    // Entries from which on the list is looked at.  us, 512 rows, one threshold from the first tile on / this: 131072 in fp32, 64 taken 60 / 53, 8 taken
+    // 52 / 42, in bf16, 16 taken 43 / 36 (40 and 24 without any candidates).
+    int limit = min(kWave, max(16, 2 * quota));
     auto push = [&](int t0) {
+        float best = most[0];
+#pragma unroll
+        for (int u = 1; u < LOADS; ++u) best = fmaxf(best, most[u]);
+        if (__ballot(best >= bar) == 0) return;
         uint32_t late = 0;  // loads whose values the list has no room for
 #pragma unroll
         for (int u = 0; u < LOADS; ++u) {
@@ -287,7 +299,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
                 n += __popcll(mask);
             }
         }
-        if (n <= kWave && !cut) return;
+        if (n <= limit && !cut) return;
         // a better q, and what does not reach the threshold any more leaves the list
         auto shorten = [&](auto parts_) {
             constexpr int N = decltype(parts_)::value;
@@ -298,8 +310,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
                 v[j] = j * kWave + lane < n ? list[j * kWave + lane] : 0;
                 hi[j] = (uint32_t)(v[j] >> 32);
             }
-            const uint32_t q = wave_kth(hi, quota, 12);
-            if (lane == 0) *(volatile uint32_t*)&shares[wave] = q;
+            if constexpr (N == 1) share(wave_kth_few(hi[0], quota));
+            else share(wave_kth(hi, quota, 12));
             const float reach = shared_bar();
             bar = fmaxf(bar, reach);
             n = 0;
@@ -311,13 +323,14 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
                 n += __popcll(mask);
             }
         };
-        if (n <= 2 * kWave) shorten(std::integral_constant<int, 2>());
+        if (n <= kWave) shorten(std::integral_constant<int, 1>());
         else shorten(std::integral_constant<int, kListParts>());
         if (n > 2 * kWave || (cut && n >= a.take)) {  // (the waves' threshold may have left fewer)
             // tokens of later tiles lose to those of the list that have the same value
             bar = fmaxf(bar, value_of(cut_parts<DTYPE, kListParts>(list, n, a.take, token_bits) + 1));
             n = a.take;
         }
+        limit = max(limit, n + quota + 8);
     };
     const int stride = kBeamWaves * kTile;
     BeamTile<LOADS> now, next;
@@ -329,13 +342,14 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
         load(t0 + stride, next);
         if (there) values(t0, now);
         if (first) {
+            uint32_t q = 0xffffffffu;
             if (there) {
                 float best = most[0];
 #pragma unroll
                 for (int u = 1; u < LOADS; ++u) best = fmaxf(best, most[u]);
-                const uint32_t q = wave_kth_few(order_of(best + 0.0f), quota);
-                if (lane == 0) shares[wave] = q;
+                q = wave_kth_few(order_of(best + 0.0f), quota);
             }
+            share(q);
             __syncthreads();
             bar = fmaxf(bar, shared_bar());
         }
@@ -464,8 +478,7 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
             const float base = m == -kInf ? 0.0f : m;
             if (has) s = mine.sum * (double)__builtin_amdgcn_exp2f((mine.top - base) * 1.4426950408889634f);
             for (int k = sixteenth + 16; k < a.slices; k += 16) s += sums[k].sum * (double)__builtin_amdgcn_exp2f((sums[k].top - base) * 1.4426950408889634f);
-#pragma unroll
-            for (int step = 8; step; step >>= 1) s += __shfl_xor(s, step);
+            s = dpp_add64<0x121>(dpp_add64<0x122>(dpp_add64<0x124>(dpp_add64<0x128>(s))));
         }
         // (every lane and part of a row writes the same)
         row_top[r] = m;
