@@ -960,6 +960,12 @@ def _beam_out(t, shape, dtype, like, name, stream):
     return t
 
 
+def _overlap(a, b) -> bool:
+    """Whether two contiguous tensors share bytes."""
+    x, y = a.data_ptr(), b.data_ptr()
+    return x < y + b.numel() * b.element_size() and y < x + a.numel() * a.element_size()
+
+
 def floe_beam_select(logits, score, take: int = None, done=None, eos: int = -1, score_out=None, parent=None, token=None, done_out=None, workspace=None,
                      stream=None):
     """The `take` best continuations (as many as beams by default) of each group: logits [groups * beams][vocab] fp16, bf16 or fp32 (rows may lie
@@ -977,10 +983,14 @@ def floe_beam_select(logits, score, take: int = None, done=None, eos: int = -1, 
             _beam_out(t, sizes, dtype, logits, name, stream)
     take = beams if take is None else take
     out = groups, take
+    given = (score_out, "score_out"), (parent, "parent"), (token, "token"), (done_out, "done_out")
     score_out = _beam_out(score_out, out, torch.float32, logits, "score_out", stream)
     parent = _beam_out(parent, out, torch.int32, logits, "parent", stream)
     token = _beam_out(token, out, torch.int32, logits, "token", stream)
     done_out = _beam_out(done_out, out, torch.uint8, logits, "done_out", stream)
+    for t, name in given:
+        if t is not None and any(i is not None and _overlap(t, i) for i in (score, done)):
+            raise ValueError(f"floe_beam_select: {name} lies over an input (a group's results are written while others are still read)")
     b, (call, need) = _BEAM_FIELDS.pack(groups, beams, vocab, take, kind, eos), _beam_calls()
     workspace, wp, wn = _scratch(workspace, logits, need(b), stream)
     rc = call(b, logits.data_ptr(), strides[0] if rows > 1 else vocab, score.data_ptr(), None if done is None else done.data_ptr(), score_out.data_ptr(),

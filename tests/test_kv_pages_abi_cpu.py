@@ -231,3 +231,14 @@ def test_the_model_of_the_pool_keeps_counts_and_tables_together():
         else:
             model.compact(table, 4)
         assert Pool(pages, P_).count(table).refs == model.refs
+
+
+def test_a_selection_into_its_own_inputs_is_refused(monkeypatch):
+    monkeypatch.setattr(B, "_launches_on", lambda *a: None)
+    x, s, d = torch.zeros((6, 8), dtype=torch.float16), torch.zeros((2, 3)), torch.zeros((2, 3), dtype=torch.uint8)
+    both = torch.zeros(9)
+    for score, done, more in ((s, None, dict(score_out=s)), (s, d, dict(done_out=d)), (both[:6].view(2, 3), None, dict(score_out=both[3:].view(2, 3))),
+                              (both[3:].view(2, 3), None, dict(score_out=both[:6].view(2, 3))), (s, None, dict(parent=s.view(torch.int32))),
+                              (s, None, dict(take=1, token=s.view(torch.int32).flatten()[4:].view(2, 1)))):
+        with pytest.raises(ValueError, match="over an input"):
+            F.floe_beam_select(x, score, done=done, eos=1 if done is not None else -1, **more)
