@@ -488,9 +488,10 @@ __global__ __launch_bounds__(kReserveThreads) void kv_compact_few_kernel(KvPool 
 }
 
 // ---- copy
-// Bound by bytes, mostly those written (a page that goes to several places is read from L2).  Stores leave the caches to the sources: us of a
-// whole step of 128 beams with eight layers (82 MB written), of a fork and its end (252 MB), of packing and what is around it (472 MB), a
-// workgroup taking 16 KB 46 70 177, with plain stores 52 80 182; 4 KB 50 87 197, 8 KB 46 77 182, 32 KB 51 74 179.
+// Bound by bytes, mostly those written (a page that goes to several places is read from L2: a workgroup's number mod 8 is its XCD, and pages
+// mostly have a multiple of eight pieces).  Stores leave the caches to the sources.  us of a whole step of 128 beams with eight layers (82 MB
+// written), of a fork and its end (252 MB), of packing and what is around it (472 MB), replayed: 45.8 69.3 174; with nontemporal stores alone
+// 46.2 73 175.5, plain ones 6 10 5 more.  16 KB for a workgroup: 4 KB took 4 17 20 more, 8 KB 0 7 5, 32 KB 5 4 2.
 __global__ __launch_bounds__(kThreads) void kv_copy_pages_kernel(KvCopyArgs a) {
     const int pair = blockIdx.x / a.pieces, piece = blockIdx.x - pair * a.pieces, tid = threadIdx.x;
     const int from = a.pairs[2 * pair], to = a.pairs[2 * pair + 1];
@@ -501,20 +502,22 @@ __global__ __launch_bounds__(kThreads) void kv_copy_pages_kernel(KvCopyArgs a) {
     const int at0 = (is_v ? piece - half : piece) * kCopyBytes;
     const uint8_t* src = (is_v ? c.v : c.k) + (size_t)from * a.bytes;
     uint8_t* dst = (is_v ? c.v : c.k) + (size_t)to * a.bytes;
+    float* scales = is_v ? c.vs : c.ks;
+    const float scale = scales[(size_t)from * a.heads + min(tid, a.heads - 1)];  // (by every piece, so that it needs no condition)
     if (at0 + kCopyBytes <= a.bytes) {  // (requests behind conditions of their own cost a quarter)
+        constexpr int kPastCaches = 16 | 2;  // sc1 (written through) and nt
+        const __amdgpu_buffer_rsrc_t to_page = __builtin_amdgcn_make_buffer_rsrc(dst + at0, 0, kCopyBytes, 0x00027000);
         u32x4 x[kCopyLoads];
 #pragma unroll
         for (int i = 0; i < kCopyLoads; ++i) x[i] = *(const FLOE_GLOBAL u32x4*)(src + at0 + (i * kThreads + tid) * 16);
 #pragma unroll
-        for (int i = 0; i < kCopyLoads; ++i) __builtin_nontemporal_store(x[i], (FLOE_GLOBAL u32x4*)(dst + at0 + (i * kThreads + tid) * 16));
+        for (int i = 0; i < kCopyLoads; ++i) __builtin_amdgcn_raw_buffer_store_b128(x[i], to_page, (i * kThreads + tid) * 16, 0, kPastCaches);
     } else {
         for (int at = at0 + tid * 16; at < a.bytes; at += kThreads * 16)
             __builtin_nontemporal_store(*(const FLOE_GLOBAL u32x4*)(src + at), (FLOE_GLOBAL u32x4*)(dst + at));
     }
-    if (at0 == 0) {
-        float* s = is_v ? c.vs : c.ks;
-        for (int h = tid; h < a.heads; h += kThreads) s[(size_t)to * a.heads + h] = s[(size_t)from * a.heads + h];
-    }
+    static_assert(kThreads >= 256, "a thread per head: a cache has up to 256");
+    if (at0 == 0 && tid < a.heads) scales[(size_t)to * a.heads + tid] = scale;
 }
 
 }  // namespace
