@@ -467,7 +467,7 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
         // (asked for before it is known whether the row has any)
         const BeamSum mine = sums[has ? sixteenth : 0];
         const uint64_t first = first_entry(r, w - r * parts);
-        const float score = a.score[row];
+        const float score = a.score[row] + 0.0f;  // (-0 becomes 0: candidates are ranked by c as an integer, in which the zeros differ)
         const bool alive = score > -kInf, ended = a.done && a.done[row];
         float m = -kInf;
         double s = 0.0;

@@ -242,3 +242,14 @@ def test_rows_that_lie_more_than_32_bits_of_bytes_apart():
     view.copy_(torch.randn((2, V), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV) * 2)
     check(view, torch.tensor([[-1.0, 0.5]], device=DEV), 8)
     check(view, torch.tensor([[-1.0], [0.5]], device=DEV), 3)
+
+
+@pytest.mark.parametrize("scores", [[-0.0, 0.0], [0.0, -0.0], [0.0, -0.0, -0.0, 0.0, -1.0], [-0.0, -3.0, 0.0]])
+def test_scores_of_either_zero_are_equal(scores):
+    """Equal c go by the row, and -0 is equal to 0: of rows that are done, whose c is the score itself, and of rows of one token, whose c is too."""
+    W = len(scores)
+    score = torch.tensor([scores, scores[::-1]], device=DEV)
+    done = torch.ones((2, W), dtype=torch.uint8, device=DEV)
+    for take in (1, 2, W):
+        check(torch.zeros((2 * W, 40), device=DEV), score, take, done, eos=3, exact=True)
+        check(torch.full((2 * W, 1), 2.5, device=DEV), score, take, exact=True)
