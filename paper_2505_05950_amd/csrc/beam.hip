@@ -146,6 +146,13 @@ __device__ __forceinline__ uint32_t wave_kth_few(uint32_t v, int k) {
 template <int DTYPE>
 constexpr int kElements = DTYPE == 2 ? 4 : 8;  // of sixteen bytes
 
+// exp(d) of d <= 0 to 1e-8; below -100, and for -infinity less itself, that of -100.  exp(d) = 2^n exp(y) with |y| <= log(2) / 2, by its series.
+__device__ __forceinline__ double exp_of(double d) {
+    const double t = fmax(d, -100.0) * 1.4426950408889634, n = __builtin_rint(t), y = (t - n) * 0.69314718055994531;
+    const double p = 1.0 + y * (1.0 + y * (1.0 / 2 + y * (1.0 / 6 + y * (1.0 / 24 + y * (1.0 / 120 + y * (1.0 / 720 + y * (1.0 / 5040)))))));
+    return __builtin_amdgcn_ldexp(p, (int)n);
+}
+
 template <int DTYPE>
 __device__ __forceinline__ float logit(const void* row, int i) {
     if constexpr (DTYPE == 2) return gloadf(static_cast<const float*>(row) + i);
@@ -187,6 +194,10 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     const int begin = part * a.slice, end = min(a.vocab, begin + a.slice), token_bits = 32 - __builtin_clz(a.vocab);
     uint64_t* list = lists[wave];
     float top = -kInf;   // of the lane
+    // Terms are exp(x - base) with base <= top <= base + 8: a base that followed every new maximum would have the whole sum multiplied each time,
+    // and the factors' roundings would add up over the tiles (2^24 slowly ascending values in one slice: log s off by 5e-5).  One that moves by
+    // more than 8 leaves e^-8 of what was summed, so few factors ever matter, and they are formed in 64 bits.
+    float base = -kInf;
     double sum = 0.0;    // (tiles are summed in 32 bits, and their sums in 64: chains of eight, however long the row)
     float bar = -kLargest;
     int n = 0;           // entries of the wave's list
@@ -216,7 +227,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
             }
         }
         // A NaN makes the tile's sum one, +infinity too: then the values are formed again, without them.
-        float grown, base, all;
+        float grown, next, all;
         for (bool again = false;; again = true) {
             grown = top;
             all = 0.0f;
@@ -227,12 +238,13 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
                 for (int e = 1; e < E; ++e) most[u] = fmaxf(most[u], x[u][e]);
                 grown = fmaxf(grown, most[u]);
             }
-            base = grown == -kInf ? 0.0f : grown;
+            next = grown > base + 8.0f ? grown : base;
+            const float from = next == -kInf ? 0.0f : next;
 #pragma unroll
             for (int u = 0; u < LOADS; ++u) {
                 float part = 0.0f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) part += __builtin_amdgcn_exp2f((x[u][e] - base) * kLog2e);
+                for (int e = 0; e < E; ++e) part += __builtin_amdgcn_exp2f((x[u][e] - from) * kLog2e);
                 all += part;
             }
             if (again || __ballot(all != all) == 0) break;
@@ -241,7 +253,9 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) x[u][e] = fminf(fmaxf(x[u][e], -kInf), kLargest);  // (a NaN becomes -infinity)
         }
-        sum = sum * (double)__builtin_amdgcn_exp2f((top - base) * kLog2e) + (double)all;
+        if (__ballot(next != base && sum != 0.0)) sum *= exp_of((double)base - (double)next);
+        sum += (double)all;
+        base = next;
         top = grown;
     };
     // waves of this slice that have a tile, and how many values each vouches for
@@ -362,7 +376,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
         n = a.take;
     }
     const float all = quad_max(row16_allreduce_max(top));
-    sum = wave_sum64(sum * (double)__builtin_amdgcn_exp2f((top - (all == -kInf ? 0.0f : all)) * kLog2e));
+    sum = wave_sum64(sum * exp_of((double)base - (double)all));
     if (lane == 0) {
         wave_sums[wave] = BeamSum{all, sum};
         kept[wave] = n;

@@ -253,3 +253,28 @@ def test_scores_of_either_zero_are_equal(scores):
     for take in (1, 2, W):
         check(torch.zeros((2 * W, 40), device=DEV), score, take, done, eos=3, exact=True)
         check(torch.full((2 * W, 1), 2.5, device=DEV), score, take, exact=True)
+
+
+@pytest.mark.parametrize("form,size", [("ascending", 0.25), ("ascending", 1.3), ("ascending", 40.0), ("ascending", 4000.0), ("descending", 4.0), ("steps", 60.0), ("at the end", 25.0)])
+def test_rows_of_many_tiles_in_one_slice_keep_their_sum(form, size):
+    """From 1024 rows on a row is one slice: here each lane goes over 1024 tiles, and its maximum grows in all of them, in some, or in the last one.
+    c of the best token is -log s, so its error is that of log s (TOL) and half a step of binary32.  TOL has room for it: a lane's terms are
+    exp(d) with |d| <= max(8, |x - m|), off by 2^-24 (2.3 |d| + 2) (the difference, the product, log2(e) itself; the power of two), whose mean is
+    below 2^-24 (2.3 (8 + log 2^22) + 2) = 3.3e-6 here (3.9e-6 for 2^28); 11 roundings of sums, 7e-7, two joins, 2.4e-7; a lane's sum takes
+    factors of 64 bits alone.  The rows beside count for nothing and are not read."""
+    rows, V = 1024, 1 << 22
+    i = np.arange(V, dtype=np.float64)
+    x = {"ascending": i / V, "descending": -i / V, "steps": (i // 65536) / 64, "at the end": (i == V - 1) * 1.0}[form] * size
+    x = x.astype(np.float32)
+    logits = torch.empty((rows, V), device=DEV)
+    logits[700] = torch.from_numpy(x).to(DEV)
+    score = torch.full((rows, 1), -float("inf"), device=DEV)
+    score[700] = 0.0
+    c, _, token, _ = F.floe_beam_select(logits, score, take=2)
+    x = x.astype(np.float64)
+    m, log_s = x.max(), np.log(np.exp(x - x.max()).sum())
+    order = np.lexsort((i, -x))[:2]
+    assert token[700].tolist() == order.tolist() and bool((token[:700] == -1).all()) and bool((token[701:] == -1).all())
+    for k in range(2):
+        want = (x[order[k]] - m) - log_s
+        assert abs(float(c[700, k]) - want) <= TOL + 2.0 ** -24 * abs(want), (float(c[700, k]), want)
