@@ -574,7 +574,7 @@ int floe_kv_trim(const floe_kv_pool* p, int32_t* table, const int32_t* len, int 
  * Packs the pool: with U used pages in all, the highest used page moves to the lowest free one, and so on, up to n_pairs moves; if these
  * are enough, pages 0 .. U - 1 are the used ones.  refs and table follow; pairs[i] = (from, to), (-1, -1) behind the last move:
  * floe_kv_copy_pages has to run on them before the pages are read or written.  page_map dev int32 [n_pages]: the new place of every page
- * (itself where it stays), for tables beside `table`.  pairs dev int32 [n_pairs][2].  workspace: dev, 256-byte aligned.
+ * (itself where it stays), for tables beside `table`.  pairs dev int32 [n_pairs][2], n_pairs <= 2^30.  workspace: dev, 256-byte aligned.
  */
 size_t floe_kv_compact_workspace_bytes(const floe_kv_pool* p, int n_pairs);
 int floe_kv_compact(const floe_kv_pool* p, int32_t* table, int n_seqs, int max_blocks, int32_t* pairs, int n_pairs, int32_t* page_map, void* workspace,

@@ -36,6 +36,7 @@ ReserveWs reserve_ws(const floe_kv_pool* p) {
     w.total = w.list + align_up((size_t)p->n_pages * sizeof(KvRequest));
     return w;
 }
+constexpr int kMaxPairs = 1 << 30;  // of a compaction, whose kernels number the halves of pairs in 32 bits
 struct CompactWs {
     size_t high, low, code, moves, total;
 };
@@ -106,7 +107,7 @@ int floe_kv_reserve(const floe_kv_pool* p, int32_t* table, const int32_t* len, c
 }
 
 size_t floe_kv_compact_workspace_bytes(const floe_kv_pool* p, int n_pairs) {
-    return check_pool(p) == FLOE_OK && n_pairs >= 0 ? compact_ws(p, n_pairs).total : 0;
+    return check_pool(p) == FLOE_OK && n_pairs >= 0 && n_pairs <= kMaxPairs ? compact_ws(p, n_pairs).total : 0;
 }
 
 int floe_kv_compact(const floe_kv_pool* p, int32_t* table, int n_seqs, int max_blocks, int32_t* pairs, int n_pairs, int32_t* page_map, void* workspace,
@@ -116,6 +117,7 @@ int floe_kv_compact(const floe_kv_pool* p, int32_t* table, int n_seqs, int max_b
     if ((rc = check_sizes(n_seqs, max_blocks))) return rc;
     if (n_pairs < 0 || (n_pairs && (!pairs || !aligned(pairs, 4))) || !page_map || !aligned(page_map, 4)) return FLOE_EINVAL;
     if (!workspace || !aligned(workspace, kAlign) || check_table(table, n_seqs, max_blocks)) return FLOE_EINVAL;
+    if (n_pairs > kMaxPairs) return FLOE_EUNSUPPORTED;
     const CompactWs w = compact_ws(p, n_pairs);
     if (workspace_bytes < w.total) return FLOE_EWORKSPACE;
     char* base = static_cast<char*>(workspace);

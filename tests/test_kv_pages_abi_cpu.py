@@ -242,3 +242,11 @@ def test_a_selection_into_its_own_inputs_is_refused(monkeypatch):
                               (s, None, dict(take=1, token=s.view(torch.int32).flatten()[4:].view(2, 1)))):
         with pytest.raises(ValueError, match="over an input"):
             F.floe_beam_select(x, score, done=done, eos=1 if done is not None else -1, **more)
+
+
+@pytest.mark.parametrize("n_pairs", [(1 << 30) + 1, (1 << 31) - 1])
+def test_compact_refuses_more_pairs_than_32_bits_number(lib, n_pairs):
+    """The kernels count pairs and their halves in 32 bits."""
+    assert compact(lib, n_pairs=n_pairs) == EUNSUPPORTED and lib.floe_kv_compact_workspace_bytes(pool(), n_pairs) == 0
+    if not torch.cuda.is_available():
+        assert compact(lib, n_pairs=1 << 30) == EHIP  # (the most that is taken)
