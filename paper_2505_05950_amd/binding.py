@@ -814,7 +814,8 @@ def _new(like, shape, dtype, stream):
 
 class KVPool:
     """How many table entries name each of a cache's pages: refs int32 [n_pages], zeros at the start (refs=: an array that exists).  One
-    pool serves the caches of all layers, which share their tables.  Its calls are ordered by the caller, captured ones too."""
+    pool serves the caches of all layers, which share their tables.  Its calls are ordered by the caller, captured ones too.  Captured calls
+    hold the addresses of refs and, unless handed a workspace, of the pool's own: the pool lives as long as their graphs."""
 
     def __init__(self, n_pages: int, block: int = 64, refs=None, device="cuda"):
         self.n_pages, self.block = int(n_pages), int(block)
@@ -827,15 +828,19 @@ class KVPool:
         self.refs, self._device = refs, refs.get_device()
         self._c = _KvPool(self.n_pages, self.block, refs.data_ptr())
         self._at = C.addressof(self._c)
-        # scratch of the calls: those on one pool are ordered by the caller, as they change its counts
         lib, at = load(), C.byref(self._c)
-        nbytes = max(lib.floe_kv_reserve_workspace_bytes(at), lib.floe_kv_compact_workspace_bytes(at, self.n_pages))
-        self._scratch = _workspace(nbytes, refs.device)
-        self._scratch_at = _aligned_ptr(self._scratch)
+        self._need = max(lib.floe_kv_reserve_workspace_bytes(at), lib.floe_kv_compact_workspace_bytes(at, self.n_pages))
+        self._ws = {}
 
-    def _workspace(self, given):
+    def _workspace(self, given, st: int, stream):
+        """(address, bytes) of scratch: an array per stream, from that stream's pool of memory, which takes it back in the order of the
+        stream when the pool is dropped while calls are still queued."""
         if given is None:
-            return self._scratch_at
+            ws = self._ws.get(st)
+            if ws is None:
+                array = _workspace(self._need, self.refs.device, stream)
+                ws = self._ws[st] = (*_aligned_ptr(array), array)
+            return ws[0], ws[1]
         if given.get_device() != self._device:
             raise ValueError(f"workspace: on {given.device}, the pool is on {self.refs.device}")
         return _aligned_ptr(given)
@@ -877,8 +882,9 @@ def floe_kv_reserve(pool: KVPool, table, length, cu_rows, pairs=None, missing=No
     length_at, cu_at = _i32(length, (n,), pool._device, "length"), _i32(cu_rows, (n + 1,), pool._device, "cu_rows")
     pairs = _given_or_new(pairs, (n, 2), pool, table, "pairs", stream)
     missing = _given_or_new(missing, (1,), pool, table, "missing", stream)
-    wp, wn = pool._workspace(workspace)
-    rc = _page_calls()[1](pool._at, at, length_at, cu_at, n, blocks, pairs.data_ptr(), missing.data_ptr(), wp, wn, _stream(stream))
+    st = _stream(stream)
+    wp, wn = pool._workspace(workspace, st, stream)
+    rc = _page_calls()[1](pool._at, at, length_at, cu_at, n, blocks, pairs.data_ptr(), missing.data_ptr(), wp, wn, st)
     if rc:
         _check(rc, "floe_kv_reserve")
     return pairs, missing
@@ -900,8 +906,9 @@ def floe_kv_compact(pool: KVPool, table, max_moves: int = None, pairs=None, page
     moves = pool.n_pages if max_moves is None else int(max_moves)
     pairs = _given_or_new(pairs, (moves, 2), pool, table, "pairs", stream)
     page_map = _given_or_new(page_map, (pool.n_pages,), pool, table, "page_map", stream)
-    wp, wn = pool._workspace(workspace)
-    rc = _page_calls()[3](pool._at, at, n, blocks, pairs.data_ptr(), moves, page_map.data_ptr(), wp, wn, _stream(stream))
+    st = _stream(stream)
+    wp, wn = pool._workspace(workspace, st, stream)
+    rc = _page_calls()[3](pool._at, at, n, blocks, pairs.data_ptr(), moves, page_map.data_ptr(), wp, wn, st)
     if rc:
         _check(rc, "floe_kv_compact")
     return pairs, page_map

@@ -90,3 +90,15 @@ def test_the_layers_calls(s, spaces):
     assert len(spaces) == 1
     all_of(s, layer.table, y, *spaces)
     assert torch.equal(y, F.floe_moe_layer_decode(layer, x))
+
+
+def test_the_pools_calls(s, spaces):
+    pool = F.KVPool(50000, 32, device=DEV)  # (a reserve of more than 1024 blocks and a packing of this many pages use their scratch)
+    table, before, cu = torch.full((3, 2000), -1, dtype=torch.int32, device=DEV), i32([0, 0, 0]), i32([0, 32 * 1000, 32 * 1500, 32 * 1501])
+    torch.cuda.synchronize()
+    pairs, missing = F.floe_kv_reserve(pool, table, before, cu, stream=s)
+    t, ln = F.floe_kv_reorder(pool, table, i32([32 * 1000, 32 * 500, 32]), i32([2, 1]), stream=s)
+    moves, where = F.floe_kv_compact(pool, t, stream=s)
+    assert len(spaces) == 1
+    all_of(s, pairs, missing, t, ln, moves, where, *spaces)
+    assert int(missing) == 0 and sorted(t[t >= 0].tolist()) == list(range(501)) and int((pool.refs > 0).sum()) == 501

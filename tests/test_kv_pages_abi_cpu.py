@@ -250,3 +250,32 @@ def test_compact_refuses_more_pairs_than_32_bits_number(lib, n_pairs):
     assert compact(lib, n_pairs=n_pairs) == EUNSUPPORTED and lib.floe_kv_compact_workspace_bytes(pool(), n_pairs) == 0
     if not torch.cuda.is_available():
         assert compact(lib, n_pairs=1 << 30) == EHIP  # (the most that is taken)
+
+
+def test_a_pool_s_scratch_belongs_to_the_stream_of_the_call(monkeypatch):
+    """Memory that a call on a stream uses without the caller's knowledge comes from that stream's pool: dropped with the pool, it is given out
+    again in that stream's order.  One array per stream, made when the stream's first call needs it."""
+    class Stream:
+        def __init__(self, handle):
+            self.cuda_stream = handle
+    made, used = [], []
+    make = lambda n, device, stream=None: made.append((stream, torch.empty((n + 256,), dtype=torch.uint8))) or made[-1][1]  # noqa: E731
+    call = lambda *a: used.append(a[-3:]) or 0  # noqa: E731  (workspace, bytes, stream)
+    monkeypatch.setattr(B, "_workspace", make)
+    monkeypatch.setattr(B, "_launches_on", lambda *a: None)
+    monkeypatch.setattr(B, "_stream", lambda stream: 7 if stream is None else stream.cuda_stream)
+    monkeypatch.setattr(B, "_page_calls", lambda: (call,) * 5)
+    p, t, n = F.KVPool(4, 32, device="cpu"), torch.zeros((2, 3), dtype=torch.int32), i32(5, 6)
+    outs, moves = dict(pairs=torch.zeros((2, 2), dtype=torch.int32), missing=i32(0)), dict(pairs=torch.zeros((4, 2), dtype=torch.int32), page_map=i32(0, 0, 0, 0))
+    one, two = Stream(11), Stream(12)
+    for stream in (one, None, two, one, None):
+        F.floe_kv_reserve(p, t, n, i32(0, 1, 2), **outs, stream=stream)
+        F.floe_kv_compact(p, t, **moves, stream=stream)
+    assert [s for s, _ in made] == [one, None, two]
+    spaces = {11: made[0][1], 7: made[1][1], 12: made[2][1]}
+    assert [st for _, _, st in used] == [11, 11, 7, 7, 12, 12, 11, 11, 7, 7]
+    for at, size, st in used:
+        assert spaces[st].data_ptr() <= at and at + size <= spaces[st].data_ptr() + spaces[st].numel() and at % 256 == 0
+    own = torch.empty((4096,), dtype=torch.uint8)
+    F.floe_kv_reserve(p, t, n, i32(0, 1, 2), **outs, workspace=own, stream=Stream(13))
+    assert len(made) == 3 and own.data_ptr() <= used[-1][0] < own.data_ptr() + 256
