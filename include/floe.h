@@ -542,7 +542,7 @@ typedef struct {
  *   table_out[i] = table[parent[i]], len_out[i] = len[parent[i]];   parent[i] outside [0, n_seqs): no pages, length 0
  * and `table` is no longer in use: a page's count loses what `table` named and gains what table_out names.  Several children share all
  * pages of their parent, also the one that the next token goes to: floe_kv_reserve gives whoever writes a page of its own.
- * Outputs may not overlap `table`, `len` or `parent`.  One launch.
+ * Outputs may not overlap `table`, `len`, `parent` or each other.  One launch.
  */
 int floe_kv_reorder(const floe_kv_pool* p, const int32_t* table, const int32_t* len, int n_seqs, int max_blocks, const int32_t* parent,
                     int32_t* table_out, int32_t* len_out, int n_out, void* stream);

@@ -62,9 +62,10 @@ int floe_kv_reorder(const floe_kv_pool* p, const int32_t* table, const int32_t* 
     if ((rc = check_sizes(n_seqs, max_blocks)) || (rc = check_sizes(n_out, max_blocks))) return rc;
     if ((rc = check_table(table, n_seqs, max_blocks)) || (rc = check_table(table_out, n_out, max_blocks))) return rc;
     if ((n_seqs && (!len || !aligned(len, 4))) || (n_out && (!parent || !len_out || !aligned(parent, 4) || !aligned(len_out, 4)))) return FLOE_EINVAL;
-    const size_t in = (size_t)n_seqs * max_blocks * 4, out = (size_t)n_out * max_blocks * 4;
-    if (!apart(table, in, table_out, out) || !apart(len, (size_t)n_seqs * 4, len_out, (size_t)n_out * 4) ||
-        !apart(parent, (size_t)n_out * 4, len_out, (size_t)n_out * 4) || !apart(parent, (size_t)n_out * 4, table_out, out))
+    const size_t in = (size_t)n_seqs * max_blocks * 4, out = (size_t)n_out * max_blocks * 4, len_in = (size_t)n_seqs * 4, each_out = (size_t)n_out * 4;
+    if (!apart(table_out, out, table, in) || !apart(table_out, out, len, len_in) || !apart(table_out, out, parent, each_out) ||
+        !apart(len_out, each_out, table, in) || !apart(len_out, each_out, len, len_in) || !apart(len_out, each_out, parent, each_out) ||
+        !apart(table_out, out, len_out, each_out))
         return FLOE_EINVAL;
     if (n_seqs + n_out == 0) return FLOE_OK;
     hipStream_t st = (hipStream_t)stream;

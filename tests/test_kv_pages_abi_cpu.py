@@ -279,3 +279,14 @@ def test_a_pool_s_scratch_belongs_to_the_stream_of_the_call(monkeypatch):
     own = torch.empty((4096,), dtype=torch.uint8)
     F.floe_kv_reserve(p, t, n, i32(0, 1, 2), **outs, workspace=own, stream=Stream(13))
     assert len(made) == 3 and own.data_ptr() <= used[-1][0] < own.data_ptr() + 256
+
+
+def test_reorder_refuses_outputs_over_the_other_input_and_over_each_other(lib):
+    """Some workgroups write both outputs while others still read the table, the lengths and the parents: no output lies over any of them."""
+    # table_out (24 bytes) and length (8), length_out (8) and table (24), the two outputs
+    for change in (dict(length=BIG), dict(length=BIG + 20), dict(length=BIG - 4), dict(table=2 * BIG - 20), dict(table=2 * BIG), dict(table=2 * BIG + 4),
+                   dict(length_out=BIG), dict(length_out=BIG + 20), dict(length_out=BIG - 4)):
+        assert reorder(lib, **change) == EINVAL, change
+    if not torch.cuda.is_available():
+        for change in (dict(length=BIG + 24), dict(length=BIG - 8), dict(table=2 * BIG - 24), dict(table=2 * BIG + 8), dict(length_out=BIG + 24), dict(length_out=BIG - 8)):
+            assert reorder(lib, **change) == EHIP, change
