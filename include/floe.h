@@ -601,7 +601,7 @@ int floe_kv_copy_pages(const floe_kv_cache* caches, int n_caches, const int32_t*
  * Places behind the last candidate hold score -infinity, parent -1, token -1, done 0.
  * logits dev [groups * beams] rows of `vocab` values of `dtype`, row_stride elements from row to row (any that keeps rows apart; rows need
  * no more than their type's alignment).  score dev float [groups][beams]; done dev uint8 [groups][beams], or NULL.  eos: in [0, vocab), or
- * -1: no token ends a row (done has to be NULL then).  Outputs may overlap no input.
+ * -1: no token ends a row (done has to be NULL then).  Outputs may lie over the inputs, which are read before, but not over each other.
  * Supported: take <= 64, beams <= 256, vocab < 2^28, groups * beams <= 2^20.  workspace: dev, 256-byte aligned, scratch.
  */
 typedef struct {

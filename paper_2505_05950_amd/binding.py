@@ -997,7 +997,9 @@ def floe_beam_select(logits, score, take: int = None, done=None, eos: int = -1, 
     done_out = _beam_out(done_out, out, torch.uint8, logits, "done_out", stream)
     for t, name in given:
         if t is not None and any(i is not None and _overlap(t, i) for i in (score, done)):
-            raise ValueError(f"floe_beam_select: {name} lies over an input (a group's results are written while others are still read)")
+            raise ValueError(f"floe_beam_select: {name} lies over an input (score and done stay as they are)")
+        if t is not None and any(o is not t and _overlap(t, o) for o in (score_out, parent, token, done_out)):
+            raise ValueError(f"floe_beam_select: {name} lies over another result")
     b, (call, need) = _BEAM_FIELDS.pack(groups, beams, vocab, take, kind, eos), _beam_calls()
     workspace, wp, wn = _scratch(workspace, logits, need(b), stream)
     rc = call(b, logits.data_ptr(), strides[0] if rows > 1 else vocab, score.data_ptr(), None if done is None else done.data_ptr(), score_out.data_ptr(),

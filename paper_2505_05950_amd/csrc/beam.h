@@ -10,10 +10,13 @@ constexpr int kBeamTake = 64;       // candidates of a group, at most: a lane ea
 constexpr int kBeamThreads = 256, kBeamWaves = kBeamThreads / kWave;
 constexpr int kBeamRows = 256;      // rows of a group, at most
 
+// What the groups' kernel gets to know of a slice and its row: it reads no input, so a group's results may lie over those of other groups.
 struct BeamSum {
-    float top;   // the largest logit
-    double sum;  // of exp(x - top)
+    float top;    // the largest logit
+    float score;  // of the row
+    double sum;   // of exp(x - top); kBeamDone of a row that is done
 };
+constexpr double kBeamDone = -1.0;
 struct BeamArgs {
     const void* logits;
     int64_t stride;

@@ -188,7 +188,13 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     __shared__ uint64_t shares[kBeamWaves / 2];  // q of each wave, as order; of one without a tile the largest
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = blockIdx.x / a.slices, part = blockIdx.x - row * a.slices;
-    if (!(a.score[row] > -kInf) || (a.done && a.done[row])) return;  // (the groups' kernel does not look at such a row either)
+    // (-0 becomes 0: candidates are ranked by c as an integer, in which the zeros differ)
+    const float score = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, a.score[row] + 0.0f)));
+    const bool done = a.done && a.done[row];
+    if (!(score > -kInf) || done) {  // nothing of its logits counts
+        if (tid == 0) a.sums[blockIdx.x] = BeamSum{-kInf, score, done ? kBeamDone : 0.0};
+        return;
+    }
     constexpr int kSize = DTYPE == 2 ? 4 : 2;
     const unsigned char* logits = static_cast<const unsigned char*>(a.logits) + row * a.stride * kSize;
     const int begin = part * a.slice, end = min(a.vocab, begin + a.slice), token_bits = 32 - __builtin_clz(a.vocab);
@@ -378,7 +384,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
     const float all = quad_max(row16_allreduce_max(top));
     sum = wave_sum64(sum * exp_of((double)base - (double)all));
     if (lane == 0) {
-        wave_sums[wave] = BeamSum{all, sum};
+        wave_sums[wave] = BeamSum{all, score, sum};
         kept[wave] = n;
     }
     __syncthreads();
@@ -402,7 +408,7 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
         n = a.take;
     }
     __builtin_amdgcn_wave_barrier();
-    if (lane == 0) a.sums[blockIdx.x] = BeamSum{m, s};
+    if (lane == 0) a.sums[blockIdx.x] = BeamSum{m, score, s};
     if (lane < a.take) a.best[(size_t)blockIdx.x * a.take + lane] = lane < n ? list[lane] : 0;
 }
 
@@ -481,8 +487,8 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
         // (asked for before it is known whether the row has any)
         const BeamSum mine = sums[has ? sixteenth : 0];
         const uint64_t first = first_entry(r, w - r * parts);
-        const float score = a.score[row] + 0.0f;  // (-0 becomes 0: candidates are ranked by c as an integer, in which the zeros differ)
-        const bool alive = score > -kInf, ended = a.done && a.done[row];
+        const float score = mine.score;
+        const bool alive = score > -kInf, ended = mine.sum == kBeamDone;
         float m = -kInf;
         double s = 0.0;
         if (alive && !ended) {

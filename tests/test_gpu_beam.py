@@ -278,3 +278,27 @@ def test_rows_of_many_tiles_in_one_slice_keep_their_sum(form, size):
     for k in range(2):
         want = (x[order[k]] - m) - log_s
         assert abs(float(c[700, k]) - want) <= TOL + 2.0 ** -24 * abs(want), (float(c[700, k]), want)
+
+
+@pytest.mark.parametrize("take", [2, 4, 9])
+def test_results_over_the_inputs_of_other_groups(take):
+    """The library's call, with its results where the scores, the marks and the logits lie: more groups than the card runs at a time, so that
+    some are read long after others are written."""
+    import ctypes as C
+    G, W, V = 3000, 4, 70
+    logits, score = case(40 + take, G, W, V, "fp32")
+    done = (torch.rand((G, W), generator=torch.Generator(device=DEV).manual_seed(take), device=DEV) < 0.2).to(torch.uint8)
+    want = F.floe_beam_select(logits, score, take=take, done=done, eos=5)
+    scores, ends, wide = torch.zeros((G * max(W, take),), device=DEV), torch.zeros((G * max(W, take),), dtype=torch.uint8, device=DEV), logits.clone()
+    scores[:G * W], ends[:G * W] = score.view(-1), done.view(-1)
+    flat = wide.view(-1).view(torch.int32)
+    parent, token = flat[:G * take], flat[G * take:2 * G * take]
+    lib, b = F.binding.load(), F.binding._Beam(G, W, V, take, 2, 5)
+    space = torch.empty((lib.floe_beam_workspace_bytes(C.byref(b)),), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    rc = lib.floe_beam_select(C.byref(b), wide.data_ptr(), V, scores.data_ptr(), ends.data_ptr(), scores.data_ptr(), parent.data_ptr(), token.data_ptr(), ends.data_ptr(),
+                              space.data_ptr(), space.numel(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == 0
+    for got, w in zip((scores, parent, token, ends), want):
+        assert torch.equal(got[:G * take], w.view(-1))

@@ -290,3 +290,13 @@ def test_reorder_refuses_outputs_over_the_other_input_and_over_each_other(lib):
     if not torch.cuda.is_available():
         for change in (dict(length=BIG + 24), dict(length=BIG - 8), dict(table=2 * BIG - 24), dict(table=2 * BIG + 8), dict(length_out=BIG + 24), dict(length_out=BIG - 8)):
             assert reorder(lib, **change) == EHIP, change
+
+
+def test_a_selection_whose_results_lie_over_each_other_is_refused(monkeypatch):
+    monkeypatch.setattr(B, "_launches_on", lambda *a: None)
+    x, s, room = torch.zeros((6, 8), dtype=torch.float16), torch.zeros((2, 3)), torch.zeros(20, dtype=torch.int32)
+    part = lambda i: room[i:i + 6].view(2, 3)  # noqa: E731
+    for more in (dict(parent=part(0), token=part(5)), dict(token=part(0), parent=part(5)), dict(score_out=part(3).view(torch.float32), token=part(0)),
+                 dict(done_out=room.view(torch.uint8)[23:29].view(2, 3), parent=part(0)), dict(parent=part(2), token=part(2))):
+        with pytest.raises(ValueError, match="over another result"):
+            F.floe_beam_select(x, s, **more)
