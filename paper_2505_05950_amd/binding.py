@@ -628,6 +628,13 @@ class Rope:
                                  self.interleaved)
 
 
+def _fits(n: int, name: str) -> int:
+    """A number for a 32-bit argument (ctypes would hand over its lower bits)."""
+    if -0x80000000 <= n <= 0x7fffffff:
+        return n
+    raise ValueError(f"{name}: {n} does not fit 32 bits")
+
+
 def _launches_on(device: int, stream, what: str):
     """The library launches on the current device, and a stream is one device's: both have to be the one that the memory is on."""
     if device < 0:
@@ -764,6 +771,8 @@ def floe_kv_attention(cache: KVCache, q, cu_rows, length, block_table, max_rows:
     if want_lse or lse is not None:
         lse = _kv_out(lse, cache, (n_rows, heads), torch.float32, q, "lse", stream)
     call, need = _kv_calls()[2:]
+    if sinks:
+        _fits(sinks, "sinks")
     s = _kv_seqs(cache, cu_rows, length, block_table, n_rows, max_rows, stream)
     a = _ATTENTION_FIELDS.pack(heads, causal, window, max_len, cache.head_dim ** -0.5 if scale is None else scale)
     if workspace is not None and workspace.get_device() != cache._device:
@@ -818,7 +827,7 @@ class KVPool:
     hold the addresses of refs and, unless handed a workspace, of the pool's own: the pool lives as long as their graphs."""
 
     def __init__(self, n_pages: int, block: int = 64, refs=None, device="cuda"):
-        self.n_pages, self.block = int(n_pages), int(block)
+        self.n_pages, self.block = _fits(int(n_pages), "KVPool: n_pages"), _fits(int(block), "KVPool: block")
         if self.n_pages < 1:
             raise ValueError(f"KVPool: at least one page, not {n_pages}")
         if refs is None:
@@ -851,7 +860,7 @@ class KVPool:
         if len(shape) != 2:
             raise ValueError(f"table: expected int32 [sequences][blocks], got {tuple(shape)}")
         _launches_on(self._device, stream, "the pool")
-        return _i32(table, shape, self._device, "table"), shape[0], shape[1]
+        return _i32(table, shape, self._device, "table"), _fits(shape[0], "table: sequences"), _fits(shape[1], "table: blocks")
 
 
 def _given_or_new(t, shape, pool, like, name, stream):
@@ -865,7 +874,7 @@ def floe_kv_reorder(pool: KVPool, table, length, parent, table_out=None, length_
     """Sequence i takes over the pages and the length of sequence parent[i] (outside the table: none); `table` is no longer in use afterwards.
     Returns (table_out, length_out)."""
     at, n, blocks = pool._table(table, stream)
-    m = parent.numel()
+    m = _fits(parent.numel(), "parent")
     length_at, parent_at = _i32(length, (n,), pool._device, "length"), _i32(parent, (m,), pool._device, "parent")
     table_out = _given_or_new(table_out, (m, blocks), pool, table, "table_out", stream)
     length_out = _given_or_new(length_out, (m,), pool, table, "length_out", stream)
@@ -894,7 +903,8 @@ def floe_kv_trim(pool: KVPool, table, length, window: int = 0, sinks: int = 0, s
     """Gives back the blocks of `table` that no query behind `length` tokens sees: all behind the end, and with a window those before it
     that hold none of the first `sinks` tokens."""
     at, n, blocks = pool._table(table, stream)
-    rc = _page_calls()[2](pool._at, at, _i32(length, (n,), pool._device, "length"), n, blocks, sinks, window, _stream(stream))
+    rc = _page_calls()[2](pool._at, at, _i32(length, (n,), pool._device, "length"), n, blocks, _fits(sinks, "sinks"), _fits(window, "window"),
+                          _stream(stream))
     if rc:
         _check(rc, "floe_kv_trim")
 
@@ -903,7 +913,7 @@ def floe_kv_compact(pool: KVPool, table, max_moves: int = None, pairs=None, page
     """Moves the highest used pages to the lowest free ones (max_moves at most: as many as there are pages by default); the pool and `table`
     follow at once.  Returns (pairs int32 [max_moves][2], what floe_kv_copy_pages has to copy; page_map int32 [n_pages], where each page went)."""
     at, n, blocks = pool._table(table, stream)
-    moves = pool.n_pages if max_moves is None else int(max_moves)
+    moves = pool.n_pages if max_moves is None else _fits(int(max_moves), "max_moves")
     pairs = _given_or_new(pairs, (moves, 2), pool, table, "pairs", stream)
     page_map = _given_or_new(page_map, (pool.n_pages,), pool, table, "page_map", stream)
     st = _stream(stream)
@@ -923,7 +933,7 @@ def floe_kv_copy_pages(caches, pairs, stream=None):
     if any(c._device != dev for c in caches):
         raise ValueError("floe_kv_copy_pages: the caches are on one device")
     _launches_on(dev, stream, "the cache")
-    n = pairs.shape[0] if pairs.dim() else 0
+    n = _fits(pairs.shape[0], "pairs") if pairs.dim() else 0
     at = _i32(pairs, (n, 2), dev, "pairs")
     rc = _page_calls()[4](b"".join([bytes(c._c) for c in caches]), len(caches), at, n, _stream(stream))
     if rc:

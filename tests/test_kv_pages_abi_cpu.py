@@ -300,3 +300,26 @@ def test_a_selection_whose_results_lie_over_each_other_is_refused(monkeypatch):
                  dict(done_out=room.view(torch.uint8)[23:29].view(2, 3), parent=part(0)), dict(parent=part(2), token=part(2))):
         with pytest.raises(ValueError, match="over another result"):
             F.floe_beam_select(x, s, **more)
+
+
+@pytest.mark.parametrize("value", [1 << 32, (1 << 32) + 3, 1 << 31, -(1 << 31) - 1, -(1 << 32)])
+def test_the_binding_refuses_numbers_that_do_not_fit_the_call(monkeypatch, value):
+    """ctypes cuts integers to 32 bits without a word: 2^32 first tokens would have been none."""
+    monkeypatch.setattr(B, "_launches_on", lambda *a: None)
+    reached = lambda *a: pytest.fail("the library was called")  # noqa: E731
+    monkeypatch.setattr(B, "_page_calls", lambda: (reached,) * 5)
+    monkeypatch.setattr(B, "_kv_calls", lambda: (reached,) * 4)
+    monkeypatch.setattr(B, "_kv_seqs", lambda *a: b"")
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    p, t, n = F.KVPool(4, 32, device="cpu"), torch.zeros((2, 3), dtype=torch.int32), i32(5, 6)
+    c, q = F.KVCache(4, 1, 64, 32, device="cpu"), torch.zeros((1, 1, 64), dtype=torch.float16)
+    for call in (lambda: F.floe_kv_attention(c, q, i32(0, 1), i32(1), t[:1], 1, 9, window=5, sinks=value), lambda: F.floe_kv_trim(p, t, n, sinks=value),
+                 lambda: F.floe_kv_trim(p, t, n, window=value), lambda: F.floe_kv_compact(p, t, value), lambda: F.KVPool(4, value + 32 * (value > 0), refs=i32(0, 0, 0, 0))):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    class Long:  # (a tensor of as many rows, as far as its sizes go)
+        dtype, shape = torch.int32, (abs(value) + 2 ** 32, 3)
+        is_contiguous, get_device, data_ptr, numel, dim = (lambda s: True), (lambda s: -1), (lambda s: 64), (lambda s: s.shape[0]), (lambda s: 2)
+    for call in (lambda: F.floe_kv_trim(p, Long(), n), lambda: F.floe_kv_copy_pages(c, Long()), lambda: F.floe_kv_reorder(p, t, n, Long())):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
