@@ -523,7 +523,9 @@ int floe_kv_attention_sinks(const floe_kv_cache* c, const floe_kv_seqs* s, const
  * The pages of such caches.  A model's layers share one set of tables: page p of every layer's cache belongs to the same tokens.
  *
  * A pool counts, for each page, the table entries that name it (of all tables that are in use); a page is free where that count is not
- * positive.  The caller fills refs with zeros once, then only these calls change it (a page that nobody may be given: a count of its own).
+ * positive.  The caller fills refs with zeros once, then only these calls change it.  A count that the caller adds by itself holds a page as a
+ * table entry does: it is given to nobody, but floe_kv_compact moves it like any other, and page_map says where to.  (Pages 0 .. n - 1 that
+ * are all held that way stay where they are.)
  * Everything stays on the device: no call looks at a result on the host, so a whole step can be captured.  The same state and call give
  * the same tables.
  *   refs  dev int32 [n_pages], 16-byte aligned

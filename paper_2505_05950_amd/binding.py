@@ -911,7 +911,8 @@ def floe_kv_trim(pool: KVPool, table, length, window: int = 0, sinks: int = 0, s
 
 def floe_kv_compact(pool: KVPool, table, max_moves: int = None, pairs=None, page_map=None, workspace=None, stream=None):
     """Moves the highest used pages to the lowest free ones (max_moves at most: as many as there are pages by default); the pool and `table`
-    follow at once.  Returns (pairs int32 [max_moves][2], what floe_kv_copy_pages has to copy; page_map int32 [n_pages], where each page went)."""
+    follow at once.  Returns (pairs int32 [max_moves][2], what floe_kv_copy_pages has to copy; page_map int32 [n_pages], where each page went:
+    also those that the caller holds by a count of its own, or by other tables)."""
     at, n, blocks = pool._table(table, stream)
     moves = pool.n_pages if max_moves is None else _fits(int(max_moves), "max_moves")
     pairs = _given_or_new(pairs, (moves, 2), pool, table, "pairs", stream)

@@ -350,3 +350,33 @@ def test_pages_that_lie_behind_32_bits_of_bytes():
     for t in (cache.k, cache.v):
         assert torch.equal(t[5], t[n - 2]) and torch.equal(t[n - 1], t[3]) and int(t[5].sum()) > 0
     assert bool((cache.k_scale[5] == 2.0).all()) and bool((cache.v_scale[5] == 3.0).all())
+
+
+@pytest.mark.parametrize("spare", [60, 9000])
+def test_pages_that_the_caller_holds_are_followed_through_a_packing(spare):
+    """Counts without a table entry: the lowest pages stay, a high one moves with its bytes to where the map says, and no reserve hands any of them out."""
+    ref, table, length, rng = state(3, 12, 32, 300, spare)
+    low, high = [0, 1, 2], [ref.n - 1, ref.n - 7]
+    pages = iter([p for p in range(3, ref.n) if p not in high])
+    table = [[next(pages) * 3 // 2 + 3 if e >= 0 else -1 for e in row] for row in table]  # (some free ones between)
+    ref.count(table)
+    for p in low + high:
+        assert ref.refs[p] == 0
+        ref.refs[p] = 1
+    cache = F.KVCache(ref.n, 1, 64, 32)
+    for t in (cache.k, cache.v):
+        t.copy_(torch.randint(0, 256, t.shape, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV, dtype=torch.uint8))
+    held = [cache.k[p].clone() for p in low + high]
+    pool, t = device_pool(ref), i32(table)
+    pairs, where = F.floe_kv_compact(pool, t, 400)
+    F.floe_kv_copy_pages(cache, pairs)
+    want = ref.compact(table, 400)
+    same(pool, t, ref, table)
+    assert pairs.tolist() == want[0] and where.tolist() == want[1]
+    now = [int(where[p]) for p in low + high]
+    assert now[:3] == low and now[3] != high[0] and now[4] != high[1]
+    assert all(torch.equal(cache.k[p], b) for p, b in zip(now, held))
+    n = 40
+    wide = torch.full((1, n), -1, dtype=torch.int32, device=DEV)
+    _, missing = F.floe_kv_reserve(pool, wide, i32([0]), cu_of([32 * n]))
+    assert missing.item() == 0 and not set(now) & set(wide[0].tolist())
