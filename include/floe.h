@@ -554,10 +554,12 @@ int floe_kv_reorder(const floe_kv_pool* p, const int32_t* table, const int32_t* 
  *   a page, if its entry is absent
  *   a page of its own, if others name the one that it has (count > 1).  Where all that name it are sequences of this call which write
  *   to it, the first of them keeps it.  If the block already holds tokens of the sequence (the block of len[s], len[s] not a multiple of
- *   block), pairs[s] = (old page, new page): what has to be copied, by floe_kv_copy_pages, before the append.  Otherwise pairs[s] = (-1, -1).
+ *   block), pairs[s] = (old page, new page): what has to be copied, by floe_kv_copy_pages, before the append and before any other call on
+ *   the pool (also where blocks are missing: a repeated call names only its own pairs, and the old page may be given back and out again
+ *   in between).  Otherwise pairs[s] = (-1, -1).
  * Pages are handed out from the lowest free one on, in the order of (sequence, block).
  * missing dev int32 [1]: blocks that got no page since none was free or since they lie behind max_blocks (those up to 2^20).  Their entries
- * stay as they were, so that the call can be made again when pages are free; nothing may be appended before that.
+ * stay as they were, so that the call can be made again when its pairs are copied and pages are free; nothing may be appended before that.
  * pairs dev int32 [n_seqs][2].  workspace: dev, 256-byte aligned, contents are scratch.  One launch.
  */
 size_t floe_kv_reserve_workspace_bytes(const floe_kv_pool* p);

@@ -886,7 +886,8 @@ def floe_kv_reorder(pool: KVPool, table, length, parent, table_out=None, length_
 
 def floe_kv_reserve(pool: KVPool, table, length, cu_rows, pairs=None, missing=None, workspace=None, stream=None):
     """Gives every block that an append of cu_rows behind `length` tokens writes to a page that only its sequence names.  Returns (pairs
-    int32 [sequences][2], what floe_kv_copy_pages has to copy before the append; missing int32 [1], blocks that got no page)."""
+    int32 [sequences][2], what floe_kv_copy_pages has to copy before the append and before any other call on the pool; missing int32 [1],
+    blocks that got no page: nothing is appended then, but what the pairs name is copied all the same)."""
     at, n, blocks = pool._table(table, stream)
     length_at, cu_at = _i32(length, (n,), pool._device, "length"), _i32(cu_rows, (n + 1,), pool._device, "cu_rows")
     pairs = _given_or_new(pairs, (n, 2), pool, table, "pairs", stream)

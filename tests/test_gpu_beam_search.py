@@ -108,3 +108,38 @@ def test_streams_that_give_their_pages_back_see_what_they_would_see_with_all_of_
         assert torch.equal(pool.refs, names_of(pool, table))
         most_used = max(most_used, int((pool.refs > 0).sum()))
     assert int(length.max()) > 200 and most_used <= B * (-(-sinks // P) + window // P + 2)
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_a_reserve_that_missed_pages_is_repeated_when_some_are_free(fmt):
+    """Two sequences share a begun block, a third needs a page that is not there: what the first call named is copied, a fourth sequence ends,
+    and the call is made again.  Each sequence then reads what a cache of its own holds, bit for bit."""
+    import paper_2505_05950_amd as F
+    P, heads, dim = 32, 2, 64
+    g = torch.Generator(device=DEV).manual_seed(6)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    new = lambda n: [torch.randn((n, heads, dim), generator=g, device=DEV).half() for _ in range(2)]  # noqa: E731
+    cache, pool = F.KVCache(5, heads, dim, P, fmt), F.KVPool(5, P)
+    prompt, other, cu = new(20), new(64), i32([0, 20, 84, 94])
+    k, v = (torch.cat(x) for x in zip(prompt, other, new(10)))
+    t, before = torch.full((3, 4), -1, dtype=torch.int32, device=DEV), i32([0, 0, 0])
+    F.floe_kv_reserve(pool, t, before, cu)
+    F.floe_kv_append(cache, k, v, cu, before, t, 64)
+    t, length = F.floe_kv_reorder(pool, t, i32([20, 64, 10]), i32([0, 0, 1, 2]))
+    k, v = new(3)
+    pairs, missing = F.floe_kv_reserve(pool, t, length, i32([0, 1, 2, 3, 3]))
+    F.floe_kv_copy_pages(cache, pairs)
+    assert missing.item() == 1 and pairs.tolist() == [[-1, -1], [0, 4], [-1, -1], [-1, -1]]
+    F.floe_kv_trim(pool, t, i32([20, 20, 64, 0]))
+    length = i32([20, 20, 64, 0])
+    pairs, missing = F.floe_kv_reserve(pool, t, length, i32([0, 1, 2, 3, 3]))
+    F.floe_kv_copy_pages(cache, pairs)
+    assert missing.item() == 0 and bool((pairs == -1).all()) and t[:, 0].tolist() == [0, 4, 1, -1] and t[2, 2].item() == 3
+    F.floe_kv_append(cache, k, v, i32([0, 1, 2, 3, 3]), length, t, 1)
+    for s, (old_k, old_v) in enumerate((prompt, prompt, other)):
+        alone, table, n = F.KVCache(3, heads, dim, P, fmt), i32([[0, 1, 2]]), old_k.shape[0]
+        F.floe_kv_append(alone, old_k, old_v, i32([0, n]), i32([0]), table, n)
+        F.floe_kv_append(alone, k[s:s + 1], v[s:s + 1], i32([0, 1]), i32([n]), table, 1)
+        got = F.floe_kv_gather(cache, i32([0]), i32([0, n + 1]), t[s:s + 1].contiguous(), n + 1, n + 1)
+        want = F.floe_kv_gather(alone, i32([0]), i32([0, n + 1]), table, n + 1, n + 1)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), s
