@@ -571,6 +571,9 @@ int floe_kv_reserve(const floe_kv_pool* p, int32_t* table, const int32_t* len, c
  *   window == 0,  or t > len[s] - window (seen by the query at position len[s]),  or t < sinks
  * Other entries become -1 and their pages lose a count: blocks that left the window, blocks behind the end (reserved, or of drafts that were
  * rejected), all blocks of a sequence of length 0.  One launch.
+ * With window 1 the block that the next token goes to may go too, although it holds older ones: an append behind those keeps to the scale
+ * that it finds, and a page that is handed out anew has somebody else's.  Sequences that go on are trimmed with a window of at least 2,
+ * whatever the attention's is; one whose last d tokens may still be taken back, with a window larger by d.
  */
 int floe_kv_trim(const floe_kv_pool* p, int32_t* table, const int32_t* len, int n_seqs, int max_blocks, int sinks, int window, void* stream);
 

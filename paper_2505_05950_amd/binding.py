@@ -902,7 +902,7 @@ def floe_kv_reserve(pool: KVPool, table, length, cu_rows, pairs=None, missing=No
 
 def floe_kv_trim(pool: KVPool, table, length, window: int = 0, sinks: int = 0, stream=None):
     """Gives back the blocks of `table` that no query behind `length` tokens sees: all behind the end, and with a window those before it
-    that hold none of the first `sinks` tokens."""
+    that hold none of the first `sinks` tokens.  Sequences that go on: a window of 2 or more, which keeps the block that is begun (floe.h)."""
     at, n, blocks = pool._table(table, stream)
     rc = _page_calls()[2](pool._at, at, _i32(length, (n,), pool._device, "length"), n, blocks, _fits(sinks, "sinks"), _fits(window, "window"),
                           _stream(stream))

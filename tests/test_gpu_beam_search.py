@@ -143,3 +143,30 @@ def test_a_reserve_that_missed_pages_is_repeated_when_some_are_free(fmt):
         got = F.floe_kv_gather(cache, i32([0]), i32([0, n + 1]), t[s:s + 1].contiguous(), n + 1, n + 1)
         want = F.floe_kv_gather(alone, i32([0]), i32([0, n + 1]), table, n + 1, n + 1)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), s
+
+
+@pytest.mark.parametrize("sinks", [0, 5])
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_windows_of_one_token_keep_the_block_that_is_begun(fmt, sinks):
+    """Attention with a window of 1, pages given back with a window of 2: the scale of the begun block stays, and the outputs are those of a cache that
+    keeps everything.  Pages that nobody has used hold NaN scales: an append to one of them that it takes for begun would show."""
+    import paper_2505_05950_amd as F
+    P, heads, dim, B, steps = 32, 2, 64, 3, 80
+    g = torch.Generator(device=DEV).manual_seed(8)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    small, large = F.KVCache(40, heads, dim, P, fmt), F.KVCache(B * 5, heads, dim, P, fmt)
+    small.k_scale.fill_(float("nan"))
+    small.v_scale.fill_(float("nan"))
+    pool, table, whole = F.KVPool(40, P), torch.full((B, 5), -1, dtype=torch.int32, device=DEV), torch.arange(B * 5, dtype=torch.int32, device=DEV).view(B, 5)
+    length, cu = i32([0] * B), i32([0, 1, 2, 3])
+    for step in range(steps):
+        k, v, q = (torch.randn((B, h, dim), generator=g, device=DEV).half() * (1 + step % 7) for h in (heads, heads, 4))
+        pairs, missing = F.floe_kv_reserve(pool, table, length, cu)
+        assert int(missing) == 0 and bool((pairs == -1).all())
+        for c, t in ((small, table), (large, whole)):
+            F.floe_kv_append(c, k, v, cu, length, t, 1)
+        length = length + 1
+        out = [F.floe_kv_attention(c, q, cu, length, t, 1, 5 * P, window=1, sinks=sinks) for c, t in ((small, table), (large, whole))]
+        assert torch.equal(*out) and bool(torch.isfinite(out[0]).all()), step
+        F.floe_kv_trim(pool, table, length, window=2, sinks=sinks)
+        assert int((pool.refs > 0).sum()) <= B * (2 if sinks else 1), step
