@@ -242,7 +242,10 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
     // mask and running maximum of the tile
     auto maximum = [&](int t0, bool masked, bool of_first) {
         if (masked) {
-            const int from = SINKS && of_first ? 0 : first_key, to = SINKS && of_first ? min(last_key, a.sinks - 1) : last_key;
+            int from = first_key, to = last_key;
+            if constexpr (SINKS) {  // (a condition on SINKS inside an expression takes registers in the instances without it too)
+                if (of_first) from = 0, to = min(last_key, a.sinks - 1);
+            }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const bool poisoned = !(ks[u] == ks[u]) || !(vs[u] == vs[u]);  // a NaN scale: NaN for whoever sees a token, nothing for others
@@ -365,10 +368,12 @@ __global__ __launch_bounds__(64 * NW, D >= 192 && NW == 4 ? 1 : 2) void kv_promp
             const float k_scale = gloadf(a.c.k_scale + slot), v_scale = gloadf(a.c.v_scale + slot);
             const bool poisoned = !(k_scale == k_scale) || !(v_scale == v_scale);
             const float by = fmaxf(row_scale * k_scale, 0x1p-126f), from = poisoned ? __builtin_nanf("") : off;
-            const bool of_first = SINKS && (unit >> 1) < sunk;
-            const int from_key = of_first ? 0 : first_key, to_key = of_first ? min(last_key, a.sinks - 1) : last_key;
+            int from_key = first_key, to_key = last_key;
+            if constexpr (SINKS) {
+                if ((unit >> 1) < sunk) from_key = 0, to_key = min(last_key, a.sinks - 1);
+            }
             const bool none = to_key < from_key;
-            const int lo = (none ? t0 + 2 * kPromptTokens : from_key) - (t0 + 4 * h);
+            const int lo = (none ? start + 2 * (unit + 2) * kKvGroup : from_key) - (t0 + 4 * h);
             const uint32_t more = none ? 0 : to_key - from_key;
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
