@@ -87,7 +87,7 @@ typedef enum {
     FLOE_KERNEL_KV_REORDER = 14,
     FLOE_KERNEL_KV_TRIM = 15,
     FLOE_KERNEL_KV_RESERVE = 16,
-    FLOE_KERNEL_KV_COMPACT = 17, /* its three launches together */
+    FLOE_KERNEL_KV_COMPACT = 17, /* its launches together: three, one for small pools and tables */
     FLOE_KERNEL_KV_COPY = 18,    /* likewise, of a call with more caches than a launch takes */
     FLOE_KERNEL_BEAM_ROWS = 19,  /* one pass over the logits */
     FLOE_KERNEL_BEAM_GROUPS = 20 /* the groups' best of their rows' best */

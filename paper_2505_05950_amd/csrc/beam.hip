@@ -58,7 +58,7 @@ __device__ __forceinline__ double wave_sum64(double x) {
 // The largest T that at least `k` of the wave's 64 N values reach (0 if there are fewer), in bits `low` to `high`, with `t` above them
 template <int N>
 __device__ __forceinline__ uint32_t wave_kth(const uint32_t (&v)[N], int k, int low, int high = 31, uint32_t t = 0) {
-#pragma unroll 1  // (unrolled, the kernels outgrow the instruction cache: 120 rows of 50257 in bf16 20 us instead of 12)
+#pragma unroll 1  // (unrolled, 53 KB more code: 120 rows of 50257 in bf16 take 8.8 us either way, 512 of 131072 in fp32 57 instead of 59)
     for (int bit = high; bit >= low; --bit) {
         const uint32_t c = t | (1u << bit);
         int n = 0;
@@ -275,8 +275,8 @@ __global__ __launch_bounds__(kBeamThreads) void beam_rows_kernel(BeamArgs a) {
         // (a NaN where a wave has too few values: the comparison with it leaves the bar)
         return value_of(min(min((uint32_t)a, (uint32_t)(a >> 32)), min((uint32_t)b, (uint32_t)(b >> 32))));
     };
-    // Entries from which on the list is looked at.  us, 512 rows, one threshold from the first tile on / this: 131072 in fp32, 64 taken 60 / 53, 8 taken
-    // 52 / 42, in bf16, 16 taken 43 / 36 (40 and 24 without any candidates).
+    // Entries from which on the list is looked at.  us, 512 rows of 131072, one threshold from the first tile on / this / no candidates at all: in fp32,
+    // 64 taken 63 / 59 / 47, 8 taken 60 / 51 / 48, in bf16, 16 taken 43 / 38 / 29.
     int limit = min(kWave, max(16, 2 * quota));
     auto push = [&](int t0) {
         float best = most[0];
@@ -616,7 +616,7 @@ __global__ __launch_bounds__(kGroupThreads) void beam_groups_kernel(BeamArgs a) 
 }  // namespace
 
 // Tiles of one load per lane where these are few: a wave's way is shorter then; else of four.  us, one / four, 16-bit logits: 4 rows of
-// 32000 3.8 / 4.7, 64 rows 4.5 / 5.3, 120 rows of 50257 10.0 / 7.8, 128 rows of 65536 10.6 / 7.2.
+// 32000 4.6 / 5.8, 64 rows 5.8 / 7.2, 120 rows of 50257 12.2 / 8.9, 128 rows of 65536 12.0 / 8.7.
 // A slice is a multiple of what a workgroup's four waves take at a time, as large as leaves every compute unit four workgroups.
 BeamCut beam_cut(int rows, int vocab, int dtype) {
     const int one = kBeamWaves * kWave * (dtype == 2 ? 4 : 8);

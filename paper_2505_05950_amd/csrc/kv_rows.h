@@ -7,7 +7,8 @@
 // whatever the scales are.  The exponent's base of a row is set so that its largest weight is 2^14, and set again only when a weight would
 // pass 2^15 (after the first tokens it hardly ever is): fp16 holds the weights, down to 2^-38 of the largest.  Their rounding is what
 // the result is off by beside its own: 2.2e-4 of it in all with fp16 outputs (2.1e-4 is the rounding of the output), 2.5e-4 when the
-// base is set to 2^7, which costs 1 % less time on long prompts.  Queries in bf16 are scaled per row by a power of two into fp16's range.
+// base is set to 2^7, which costs 1 % less time on long prompts; where few tokens have most of a row's weight 2.5e-4 to 2.9e-4, and with bf16
+// outputs, whose rounding is 1.7e-3, nothing that shows.  Queries in bf16 are scaled per row by a power of two into fp16's range.
 //
 // The sum below the line does without V's scale, and the scales of a sequence can lie 181 powers of two apart (2^-60 is an append's least
 // one, a block of the largest bf16 values has 2^121): a token whose weight times scale binary32 no longer holds can have all of the
